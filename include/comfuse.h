@@ -61,7 +61,8 @@ extern "C" {
 typedef enum {
   CF_F32 = 0,       /* IEEE binary32 */
   CF_BF16 = 1,      /* bfloat16 */
-  CF_FP8_E4M3 = 2   /* OCP E4M3FN: bias 7, max 448, no infinities */
+  CF_FP8_E4M3 = 2,  /* OCP E4M3FN: bias 7, max 448, no infinities */
+  CF_I8 = 3         /* two's complement integers of 8 bits */
 } cf_dtype;
 
 typedef enum {
@@ -314,6 +315,117 @@ cf_status cf_gemm(int64_t batch, int64_t M, int64_t N, int64_t K,
 cf_status cf_rowop(int64_t batch, int64_t M, int64_t N, cf_dtype in,
                    const void* P, int64_t ldp, int64_t sp,
                    const cf_node* nodes, int n_nodes, void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * cf_rmsnorm_quant — residual addition, RMSNorm and 8-bit codes in one pass
+ * over the rows, the form in which cf_gemm_i8 takes its tokens:
+ *
+ *     h = X + R                         (fp32; H = h rounded to dtype)
+ *     t = h * gamma,  d = max_n |t| / qmax        (qmax: 127 I8, 448 E4M3)
+ *     Q = code(t / d),  s = d / sqrt(mean(h^2) + eps)
+ *
+ * so that Q * s stands for the normed row h / sqrt(mean(h^2) + eps) * gamma.
+ * The row's norm cancels in t / d: the codes do not depend on the order of the
+ * sum of squares.  t / d is the IEEE quotient in fp32, rounded to the nearest
+ * code, ties to even.  norm = 0 leaves the norm out (s = d): plain
+ * quantisation of the rows.
+ *
+ * X, R (NULL: 0) and H (NULL: not wanted) are M x N in dtype F32 or BF16,
+ * gamma fp32 [N] or NULL (1), Q M x N of code_dtype I8 or FP8_E4M3 (a byte an
+ * element, ldq a multiple of 16), s fp32 [M].  1 <= N <= 32768; bytes between N
+ * and a leading dimension are neither used nor written.  H may be R itself
+ * (same pointer and ld): the residual stream is then updated in place.
+ * A row whose t is all zero gets s = 0 and zero codes; a row in which some t
+ * is NaN or infinite gets s = NaN and zero codes.  The mean of squares is held
+ * in fp32: s is 0 where it overflows (|h| about 1.8e19 and more).
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  size_t struct_size;            /* = sizeof(cf_rmsnorm_quant_args) */
+  int64_t M, N;
+  cf_dtype dtype;
+  const void* X; int64_t ldx;
+  const void* R; int64_t ldr;
+  void* H; int64_t ldh;
+  const float* gamma;
+  int norm;                      /* 1: RMSNorm, 0: quantise t as it is */
+  float eps;
+  cf_dtype code_dtype;
+  void* Q; int64_t ldq;
+  float* s;
+} cf_rmsnorm_quant_args;
+
+cf_status cf_rmsnorm_quant(const cf_rmsnorm_quant_args* a, void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * cf_gemm_i8 — matrix product of 8-bit integers with a scale for each token
+ * (row of A) and each channel (row of B):
+ *
+ *     C = act(float(sum_k A[m,k] B[n,k]) * sa[m] * sb[n] + bias[n])
+ *
+ * A M x K and B N x K (CF_LAYOUT_NK) of I8, sa fp32 [M], sb fp32 [N] (NULL: 1),
+ * bias fp32 [N] or NULL, C M x N in out_dtype F32 or BF16.  The sum is exact (32-bit integers;
+ * hence K <= 131056) and its conversion, the scales and act are fp32.
+ * Shape rules: K % 16 == 0; N >= 1 any; columns between N and ldc are left as
+ * they are.  act: none, GELU (erf), GELU_TANH or RELU.
+ * ------------------------------------------------------------------------ */
+typedef enum { CF_ACT_NONE = 0, CF_ACT_GELU = 1, CF_ACT_GELU_TANH = 2, CF_ACT_RELU = 3 } cf_act;
+
+typedef struct {
+  size_t struct_size;            /* = sizeof(cf_gemm_i8_args) */
+  int64_t M, N, K;
+  const void* A; int64_t lda;
+  const void* B; int64_t ldb;
+  const float* sa;
+  const float* sb;
+  const float* bias;
+  cf_act act;
+  cf_dtype out_dtype;
+  void* C; int64_t ldc;
+} cf_gemm_i8_args;
+
+cf_status cf_gemm_i8(const cf_gemm_i8_args* a, void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * cf_attention_prefix — attention of a batch whose sequences share a prefix:
+ * sequence b attends to the P prefix keys, stored once, and to the first
+ * lens[b] of its own keys:
+ *
+ *     O_b = softmax(scale Q_b [Kp; Ks_b]^T) [Vp; Vs_b]
+ *
+ * Q, O: batch x H x Lq rows of d; Kp, Vp: Hk x P rows; Ks, Vs: batch x Hk x S
+ * rows, all bf16, each matrix with its own strides (elements, multiples of 8; rows
+ * have unit stride).  H is a multiple of Hk: query head h reads key head
+ * h / (H / Hk).  d in {64, 128}.  P >= 0, S >= 0; Kp and Vp (Ks and Vs) may be
+ * NULL where P (S) is 0.  lens: int32 [batch] in device memory, or NULL for S
+ * everywhere; values outside [0, S] are clamped.  causal = 1: query i sees the
+ * own keys j < lens[b] - (Lq - 1 - i) (the queries are the sequence's last Lq
+ * tokens); the prefix is visible to all.  A query that sees no key gets O = 0.
+ * Own rows at and behind lens[b] are not used, whatever they hold; an infinity or
+ * NaN in a value row that causal hides from some queries of a call only reaches them too
+ * (as 0 * NaN).  scale finite and > 0.  The softmax is exact (running maximum and sum in fp32);
+ * P is rounded to bf16 for the second product, as in cf_b2bgemm.
+ * Workspace: cf_attention_prefix_workspace() bytes (may be 0), 16-byte aligned,
+ * no initial contents required; it holds partial results during the call
+ * only.  Calls that share it must not overlap in time.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  size_t struct_size;            /* = sizeof(cf_attention_prefix_args) */
+  int64_t batch, H, Hk, Lq, P, S, d;
+  cf_dtype dtype;                /* CF_BF16 */
+  const void* Q;  int64_t q_b, q_h, q_l;      /* strides over batch, head, row */
+  const void* Kp; int64_t kp_h, kp_l;
+  const void* Vp; int64_t vp_h, vp_l;
+  const void* Ks; int64_t ks_b, ks_h, ks_l;
+  const void* Vs; int64_t vs_b, vs_h, vs_l;
+  const int32_t* lens;
+  int causal;
+  float scale;
+  void* O; int64_t o_b, o_h, o_l;
+} cf_attention_prefix_args;
+
+size_t    cf_attention_prefix_workspace(const cf_attention_prefix_args* a);
+cf_status cf_attention_prefix(const cf_attention_prefix_args* a, void* workspace,
+                              size_t ws_bytes, void* hip_stream);
 
 /* ------------------------------------------------------------------------
  * cf_workspace_check — reads and clears the error word of a workspace used by

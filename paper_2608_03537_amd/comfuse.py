@@ -12,6 +12,7 @@ allocate the outputs.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 import threading
 
@@ -19,12 +20,13 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcomfuse.so")
 
 # ---------------------------------------------------------------- enums
-CF_F32, CF_BF16, CF_FP8_E4M3 = 0, 1, 2
+CF_F32, CF_BF16, CF_FP8_E4M3, CF_I8 = 0, 1, 2, 3
 CF_LAYOUT_KN, CF_LAYOUT_NK = 0, 1
 (CF_N_SCALE, CF_N_BIAS, CF_N_RESIDUAL, CF_N_LAYERNORM, CF_N_RMSNORM, CF_N_GELU,
  CF_N_GELU_TANH, CF_N_RELU, CF_N_STORE, CF_N_ROWAMAX_QUANT, CF_N_SOFTMAX, CF_N_SOFTCAP) = range(12)
 CF_MID_GELU_BIAS, CF_MID_SOFTMAX, CF_MID_RELU_BIAS = 0, 1, 2
 CF_OUT_STORE, CF_OUT_BIAS_RESIDUAL_LN, CF_OUT_BIAS_RELU = 0, 1, 2
+CF_ACT_NONE, CF_ACT_GELU, CF_ACT_GELU_TANH, CF_ACT_RELU = 0, 1, 2, 3
 PATH_AUTO, PATH_WHOLE_ROW, PATH_CLUSTER, PATH_SPLIT = 0, 1, 2, 3
 CF_WS_HEADER_BYTES = 8916992       # zero-filled start of a row workspace
 CF_WS_OPTIONAL_BYTES = 8917008     # a workspace query's answer where the workspace may be left out
@@ -67,6 +69,29 @@ class B2BArgs(C.Structure):
                 ("O", vp), ("ldo", i64), ("so", i64)]
 
 
+class RmsnormQuantArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_size_t), ("M", i64), ("N", i64), ("dtype", C.c_int), ("X", vp), ("ldx", i64),
+                ("R", vp), ("ldr", i64), ("H", vp), ("ldh", i64), ("gamma", vp), ("norm", C.c_int),
+                ("eps", C.c_float), ("code_dtype", C.c_int), ("Q", vp), ("ldq", i64), ("s", vp)]
+
+
+class GemmI8Args(C.Structure):
+    _fields_ = [("struct_size", C.c_size_t), ("M", i64), ("N", i64), ("K", i64), ("A", vp), ("lda", i64),
+                ("B", vp), ("ldb", i64), ("sa", vp), ("sb", vp), ("bias", vp), ("act", C.c_int),
+                ("out_dtype", C.c_int), ("C", vp), ("ldc", i64)]
+
+
+class AttentionPrefixArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_size_t), ("batch", i64), ("H", i64), ("Hk", i64), ("Lq", i64), ("P", i64),
+                ("S", i64), ("d", i64), ("dtype", C.c_int),
+                ("Q", vp), ("q_b", i64), ("q_h", i64), ("q_l", i64),
+                ("Kp", vp), ("kp_h", i64), ("kp_l", i64), ("Vp", vp), ("vp_h", i64), ("vp_l", i64),
+                ("Ks", vp), ("ks_b", i64), ("ks_h", i64), ("ks_l", i64),
+                ("Vs", vp), ("vs_b", i64), ("vs_h", i64), ("vs_l", i64),
+                ("lens", vp), ("causal", C.c_int), ("scale", C.c_float),
+                ("O", vp), ("o_b", i64), ("o_h", i64), ("o_l", i64)]
+
+
 class CfError(RuntimeError):
     def __init__(self, status, detail):
         self.status = status
@@ -106,6 +131,13 @@ def lib():
                 L.cf_rowop.argtypes = [i64, i64, i64, C.c_int, vp, i64, i64, C.POINTER(Node), C.c_int, vp]
                 L.cf_gemm_subgraph_noalloc.restype = C.c_int
                 L.cf_gemm_subgraph_noalloc.argtypes = [C.POINTER(SubgraphArgs), vp]
+                for name, argt, ws in [("cf_rmsnorm_quant", RmsnormQuantArgs, False), ("cf_gemm_i8", GemmI8Args, False),
+                                       ("cf_attention_prefix", AttentionPrefixArgs, True)]:
+                    f = getattr(L, name)
+                    f.restype = C.c_int
+                    f.argtypes = [C.POINTER(argt), vp, C.c_size_t, vp] if ws else [C.POINTER(argt), vp]
+                L.cf_attention_prefix_workspace.restype = C.c_size_t
+                L.cf_attention_prefix_workspace.argtypes = [C.POINTER(AttentionPrefixArgs)]
                 L.cf_workspace_check.restype = C.c_int
                 L.cf_workspace_check.argtypes = [vp, C.c_size_t, vp]
                 _lib = L
@@ -156,6 +188,22 @@ def cf_gemm(*args):
 
 def cf_rowop(batch, M, N, dtype, P, ldp, sp, nodes, n_nodes, stream):
     return lib().cf_rowop(batch, M, N, dtype, P, ldp, sp, nodes, n_nodes, stream)
+
+
+def cf_rmsnorm_quant(args, stream):
+    return lib().cf_rmsnorm_quant(C.byref(args), stream)
+
+
+def cf_gemm_i8(args, stream):
+    return lib().cf_gemm_i8(C.byref(args), stream)
+
+
+def cf_attention_prefix(args, workspace, ws_bytes, stream):
+    return lib().cf_attention_prefix(C.byref(args), workspace, ws_bytes, stream)
+
+
+def cf_attention_prefix_workspace(args):
+    return lib().cf_attention_prefix_workspace(C.byref(args))
 
 
 def cf_workspace_check(workspace, ws_bytes, stream):
@@ -224,10 +272,11 @@ def _graph_workspace(nbytes, key, device, stream):
     capture = _capture_id(stream)
     have = _ws_graph.get(key)
     if have is None or capture is None or have[0] != capture or have[1].numel() < nbytes:
-        header = CF_WS_HEADER_BYTES if key[2] == "rows" else CF_B2B_WS_HEADER_BYTES
+        header = {"rows": CF_WS_HEADER_BYTES, "b2b": CF_B2B_WS_HEADER_BYTES}.get(key[2], 0)
         with torch.cuda.stream(stream):
             ws = torch.empty(max(nbytes, header), dtype=torch.uint8, device=device)
-            ws[:header].view(torch.int32).zero_()
+            if header:
+                ws[:header].view(torch.int32).zero_()
         have = _ws_graph[key] = (capture, ws)
     return have[1]
 
@@ -238,7 +287,8 @@ def workspace(nbytes, device, stream=None, kind="rows"):
     share it; calls on different streams get different workspaces (the
     row-cluster round counters live in it).  kind "b2b" is that of the split
     MLP and of attention with split keys (their arrival counters must not meet
-    another entry point's data).  Calls captured into a graph share one of the
+    another entry point's data); "prefix" that of attention_prefix, which needs no
+    initial contents.  Calls captured into a graph share one of the
     capture's own, never an eager one: a graph outlives what the cache holds,
     and its replays may overlap eager calls or another graph."""
     torch = _torch()
@@ -542,4 +592,173 @@ def b2b_attention(Q, K, V, scale=None, out=None, stream=None, ws=None):
     if ws is None:
         ws = _attention_workspace(a, Q.device, stream)
     _check(cf_b2bgemm(a, _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
+    return O
+
+
+# ---------------------------------------------------------------- 8-bit serving path
+# These helpers run on the operands' device, whichever is current, and allocate on
+# the stream that the call uses.
+def _rows(M, N, dtype, device, size):
+    """An [M, N] tensor whose rows start every multiple of 16 bytes (`size`: bytes of an element)."""
+    torch = _torch()
+    per = 16 // size
+    ld = -(-N // per) * per
+    t = torch.empty((M, ld), dtype=dtype, device=device)
+    return t if ld == N else t[:, :N]
+
+
+def _placed(call):
+    """Runs a helper with its first operand's device current, and with `stream`
+    (given: of that device) as the stream that new tensors belong to."""
+    @functools.wraps(call)
+    def placed(X, *args, stream=None, **kw):
+        torch = _torch()
+        device = X.device
+        if device.type != "cuda":
+            raise ValueError(f"expected operands on a GPU, got {device}")
+        if stream is not None:
+            if stream.device != device:
+                raise ValueError(f"operands on {device}, stream of {stream.device}")
+            with torch.cuda.stream(stream):
+                return call(X, *args, stream=stream, **kw)
+        if device.index != torch.cuda.current_device():
+            with torch.cuda.device(device):
+                return call(X, *args, stream=None, **kw)
+        return call(X, *args, stream=None, **kw)
+    return placed
+
+
+def _row_ld(t, size):
+    """Leading dimension of a 2-D tensor with unit column stride; a single row's
+    is free, and taken as the row rounded up to 16 bytes."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] != 1):
+        raise ValueError("expected a 2-D tensor with unit column stride")
+    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] * size // 16) * 16 // size
+
+
+def _vector(t, n, name):
+    torch = _torch()
+    if t is not None and (t.dtype != torch.float32 or t.shape != (n,) or (n > 1 and t.stride(0) != 1)):
+        raise ValueError(f"{name}: expected a contiguous fp32 vector of {n}")
+    return t
+
+
+def _same_device(device, *tensors):
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"operands on {device} and {t.device}")
+
+
+_CODES = {"int8": CF_I8, "e4m3": CF_FP8_E4M3}
+
+
+@_placed
+def rmsnorm_quant(X, R=None, gamma=None, *, eps=1e-5, norm=True, code="int8", residual=None, out=None, scale=None,
+                  stream=None):
+    """(Q, s, H): 8-bit codes and row scales of RMSNorm(X + R) * gamma, and H = X + R.
+
+    X, R [M, N] bf16 or fp32, gamma fp32 [N].  Q is int8 [M, N], or uint8 holding
+    E4M3 codes (code="e4m3"); s fp32 [M]; Q * s stands for the normed row.
+    norm=False quantises the rows as they are.  H is None without R; `residual`
+    names the tensor it goes to, which may be R (in place).  `out` and `scale`
+    take Q and s.  Q is what gemm_i8 takes as its tokens, s as sa.
+    """
+    torch = _torch()
+    M, N = X.shape
+    dt, size = _dt(X), X.element_size()
+    _same_device(X.device, R, gamma, residual, out, scale)
+    for t, name in ((R, "R"), (residual, "residual")):
+        if t is not None and (t.dtype != X.dtype or t.shape != X.shape):
+            raise ValueError(f"{name}: expected {tuple(X.shape)} of {X.dtype}")
+    _vector(gamma, N, "gamma")
+    qdt = torch.int8 if code == "int8" else torch.uint8
+    Q = out if out is not None else _rows(M, N, qdt, X.device, 1)
+    s = scale if scale is not None else torch.empty((M,), dtype=torch.float32, device=X.device)
+    if Q.shape != X.shape or Q.dtype != qdt:
+        raise ValueError(f"out: expected {tuple(X.shape)} of {qdt}")
+    _vector(s, M, "scale")
+    H = residual if residual is not None else None if R is None else _rows(M, N, X.dtype, X.device, size)
+    a = RmsnormQuantArgs(C.sizeof(RmsnormQuantArgs), M, N, dt, X.data_ptr(), _row_ld(X, size),
+                         _ptr(R), 0 if R is None else _row_ld(R, size), _ptr(H), 0 if H is None else _row_ld(H, size),
+                         _ptr(gamma), 1 if norm else 0, eps, _CODES[code], Q.data_ptr(), _row_ld(Q, 1), s.data_ptr())
+    _check(cf_rmsnorm_quant(a, _stream(stream)))
+    return Q, s, H
+
+
+_ACTS = {"none": CF_ACT_NONE, "gelu": CF_ACT_GELU, "gelu_tanh": CF_ACT_GELU_TANH, "relu": CF_ACT_RELU}
+
+
+@_placed
+def gemm_i8(A, B, sa=None, sb=None, *, bias=None, act="none", out_dtype=None, out=None, stream=None):
+    """C = act((A . B^T) * sa[:, None] * sb + bias) of int8 A [M, K] and B [N, K].
+
+    sa fp32 [M] (a scale per token), sb fp32 [N] (per channel), bias fp32 [N];
+    act "none", "gelu", "gelu_tanh" or "relu"; C bf16 (or fp32) [M, N].
+    """
+    torch = _torch()
+    M, K = A.shape
+    N = B.shape[0]
+    if A.dtype != torch.int8 or B.dtype != torch.int8:
+        raise TypeError(f"expected int8 operands, got {A.dtype} and {B.dtype}")
+    if B.shape != (N, K):
+        raise ValueError(f"B: expected [N, {K}], got {tuple(B.shape)}")
+    _same_device(A.device, B, sa, sb, bias, out)
+    _vector(sa, M, "sa")
+    _vector(sb, N, "sb")
+    _vector(bias, N, "bias")
+    if out is None:
+        dt = out_dtype or torch.bfloat16
+        Cm = _rows(M, N, dt, A.device, 4 if dt == torch.float32 else 2)
+    else:
+        Cm = out
+        if Cm.shape != (M, N):
+            raise ValueError(f"out: expected {(M, N)}, got {tuple(Cm.shape)}")
+    a = GemmI8Args(C.sizeof(GemmI8Args), M, N, K, A.data_ptr(), _row_ld(A, 1), B.data_ptr(), _row_ld(B, 1),
+                   _ptr(sa), _ptr(sb), _ptr(bias), _ACTS[act], _dt(Cm), Cm.data_ptr(), _row_ld(Cm, Cm.element_size()))
+    _check(cf_gemm_i8(a, _stream(stream)))
+    return Cm
+
+
+@_placed
+def attention_prefix(Q, Kp, Vp, Ks=None, Vs=None, lens=None, *, causal=False, scale=None, out=None, ws=None,
+                     stream=None):
+    """O = softmax(scale * Q [Kp; Ks]^T) [Vp; Vs] for sequences that share the prefix Kp, Vp.
+
+    Q [B, H, Lq, d]; Kp, Vp [Hk, P, d], one copy for the batch; Ks, Vs
+    [B, Hk, S, d], of which sequence b uses the first lens[b] (int32 [B] on the
+    device; None: all S); bf16, d 64 or 128, H a multiple of Hk, any strides that
+    are multiples of 8 elements with unit innermost stride (caches stored
+    token-major are passed as transposed views).  causal: query i sees the own
+    keys j < lens[b] - (Lq - 1 - i).  A query that sees no key gets 0.
+    """
+    torch = _torch()
+    B, H, Lq, d = Q.shape
+    Hk, P = Kp.shape[0], Kp.shape[1]
+    S = 0 if Ks is None else Ks.shape[2]
+    _same_device(Q.device, Kp, Vp, Ks, Vs, lens, out)
+    if (Ks is None) != (Vs is None):
+        raise ValueError("Ks and Vs come together")
+    for t, shape, name in ((Kp, (Hk, P, d), "Kp"), (Vp, (Hk, P, d), "Vp"), (Ks, (B, Hk, S, d), "Ks"),
+                           (Vs, (B, Hk, S, d), "Vs"), (out, (B, H, Lq, d), "out")):
+        if t is not None and t.shape != shape:
+            raise ValueError(f"{name}: expected {shape}, got {tuple(t.shape)}")
+    O = out if out is not None else torch.empty_like(Q)
+    for t in (Q, Kp, Vp, Ks, Vs, O):
+        if t is not None and (t.dtype != torch.bfloat16 or t.stride(-1) != 1):
+            raise ValueError("expected bf16 tensors with unit innermost stride")
+    if lens is not None and (lens.dtype != torch.int32 or lens.shape != (B,) or not lens.is_contiguous()):
+        raise ValueError(f"lens: expected a contiguous int32 vector of {B}")
+    ks = (0, 0, 0) if Ks is None else Ks.stride()
+    vs = (0, 0, 0) if Vs is None else Vs.stride()
+    q, o, kp, vpr = Q.stride(), O.stride(), Kp.stride(), Vp.stride()
+    a = AttentionPrefixArgs(C.sizeof(AttentionPrefixArgs), B, H, Hk, Lq, P, S, d, CF_BF16,
+                            Q.data_ptr(), q[0], q[1], q[2], Kp.data_ptr(), kp[0], kp[1], Vp.data_ptr(), vpr[0], vpr[1],
+                            _ptr(Ks), ks[0], ks[1], ks[2], _ptr(Vs), vs[0], vs[1], vs[2], _ptr(lens),
+                            1 if causal else 0, d ** -0.5 if scale is None else scale,
+                            O.data_ptr(), o[0], o[1], o[2])
+    if ws is None:
+        need = cf_attention_prefix_workspace(a)
+        if need:
+            ws = workspace(need, Q.device, stream, kind="prefix")
+    _check(cf_attention_prefix(a, _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
     return O

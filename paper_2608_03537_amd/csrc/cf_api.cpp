@@ -1070,4 +1070,209 @@ cf_status cf_b2bgemm(const cf_b2b_args* a, void* workspace, size_t ws_bytes, voi
   }
 }
 
+cf_status cf_rmsnorm_quant(const cf_rmsnorm_quant_args* a, void* hip_stream) {
+  try {
+    if (!a) return fail(CF_ERR_NULL, "args is NULL");
+    if (a->struct_size != sizeof(cf_rmsnorm_quant_args))
+      return fail(CF_ERR_STRUCT, "struct_size %zu != %zu", a->struct_size, sizeof(cf_rmsnorm_quant_args));
+    if (a->M < 0 || a->M > (int64_t)1 << 30 || a->N <= 0 || a->N > kRmsQuantMaxN)
+      return fail(CF_ERR_SHAPE, "need 0 <= M <= 2^30, 0 < N <= %lld", (long long)kRmsQuantMaxN);
+    if (a->dtype != CF_F32 && a->dtype != CF_BF16) return fail(CF_ERR_DTYPE, "dtype must be F32 or BF16");
+    if (a->code_dtype != CF_I8 && a->code_dtype != CF_FP8_E4M3)
+      return fail(CF_ERR_DTYPE, "code_dtype must be I8 or FP8_E4M3");
+    if (a->norm != 0 && a->norm != 1) return fail(CF_ERR_UNSUPPORTED, "norm must be 0 or 1");
+    if (!(a->eps >= 0.0f) || !std::isfinite(a->eps)) return fail(CF_ERR_SHAPE, "eps must be finite and >= 0");
+    cf_status s;
+    if ((s = check_matrix("X", a->X, a->M, a->N, a->ldx, a->dtype, true)) != CF_OK ||
+        (s = check_matrix("R", a->R, a->M, a->N, a->ldr, a->dtype, false)) != CF_OK ||
+        (s = check_matrix("H", a->H, a->M, a->N, a->ldh, a->dtype, false)) != CF_OK ||
+        (s = check_matrix("Q", a->Q, a->M, a->N, a->ldq, a->code_dtype, true)) != CF_OK ||
+        (s = check_vec("gamma", a->gamma)) != CF_OK)
+      return s;
+    if (a->M > 0 && !a->s) return fail(CF_ERR_NULL, "s is NULL");
+    if (reinterpret_cast<uintptr_t>(a->s) & 3u) return fail(CF_ERR_ALIGN, "s is not 4-byte aligned");
+    for (const void* out : {(const void*)a->Q, (const void*)a->s})
+      if (outputs_alias(out, {a->X, a->R, a->H, a->gamma})) return fail(CF_ERR_ALIAS, "an output aliases another operand");
+    if (outputs_alias(a->Q, {a->s}) || outputs_alias(a->H, {a->X, a->gamma}))
+      return fail(CF_ERR_ALIAS, "an output aliases another operand");
+    // H may be R: every element is read by the thread that writes it.
+    if (a->H && a->H == a->R && a->ldh != a->ldr) return fail(CF_ERR_ALIAS, "H is R with another leading dimension");
+    if (a->M == 0) return CF_OK;
+    RmsQuantParams p{};
+    p.M = (int)a->M;
+    p.N = (int)a->N;
+    p.f32 = a->dtype == CF_F32;
+    p.X = a->X;
+    p.ldx = a->ldx;
+    p.R = a->R;
+    p.ldr = a->ldr;
+    p.H = a->H;
+    p.ldh = a->ldh;
+    p.gamma = a->gamma;
+    p.norm = a->norm;
+    p.eps = a->eps;
+    p.e4m3 = a->code_dtype == CF_FP8_E4M3;
+    p.Q = a->Q;
+    p.ldq = a->ldq;
+    p.s = a->s;
+    return hip_status(launch_rms_quant(p, reinterpret_cast<hipStream_t>(hip_stream)), "row quantisation launch");
+  } catch (...) {
+    return fail(CF_ERR_HIP, "internal error");
+  }
+}
+
+// The sum of K products of two int8 values fits 32 bits: |product| <= 2^14.
+static constexpr int64_t kGemmI8MaxK = 131056;
+
+cf_status cf_gemm_i8(const cf_gemm_i8_args* a, void* hip_stream) {
+  try {
+    if (!a) return fail(CF_ERR_NULL, "args is NULL");
+    if (a->struct_size != sizeof(cf_gemm_i8_args))
+      return fail(CF_ERR_STRUCT, "struct_size %zu != %zu", a->struct_size, sizeof(cf_gemm_i8_args));
+    if (a->M < 0 || a->M > (int64_t)1 << 30 || a->N <= 0 || a->N > (int64_t)1 << 20)
+      return fail(CF_ERR_SHAPE, "need 0 <= M <= 2^30, 0 < N <= 2^20");
+    if (a->K <= 0 || a->K > kGemmI8MaxK || a->K % 16 != 0)
+      return fail(CF_ERR_SHAPE, "K = %lld must be a multiple of 16 up to %lld", (long long)a->K, (long long)kGemmI8MaxK);
+    if (a->out_dtype != CF_F32 && a->out_dtype != CF_BF16) return fail(CF_ERR_DTYPE, "out_dtype must be F32 or BF16");
+    if (a->act != CF_ACT_NONE && a->act != CF_ACT_GELU && a->act != CF_ACT_GELU_TANH && a->act != CF_ACT_RELU)
+      return fail(CF_ERR_UNSUPPORTED, "unknown act");
+    cf_status s;
+    if ((s = check_matrix("A", a->A, a->M, a->K, a->lda, CF_I8, true)) != CF_OK ||
+        (s = check_matrix("B", a->B, a->M > 0 ? a->N : 0, a->K, a->ldb, CF_I8, true)) != CF_OK ||
+        (s = check_matrix("C", a->C, a->M, a->N, a->ldc, a->out_dtype, true)) != CF_OK ||
+        (s = check_vec("sb", a->sb)) != CF_OK || (s = check_vec("bias", a->bias)) != CF_OK)
+      return s;
+    if (reinterpret_cast<uintptr_t>(a->sa) & 3u) return fail(CF_ERR_ALIGN, "sa is not 4-byte aligned");
+    if (outputs_alias(a->C, {a->A, a->B, a->sa, a->sb, a->bias})) return fail(CF_ERR_ALIAS, "C aliases an input");
+    if (a->M == 0) return CF_OK;
+    static_assert((int)CF_ACT_GELU == (int)ACT_GELU && (int)CF_ACT_GELU_TANH == (int)ACT_GELU_TANH &&
+                      (int)CF_ACT_RELU == (int)ACT_RELU, "act values");
+    GemmI8Params p{};
+    p.M = (int)a->M;
+    p.N = (int)a->N;
+    p.K = (int)a->K;
+    p.A = reinterpret_cast<const int8_t*>(a->A);
+    p.lda = a->lda;
+    p.B = reinterpret_cast<const int8_t*>(a->B);
+    p.ldb = a->ldb;
+    p.sa = a->sa;
+    p.sb = a->sb;
+    p.bias = a->bias;
+    p.act = a->act;
+    p.C = a->C;
+    p.ldc = a->ldc;
+    p.c_f32 = a->out_dtype == CF_F32;
+    return hip_status(launch_gemm_i8(p, reinterpret_cast<hipStream_t>(hip_stream)), "int8 GEMM launch");
+  } catch (...) {
+    return fail(CF_ERR_HIP, "internal error");
+  }
+}
+
+// One operand of cf_attention_prefix: rows of d elements in up to two outer
+// dimensions (batch, head); strides that move nothing (size 1) are free.
+static cf_status check_rows(const char* name, const void* p, bool used, int64_t nb, int64_t sb, int64_t nh, int64_t sh,
+                            int64_t rows, int64_t sl, int64_t d) {
+  if (!used) return CF_OK;
+  if (!p) return fail(CF_ERR_NULL, "%s is NULL", name);
+  if (!aligned16(p)) return fail(CF_ERR_ALIGN, "%s is not 16-byte aligned", name);
+  if (rows > 1 && sl < d) return fail(CF_ERR_LD, "%s: row stride %lld < %lld", name, (long long)sl, (long long)d);
+  if (rows > 1 && sl * 2 >= kMaxRowPitch)
+    return fail(CF_ERR_LD, "%s: row stride of %lld bytes or more", name, (long long)kMaxRowPitch);
+  if ((nb > 1 && (sb < 0 || sb % 8 != 0)) || (nh > 1 && (sh < 0 || sh % 8 != 0)) || (rows > 1 && sl % 8 != 0))
+    return fail(CF_ERR_ALIGN, "%s: strides must be non-negative multiples of 8 elements", name);
+  return CF_OK;
+}
+
+// Sizes only: what the workspace query needs.
+static cf_status prefix_sizes(const cf_attention_prefix_args* a, PrefixParams& p) {
+  if (!a) return fail(CF_ERR_NULL, "args is NULL");
+  if (a->struct_size != sizeof(cf_attention_prefix_args))
+    return fail(CF_ERR_STRUCT, "struct_size %zu != %zu", a->struct_size, sizeof(cf_attention_prefix_args));
+  if (a->dtype != CF_BF16) return fail(CF_ERR_DTYPE, "cf_attention_prefix computes in bf16 only");
+  if (a->batch < 0 || a->batch > 65535 || a->H <= 0 || a->Hk <= 0 || a->H > 65535 || a->Lq < 0 ||
+      a->Lq > (int64_t)1 << 24 || a->P < 0 || a->S < 0 || a->P > (int64_t)1 << 30 || a->S > (int64_t)1 << 30)
+    return fail(CF_ERR_SHAPE, "need 0 <= batch <= 65535, 0 < H <= 65535, 0 <= Lq <= 2^24, 0 <= P, S <= 2^30");
+  if (a->H % a->Hk != 0) return fail(CF_ERR_SHAPE, "H = %lld is not a multiple of Hk = %lld", (long long)a->H, (long long)a->Hk);
+  if (a->batch * a->Hk > 65535) return fail(CF_ERR_SHAPE, "batch * Hk exceeds 65535");
+  if (a->batch * a->H * a->Lq > (int64_t)1 << 30) return fail(CF_ERR_SHAPE, "batch * H * Lq exceeds 2^30");
+  if (a->d != 64 && a->d != 128) return fail(CF_ERR_UNSUPPORTED, "head dim %lld not compiled (64, 128)", (long long)a->d);
+  if (a->causal != 0 && a->causal != 1) return fail(CF_ERR_UNSUPPORTED, "causal must be 0 or 1");
+  if (!std::isfinite(a->scale) || !(a->scale > 0.0f)) return fail(CF_ERR_SHAPE, "scale must be finite and > 0");
+  p = PrefixParams{};
+  p.B = (int)a->batch;
+  p.H = (int)a->H;
+  p.Hk = (int)a->Hk;
+  p.Lq = (int)a->Lq;
+  p.P = (int)a->P;
+  p.S = (int)a->S;
+  p.d = (int)a->d;
+  p.causal = a->causal;
+  p.scale = a->scale;
+  return CF_OK;
+}
+
+size_t cf_attention_prefix_workspace(const cf_attention_prefix_args* a) {
+  try {
+    PrefixParams p;
+    if (prefix_sizes(a, p) != CF_OK || p.B == 0 || p.Lq == 0) return 0;
+    return prefix_workspace(p);
+  } catch (...) {
+    return 0;
+  }
+}
+
+cf_status cf_attention_prefix(const cf_attention_prefix_args* a, void* workspace, size_t ws_bytes, void* hip_stream) {
+  try {
+    PrefixParams p;
+    cf_status s = prefix_sizes(a, p);
+    if (s != CF_OK) return s;
+    const bool any = p.B > 0 && p.Lq > 0;
+    if ((s = check_rows("Q", a->Q, any, p.B, a->q_b, p.H, a->q_h, p.Lq, a->q_l, p.d)) != CF_OK ||
+        (s = check_rows("O", a->O, any, p.B, a->o_b, p.H, a->o_h, p.Lq, a->o_l, p.d)) != CF_OK ||
+        (s = check_rows("Kp", a->Kp, any && p.P > 0, 1, 0, p.Hk, a->kp_h, p.P, a->kp_l, p.d)) != CF_OK ||
+        (s = check_rows("Vp", a->Vp, any && p.P > 0, 1, 0, p.Hk, a->vp_h, p.P, a->vp_l, p.d)) != CF_OK ||
+        (s = check_rows("Ks", a->Ks, any && p.S > 0, p.B, a->ks_b, p.Hk, a->ks_h, p.S, a->ks_l, p.d)) != CF_OK ||
+        (s = check_rows("Vs", a->Vs, any && p.S > 0, p.B, a->vs_b, p.Hk, a->vs_h, p.S, a->vs_l, p.d)) != CF_OK)
+      return s;
+    if (reinterpret_cast<uintptr_t>(a->lens) & 3u) return fail(CF_ERR_ALIGN, "lens is not 4-byte aligned");
+    if (outputs_alias(a->O, {a->Q, a->Kp, a->Vp, a->Ks, a->Vs, a->lens})) return fail(CF_ERR_ALIAS, "O aliases an input");
+    if (!any) return CF_OK;
+    const size_t need = prefix_workspace(p);
+    if (need > 0) {
+      if (!workspace) return fail(CF_ERR_WORKSPACE, "workspace of %zu bytes required", need);
+      if (ws_bytes < need) return fail(CF_ERR_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+      if (!aligned16(workspace)) return fail(CF_ERR_ALIGN, "workspace is not 16-byte aligned");
+      if (outputs_alias(workspace, {a->O, a->Q, a->Kp, a->Vp, a->Ks, a->Vs, a->lens}))
+        return fail(CF_ERR_ALIAS, "the workspace aliases an operand");
+    }
+    p.Q = reinterpret_cast<const uint16_t*>(a->Q);
+    p.q_b = a->q_b;
+    p.q_h = a->q_h;
+    p.q_l = a->q_l;
+    p.Kp = reinterpret_cast<const uint16_t*>(a->Kp);
+    p.kp_h = a->kp_h;
+    p.kp_l = a->kp_l;
+    p.Vp = reinterpret_cast<const uint16_t*>(a->Vp);
+    p.vp_h = a->vp_h;
+    p.vp_l = a->vp_l;
+    p.Ks = reinterpret_cast<const uint16_t*>(a->Ks);
+    p.ks_b = a->ks_b;
+    p.ks_h = a->ks_h;
+    p.ks_l = a->ks_l;
+    p.Vs = reinterpret_cast<const uint16_t*>(a->Vs);
+    p.vs_b = a->vs_b;
+    p.vs_h = a->vs_h;
+    p.vs_l = a->vs_l;
+    p.lens = a->lens;
+    p.O = reinterpret_cast<uint16_t*>(a->O);
+    p.o_b = a->o_b;
+    p.o_h = a->o_h;
+    p.o_l = a->o_l;
+    p.ws = reinterpret_cast<float*>(workspace);
+    return hip_status(launch_prefix(p, reinterpret_cast<hipStream_t>(hip_stream)), "prefix attention launch");
+  } catch (...) {
+    return fail(CF_ERR_HIP, "internal error");
+  }
+}
+
 }  // extern "C"

@@ -1,0 +1,62 @@
+// Device helpers of the attention kernels: packed P fragments, LDS reads as
+// inline assembly with their waits, lane-pair reductions.
+#pragma once
+
+#include <type_traits>
+
+#include "cf_device.h"
+
+namespace cf {
+
+// Accumulator elements 8s .. 8s+7 of a block, as 8 packed bf16.
+__device__ __forceinline__ u32x4_t pack_step(const f32x16_t& v, int s) {
+  return u32x4_t{pack_bf16x2(v[8 * s + 0], v[8 * s + 1]), pack_bf16x2(v[8 * s + 2], v[8 * s + 3]),
+                 pack_bf16x2(v[8 * s + 4], v[8 * s + 5]), pack_bf16x2(v[8 * s + 6], v[8 * s + 7])};
+}
+
+// Transposing 8-byte LDS read (ds_read_b64_tr_b16) at LDS byte address
+// addr + OFF, written as inline assembly.  The compiler builtin carries no
+// memory operand, so the compiler's wait insertion assumes it may read bytes
+// that an outstanding direct-to-LDS load is still writing and puts a wait for
+// every such load (vmcnt(0)) in front of it.  The caller knows the stage it
+// reads is not the one being loaded; it waits for the result itself
+// (lgkm_wait), since the compiler does not know this instruction loads.
+template <int OFF>
+__device__ __forceinline__ u32x2_t ds_read_tr_b64(uint32_t addr) {
+  static_assert(OFF >= 0 && OFF < 65536, "ds offset field");
+  u32x2_t v;
+  asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "i"(OFF));
+  return v;
+}
+// 16-byte LDS read at byte address addr + OFF as inline assembly, for the
+// same reason (K rows sit in a stage that direct loads also write); the
+// caller waits for the result.
+template <int OFF>
+__device__ __forceinline__ u32x4_t ds_read_b128_at(uint32_t addr) {
+  static_assert(OFF >= 0 && OFF < 65536, "ds offset field");
+  u32x4_t v;
+  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "i"(OFF));
+  return v;
+}
+// Wait until at most N LDS operations of this wave are outstanding; v is tied
+// to the wait so that its uses cannot move above it.  The count is exact only
+// while no scalar memory load is in flight (they share the counter and return
+// out of order): the kernel's loop issues none, and each step begins with a
+// full wait (lds_sync).
+template <int N>
+__device__ __forceinline__ void lgkm_wait(u32x4_t& v) {
+  asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(v) : "i"(N));
+}
+// Calls f(std::integral_constant<int, I>) for I = B .. E-1 in order.
+template <int B, int E, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (B < E) {
+    f(std::integral_constant<int, B>{});
+    static_for<B + 1, E>(f);
+  }
+}
+
+__device__ __forceinline__ float lane_pair_sum(float v) { return v + __shfl_xor(v, 32); }
+__device__ __forceinline__ float lane_pair_max(float v) { return fmaxf(v, __shfl_xor(v, 32)); }
+
+}  // namespace cf
