@@ -1,12 +1,27 @@
 // Matrix product of 8-bit integers with a scale per token and per channel:
 //     C[m, n] = act(float(sum_k A[m, k] B[n, k]) sa[m] sb[n] + bias[n]).
 // The sum is exact in 32 bits for K <= 131056 (|product| <= 2^14), so the order
-// of its terms is free: waves may split K and tiles may differ in shape without
-// changing a bit.
+// of its terms is free: waves split K and tiles differ in shape without
+// changing a bit of the result.
+//
+// An MFMA covers 32 bytes of k per operand row in 32 cycles, as the bf16 one does,
+// so in bytes these loops are those of a bf16 product with half the k.  Tiles:
+//   wave tiles   32 x 32 to 64 x 64, a ring of LDS stages per wave (or per pair of
+//                waves); the waves or pairs of a workgroup split K and their sums meet in LDS.
+//   128 x 128    four waves of 64 x 64 share a ring, one or two workgroups a CU.
+//   256 x 256    big_product in cf_gemm_big.h.
+// What bounds them: a CU's direct loads into LDS take about 32 cycles per KB (64 x 64
+// tiles reach 60 GB/s a CU with all CUs busy), so a tile's time is its operand bytes
+// over that rate, and few tokens are the weights' stream.  256 x 256 tiles run
+// 16384 x 4096 x 4096 in 262 us, 2.1 POP/s; with operands of zeros, whose MFMAs draw
+// less power, in 184: the clock that full power leaves bounds them.  kForms has
+// the measurements of all.  A form that loads fragments straight into registers
+// was slower from 16 tokens on (48 x 12288 x 4096 29 us against 12.8: rows of a power
+// of two apart meet in the same sets of the first-level cache).
 #include <algorithm>
 
-#include "cf_device.h"
-#include "cf_internal.h"
+#include "cf_attn.h"
+#include "cf_gemm_big.h"
 
 namespace cf {
 
@@ -17,53 +32,365 @@ typedef __attribute__((__vector_size__(16 * sizeof(int)))) int i32x16_t;
 
 // D (32 n x 32 m) += W (32 n x 32 k) X (32 k x 32 m): lane l gives 16 k of row l % 32 of
 // either operand, k group l / 32; layout of D as for the bf16 atom (acc_row).
-__device__ __forceinline__ void mma_i8(i32x16_t& acc, u32x4_t w, u32x4_t x) {
-  acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4_t, w), __builtin_bit_cast(i32x4_t, x), acc, 0, 0,
-                                              0);
-}
+struct MmaI8 {
+  __device__ __forceinline__ static void run(i32x16_t& acc, u32x4_t w, u32x4_t x) {
+    acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4_t, w), __builtin_bit_cast(i32x4_t, x), acc, 0,
+                                                0, 0);
+  }
+};
 
-__device__ __forceinline__ float act_i8(float x, int act) {
-  if (act == ACT_GELU) return gelu_erf(x);
-  if (act == ACT_GELU_TANH) return gelu_tanh(x);
-  if (act == ACT_RELU) return x < 0.0f ? 0.0f : x;
+template <int ACT>
+__device__ __forceinline__ float act_i8(float x) {
+  if constexpr (ACT == ACT_GELU) return gelu_erf(x);
+  if constexpr (ACT == ACT_GELU_TANH) return 0.5f * x * (1.0f + tanh_exp(0.79788456080286536f * (x + 0.044715f * x * x * x)));
+  if constexpr (ACT == ACT_RELU) return x < 0.0f ? 0.0f : x;
   return x;
 }
+// f(std::integral_constant<int, act>{})
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F&& f) {
+  if (act == ACT_GELU) f(std::integral_constant<int, ACT_GELU>{});
+  else if (act == ACT_GELU_TANH) f(std::integral_constant<int, ACT_GELU_TANH>{});
+  else if (act == ACT_RELU) f(std::integral_constant<int, ACT_RELU>{});
+  else f(std::integral_constant<int, ACT_NONE>{});
+}
 
-// 64 x 64 tile, four waves of 32 x 32, operands straight from global memory.
-__global__ __launch_bounds__(256) void gemm_i8_direct_kernel(GemmI8Params p) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int lr = lane & 31, lg = lane >> 5;
-  const int m0 = blockIdx.x * 64 + (wave >> 1) * 32, n0 = blockIdx.y * 64 + (wave & 1) * 32;
-  const int8_t* a = p.A + (int64_t)min(m0 + lr, p.M - 1) * p.lda;
-  const int8_t* b = p.B + (int64_t)min(n0 + lr, p.N - 1) * p.ldb;
-  i32x16_t acc = {};
-  for (int k = lg * 16; k - lg * 16 < p.K; k += 32) {
-    const u32x4_t zero = {};
-    const bool in = k < p.K;   // K is a multiple of 16
-    mma_i8(acc, in ? gload16(b + k) : zero, in ? gload16(a + k) : zero);
-  }
-  const int m = m0 + lr;
-  if (m >= p.M) return;
-  const float sa = p.sa ? p.sa[m] : 1.0f;
+// Output pass of a tile whose sums lie in LDS: KW planes of TM rows of TN int32 (pitch TN * 4 +
+// 16 bytes), added here.  A thread takes 8 columns of a row at a time, always the same columns.
+// Its scales and biases are loaded ahead (before the main loop, where registers allow: loaded
+// here, they add a trip to memory to every tile).
+template <int TM, int TN, int NT>
+struct TileScales {
+  static constexpr int CPR = TN / 8, STEP = NT / CPR, RPT = (TM + STEP - 1) / STEP;   // a thread's rows: STEP apart
+  static_assert(NT % CPR == 0, "a thread keeps its columns");
+  float sa[RPT], sb[8], bias[8];
+  __device__ __forceinline__ void load(const GemmI8Params& p, int m0, int n0) {
+    const int n = n0 + threadIdx.x % CPR * 8, r0 = threadIdx.x / CPR;
+    auto eight = [&](const float* v, float none, float (&out)[8]) {
+      if (v && n + 8 <= p.N) {
+        const f32x4_t a = *reinterpret_cast<const f32x4_t*>(v + n), b = *reinterpret_cast<const f32x4_t*>(v + n + 4);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int n = n0 + acc_row(i, lane);
-    if (n >= p.N) continue;
-    float x = (float)acc[i] * sa * (p.sb ? p.sb[n] : 1.0f);
-    if (p.bias) x += p.bias[n];
-    x = act_i8(x, p.act);
-    const int64_t at = (int64_t)m * p.ldc + n;
-    if (p.c_f32) reinterpret_cast<float*>(p.C)[at] = x;
-    else reinterpret_cast<bf16_t*>(p.C)[at] = (bf16_t)pack_bf16x2(x, 0.0f);
+        for (int e = 0; e < 4; ++e) {
+          out[e] = a[e];
+          out[4 + e] = b[e];
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) out[e] = v && n + e < p.N ? v[n + e] : none;
+      }
+    };
+    eight(p.sb, 1.0f, sb);
+    eight(p.bias, 0.0f, bias);
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) sa[i] = p.sa ? p.sa[min(m0 + r0 + i * STEP, p.M - 1)] : 1.0f;
   }
+};
+
+template <int TM, int TN, int KW, int NT>
+__device__ __forceinline__ void finish_tile(const GemmI8Params& p, const TileScales<TM, TN, NT>& sc, const char* smem,
+                                            int m0, int n0) {
+  using Sc = TileScales<TM, TN, NT>;
+  constexpr int PITCH = TN * 4 + 16;
+  const int tid = threadIdx.x, c8 = tid % Sc::CPR * 8, left = p.N - n0 - c8;
+  if (left <= 0) return;
+  const int rows = min(TM, p.M - m0);
+  with_act(p.act, [&](auto act_t) {
+    constexpr int ACT = decltype(act_t)::value;
+#pragma unroll
+    for (int i = 0; i < Sc::RPT; ++i) {
+      const int r = tid / Sc::CPR + i * Sc::STEP;
+      if (r >= rows) break;
+      const char* src = smem + r * PITCH + c8 * 4;
+      i32x4_t a = *reinterpret_cast<const i32x4_t*>(src), b = *reinterpret_cast<const i32x4_t*>(src + 16);
+#pragma unroll
+      for (int k = 1; k < KW; ++k) {
+        a += *reinterpret_cast<const i32x4_t*>(src + k * TM * PITCH);
+        b += *reinterpret_cast<const i32x4_t*>(src + k * TM * PITCH + 16);
+      }
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float x = (float)(e < 4 ? a[e] : b[e - 4]) * sc.sa[i] * sc.sb[e];
+        if (p.bias) x += sc.bias[e];
+        y[e] = act_i8<ACT>(x);
+      }
+      const int64_t at = (int64_t)(m0 + r) * p.ldc + n0 + c8;
+      if (left >= 8) {
+        if (p.c_f32) {
+          float* c = reinterpret_cast<float*>(p.C) + at;
+          __builtin_nontemporal_store(f32x4_t{y[0], y[1], y[2], y[3]}, reinterpret_cast<f32x4_t*>(c));
+          __builtin_nontemporal_store(f32x4_t{y[4], y[5], y[6], y[7]}, reinterpret_cast<f32x4_t*>(c + 4));
+        } else {
+          const u32x4_t w = {pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]),
+                             pack_bf16x2(y[6], y[7])};
+          __builtin_nontemporal_store(w, reinterpret_cast<u32x4_t*>(reinterpret_cast<bf16_t*>(p.C) + at));
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (e >= left) break;
+          if (p.c_f32) reinterpret_cast<float*>(p.C)[at + e] = y[e];
+          else reinterpret_cast<bf16_t*>(p.C)[at + e] = (bf16_t)pack_bf16x2(y[e], 0.0f);
+        }
+      }
+    }
+  });
+}
+
+// ---------------------------------------------------------------------------
+// Tile.  A group of WM x WN waves (32 BM tokens x 32 BN channels each) shares a ring of
+// NS stages of 128 bytes of k; KW groups take the stages in turn.  A group of one wave
+// needs no barrier until the end.  The 16-byte chunk ch of row r of
+// a stage sits at position ch ^ ((r >> 1) & 7), as in big_product.
+// ---------------------------------------------------------------------------
+template <int BM_, int BN_, int WM_, int WN_, int KW_, int NS_>
+struct I8Tile {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KW = KW_, NS = NS_;
+  static constexpr int GW = WM * WN, NW = GW * KW, NT = 64 * NW;
+  static constexpr int TM = 32 * BM * WM, TN = 32 * BN * WN, STAGE = (TM + TN) * 128;
+  static constexpr int RING = NS * STAGE, OUT = KW * TM * (TN * 4 + 16);
+  static constexpr int LDS = KW * RING > OUT ? KW * RING : OUT;
+  static constexpr int LPW = (TM + TN) / 8 / GW;   // wave-wide loads of a stage per wave
+  static_assert(LDS <= 160 * 1024 && LPW * NS < 64, "LDS budget, vmcnt range");
+};
+
+// Fragments of a stage's four k steps of NB 32-row blocks at a[0..3], complete.
+template <int NB>
+__device__ __forceinline__ void read_blocks(u32x4_t (&f)[NB][4], const uint32_t (&a)[4]) {
+  if constexpr (NB == 2) read_x_half<0>(f, a);
+  else read_w_half_nk<0>(f[0], a);
+}
+
+template <class S>
+__global__ __launch_bounds__(S::NT) void gemm_i8_tile_kernel(GemmI8Params p) {
+  __shared__ __attribute__((aligned(16))) char smem[S::LDS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, lg = lane >> 5;
+  const int grp = wave / S::GW, gw = wave % S::GW, wm = gw / S::WN, wn = gw % S::WN;
+  int rb, c;
+  big_tile_order((p.M + S::TM - 1) / S::TM, (p.N + S::TN - 1) / S::TN, rb, c);
+  const int m0 = rb * S::TM, n0 = c * S::TN;
+  TileScales<S::TM, S::TN, S::NT> sc;
+  sc.load(p, m0, n0);
+  char* const ring = smem + grp * S::RING;
+  const int KT = p.K / 128, steps = grp < KT ? (KT - grp - 1) / S::KW + 1 : 0;   // whole steps; those of this group
+
+  // Stage rows 0 .. TM - 1 are tokens, then TN channels; load i of a wave fills rows
+  // 8 (i GW + gw) .. + 7.  Rows past M and N are clamped (they feed nothing that is stored).
+  const char* src[S::LPW];
+#pragma unroll
+  for (int i = 0; i < S::LPW; ++i) {
+    const int row = 8 * (i * S::GW + gw) + (lane >> 3), ch = (lane & 7) ^ ((row >> 1) & 7);
+    src[i] = (row < S::TM ? reinterpret_cast<const char*>(p.A) + (int64_t)min(m0 + row, p.M - 1) * p.lda
+                          : reinterpret_cast<const char*>(p.B) + (int64_t)min(n0 + row - S::TM, p.N - 1) * p.ldb) +
+             ch * 16 + grp * 128;
+  }
+  auto load = [&](int s, int i) {   // load i of the group's step s, into stage s % NS
+    dma16(src[i] + (int64_t)s * (S::KW * 128), ring + s % S::NS * S::STAGE + gw * 1024 + i * S::GW * 1024);
+  };
+  const uint32_t s0 =
+      (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)smem) + grp * S::RING;
+  uint32_t xa[4], wa[4];
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks) {
+    const int ch = ((2 * ks + lg) ^ ((lr >> 1) & 7)) << 4;
+    xa[ks] = s0 + (wm * 32 * S::BM + lr) * 128 + ch;
+    wa[ks] = s0 + (S::TM + wn * 32 * S::BN + lr) * 128 + ch;
+  }
+  i32x16_t acc[S::BM][S::BN] = {};
+  u32x4_t xf[S::BM][4], wf[S::BN][4];
+  auto mma = [&](int ks) {
+#pragma unroll
+    for (int bm = 0; bm < S::BM; ++bm)
+#pragma unroll
+      for (int bn = 0; bn < S::BN; ++bn) MmaI8::run(acc[bm][bn], wf[bn][ks], xf[bm][ks]);
+  };
+#pragma unroll
+  for (int s = 0; s < S::NS - 1; ++s)
+    if (s < steps) {
+#pragma unroll
+      for (int i = 0; i < S::LPW; ++i) load(s, i);
+    }
+  const int all = (KT + S::KW - 1) / S::KW;   // every group passes every barrier
+  for (int s = 0; s < all; ++s) {
+    if (s + S::NS - 2 < steps) wait_vmcnt<S::LPW*(S::NS - 2)>();
+    else wait_vmcnt<0>();
+    if constexpr (S::GW > 1) lds_barrier();   // every wave's loads of step s are in, and step s - 1 has been read
+    if (s >= steps) continue;
+    const uint32_t at = s % S::NS * S::STAGE;
+    const uint32_t x[4] = {xa[0] + at, xa[1] + at, xa[2] + at, xa[3] + at};
+    const uint32_t w[4] = {wa[0] + at, wa[1] + at, wa[2] + at, wa[3] + at};
+    // The loads of a later step go between the MFMAs: in front of the reads they would hold them up.
+    read_blocks<S::BM>(xf, x);
+    read_blocks<S::BN>(wf, w);
+    __builtin_amdgcn_sched_barrier(0);
+    mma(0);
+    __builtin_amdgcn_sched_barrier(0);
+    if (s + S::NS - 1 < steps) {
+#pragma unroll
+      for (int i = 0; i < S::LPW; ++i) load(s + S::NS - 1, i);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    mma(1);
+    mma(2);
+    mma(3);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  // k behind the last whole step, straight from memory; the last group takes it
+  if (grp == S::KW - 1 && KT * 128 < p.K) {
+    auto frag = [&](const int8_t* row, int ks) {
+      const int k = KT * 128 + ks * 32 + lg * 16;
+      u32x4_t v = {};
+      if (k < p.K) v = gload16(row + k);
+      return v;
+    };
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+#pragma unroll
+      for (int b = 0; b < S::BM; ++b)
+        xf[b][ks] = frag(p.A + (int64_t)min(m0 + (wm * S::BM + b) * 32 + lr, p.M - 1) * p.lda, ks);
+#pragma unroll
+      for (int b = 0; b < S::BN; ++b)
+        wf[b][ks] = frag(p.B + (int64_t)min(n0 + (wn * S::BN + b) * 32 + lr, p.N - 1) * p.ldb, ks);
+      mma(ks);
+    }
+  }
+  __syncthreads();
+  constexpr int PITCH = S::TN * 4 + 16;
+  char* const out = smem + grp * S::TM * PITCH;
+#pragma unroll
+  for (int bm = 0; bm < S::BM; ++bm)
+#pragma unroll
+    for (int bn = 0; bn < S::BN; ++bn)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const i32x16_t& v = acc[bm][bn];
+        *reinterpret_cast<i32x4_t*>(out + ((wm * S::BM + bm) * 32 + lr) * PITCH +
+                                    ((wn * S::BN + bn) * 32 + 8 * g + 4 * lg) * 4) =
+            i32x4_t{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+      }
+  __syncthreads();
+  finish_tile<S::TM, S::TN, S::KW, S::NT>(p, sc, smem, m0, n0);
+}
+
+// ---------------------------------------------------------------------------
+// Big.
+// ---------------------------------------------------------------------------
+constexpr int kI8BigPitch = kBigT * 4 + 16;
+constexpr int kI8BigLds = 128 * kI8BigPitch > 2 * kBigStep ? 128 * kI8BigPitch : 2 * kBigStep;
+
+__global__ __launch_bounds__(512, 1) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void gemm_i8_big_kernel(GemmI8Params p) {
+  __shared__ __attribute__((aligned(16))) char smem[kI8BigLds];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 2, wn = wave & 3, lr = lane & 31, lg = lane >> 5;
+  int rb, c;
+  big_tile_order((p.M + kBigT - 1) / kBigT, (p.N + kBigT - 1) / kBigT, rb, c);
+  const int m0 = rb * kBigT, n0 = c * kBigT, KT = p.K / 128;
+  i32x16_t acc[2][2][2] = {};   // [token half][32-token block][channel half]
+  big_product<false, MmaI8>(acc, reinterpret_cast<const char*>(p.A) + (int64_t)m0 * p.lda, p.lda, p.M - m0,
+                            reinterpret_cast<const char*>(p.B) + (int64_t)n0 * p.ldb, p.ldb, p.N - n0, KT, smem);
+  // k behind the last whole step, straight from memory
+#pragma unroll 1
+  for (int k = KT * 128 + lg * 16; k - lg * 16 < p.K; k += 32) {
+    u32x4_t w[2], x[2][2];
+    const bool in = k < p.K;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      w[h] = u32x4_t{};
+      if (in) w[h] = gload16(p.B + (int64_t)min(n0 + h * 128 + wn * 32 + lr, p.N - 1) * p.ldb + k);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        x[h][b] = u32x4_t{};
+        if (in) x[h][b] = gload16(p.A + (int64_t)min(m0 + h * 128 + wm * 64 + b * 32 + lr, p.M - 1) * p.lda + k);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) MmaI8::run(acc[i >> 2][(i >> 1) & 1][i & 1], w[i & 1], x[i >> 2][(i >> 1) & 1]);
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int nh = 0; nh < 2; ++nh)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const i32x16_t& v = acc[h][b][nh];
+          *reinterpret_cast<i32x4_t*>(smem + (wm * 64 + b * 32 + lr) * kI8BigPitch + (nh * 128 + wn * 32 + 8 * g + 4 * lg) * 4) =
+              i32x4_t{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+        }
+    TileScales<128, kBigT, 512> sc;
+    sc.load(p, m0 + h * 128, n0);
+    __syncthreads();
+    finish_tile<128, kBigT, 1, 512>(p, sc, smem, m0 + h * 128, n0);
+    __syncthreads();
+  }
+}
+
+template <class S>
+hipError_t launch_tile(const GemmI8Params& p, hipStream_t st) {
+  const int64_t wgs = (int64_t)((p.M + S::TM - 1) / S::TM) * ((p.N + S::TN - 1) / S::TN);
+  hipLaunchKernelGGL((gemm_i8_tile_kernel<S>), dim3((unsigned)wgs), dim3(S::NT), 0, st, p);
+  return hipGetLastError();
+}
+hipError_t launch_big(const GemmI8Params& p, hipStream_t st) {
+  const int64_t wgs = (int64_t)((p.M + kBigT - 1) / kBigT) * ((p.N + kBigT - 1) / kBigT);
+  hipLaunchKernelGGL(gemm_i8_big_kernel, dim3((unsigned)wgs), dim3(512), 0, st, p);
+  return hipGetLastError();
+}
+
+// The tiles and their estimated time: rounds of `per` workgroups, each `step` us for
+// every 128 bytes of k and `start` us besides.  Fitted to M x N of 1 to 16384 with K of 512
+// to 16384; for instance (us, in this order, - not run):
+//     1 x 4096 x 4096        5.8  7.1  7.6  9.8   16   21    -    -
+//     16 x 12288 x 4096     12.5 14.0 11.0 11.6   16   22    -    -
+//     48 x 12288 x 4096     16.9 15.2 15.6 12.8   18   23    -    -
+//     128 x 4096 x 4096     11.2  8.2  8.5 10.7   17   24   30   42
+//     512 x 4096 x 4096       38   25   27 20.0 18.2   24   30   45
+//     1024 x 4096 x 4096      73   49   52   37   35 25.9   31   45
+//     2048 x 4096 x 4096     144   95  101   73   68   51 38.8   46
+//     4096 x 4096 x 4096     285  187  199  141  133  100   77 64.8
+//     8192 x 1024 x 1024      82   52   55   37   29   22 17.5   24
+struct Form {
+  int tm, tn, per;
+  double step, start;
+  hipError_t (*launch)(const GemmI8Params&, hipStream_t);
+};
+constexpr int kCUs = 256;
+const Form kForms[] = {
+    {32, 32, kCUs, 0.09, 1.7, launch_tile<I8Tile<1, 1, 1, 1, 4, 4>>},
+    {64, 32, kCUs, 0.13, 1.9, launch_tile<I8Tile<2, 1, 1, 1, 4, 3>>},
+    {32, 64, kCUs, 0.12, 2.2, launch_tile<I8Tile<1, 2, 1, 1, 6, 2>>},
+    {64, 64, kCUs, 0.19, 2.6, launch_tile<I8Tile<2, 2, 1, 1, 4, 2>>},
+    {64, 128, kCUs, 0.40, 3.6, launch_tile<I8Tile<2, 2, 1, 2, 2, 3>>},
+    {128, 128, kCUs, 0.64, 4.6, launch_tile<I8Tile<2, 2, 2, 2, 1, 4>>},
+    {128, 128, 2 * kCUs, 1.06, 4.2, launch_tile<I8Tile<2, 2, 2, 2, 1, 2>>},
+    {kBigT, kBigT, kCUs, 0.88, 14.3, launch_big},
+};
+constexpr double kBigBusy = 0.62;   // added to the step of 256 x 256 tiles times the share of CUs at work (clocks)
+
+const Form& choose_form(int64_t M, int64_t N, int64_t K) {
+  const Form* best = nullptr;
+  double least = 0;
+  const double kt = (double)((K + 127) / 128);
+  for (const Form& f : kForms) {
+    if (f.tm == kBigT && K < 256) continue;   // its loop needs two whole steps
+    const int64_t wgs = ((M + f.tm - 1) / f.tm) * ((N + f.tn - 1) / f.tn), rounds = (wgs + f.per - 1) / f.per;
+    if (wgs > INT32_MAX / 2) continue;
+    double step = f.step;
+    if (f.tm == kBigT) step += kBigBusy * std::min(1.0, (double)wgs / kCUs);
+    const double t = (double)rounds * (step * kt + f.start);
+    if (!best || t < least) {
+      best = &f;
+      least = t;
+    }
+  }
+  return *best;
 }
 
 }  // namespace
 
-hipError_t launch_gemm_i8(const GemmI8Params& p, hipStream_t st) {
-  const dim3 grid((unsigned)((p.M + 63) / 64), (unsigned)((p.N + 63) / 64));
-  hipLaunchKernelGGL(gemm_i8_direct_kernel, grid, dim3(256), 0, st, p);
-  return hipGetLastError();
-}
+hipError_t launch_gemm_i8(const GemmI8Params& p, hipStream_t st) { return choose_form(p.M, p.N, p.K).launch(p, st); }
 
 }  // namespace cf
