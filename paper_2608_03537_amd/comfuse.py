@@ -12,7 +12,6 @@ allocate the outputs.
 from __future__ import annotations
 
 import ctypes as C
-import functools
 import os
 import threading
 
@@ -596,63 +595,69 @@ def b2b_attention(Q, K, V, scale=None, out=None, stream=None, ws=None):
 
 
 # ---------------------------------------------------------------- 8-bit serving path
-# These helpers run on the operands' device, whichever is current, and allocate on
-# the stream that the call uses.
+# These helpers run on the operands' device, whichever is current, and their new
+# tensors belong to the stream that the call uses.  A decoding step makes many
+# small calls, so they ask torch for the raw device and stream numbers (a
+# torch.cuda.Stream object costs 2.7 us a call) and fill the argument block in one go.
+def _elsewhere(call, X, stream, *args, **kw):
+    """The call with `stream` current (given: of X's device), or with X's device current."""
+    torch = _torch()
+    if not X.is_cuda:
+        raise ValueError(f"expected operands on a GPU, got {X.device}")
+    if stream is not None and stream.device != X.device:
+        raise ValueError(f"operands on {X.device}, stream of {stream.device}")
+    with torch.cuda.stream(stream) if stream is not None else torch.cuda.device(X.device):
+        return call(X, *args, **kw)
+
+
+def _here(X, stream):
+    """Whether the call can run on the current device and stream."""
+    return stream is None and X.is_cuda and X.get_device() == _torch()._C._cuda_getDevice()
+
+
+def _raw_stream(device):
+    return _torch()._C._cuda_getCurrentRawStream(device)
+
+
 def _rows(M, N, dtype, device, size):
     """An [M, N] tensor whose rows start every multiple of 16 bytes (`size`: bytes of an element)."""
-    torch = _torch()
     per = 16 // size
     ld = -(-N // per) * per
-    t = torch.empty((M, ld), dtype=dtype, device=device)
+    t = _torch().empty(M, ld, dtype=dtype, device=device)
     return t if ld == N else t[:, :N]
 
 
-def _placed(call):
-    """Runs a helper with its first operand's device current, and with `stream`
-    (given: of that device) as the stream that new tensors belong to."""
-    @functools.wraps(call)
-    def placed(X, *args, stream=None, **kw):
-        torch = _torch()
-        device = X.device
-        if device.type != "cuda":
-            raise ValueError(f"expected operands on a GPU, got {device}")
-        if stream is not None:
-            if stream.device != device:
-                raise ValueError(f"operands on {device}, stream of {stream.device}")
-            with torch.cuda.stream(stream):
-                return call(X, *args, stream=stream, **kw)
-        if device.index != torch.cuda.current_device():
-            with torch.cuda.device(device):
-                return call(X, *args, stream=None, **kw)
-        return call(X, *args, stream=None, **kw)
-    return placed
-
-
-def _row_ld(t, size):
-    """Leading dimension of a 2-D tensor with unit column stride; a single row's
+def _row_ld(t, M, N, size):
+    """Leading dimension of an [M, N] tensor with unit column stride; a single row's
     is free, and taken as the row rounded up to 16 bytes."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] != 1):
+    s = t.stride()
+    if s[1] != 1 and N != 1:
         raise ValueError("expected a 2-D tensor with unit column stride")
-    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] * size // 16) * 16 // size
+    return s[0] if M > 1 else -(-N * size // 16) * 16 // size
 
 
-def _vector(t, n, name):
-    torch = _torch()
-    if t is not None and (t.dtype != torch.float32 or t.shape != (n,) or (n > 1 and t.stride(0) != 1)):
-        raise ValueError(f"{name}: expected a contiguous fp32 vector of {n}")
+def _vector(t, n, device, name):
+    """The address of a contiguous fp32 vector of n on `device`, or None."""
+    if t is None:
+        return None
+    if t.dtype is not _torch().float32 or t.dim() != 1 or t.size(0) != n or not t.is_contiguous() or \
+            t.get_device() != device:
+        raise ValueError(f"{name}: expected a contiguous fp32 vector of {n} beside the other operands")
+    return t.data_ptr()
+
+
+def _like(t, shape, dtype, device, name):
+    """t, checked to be of a shape and type on `device`."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        raise ValueError(f"{name}: expected {tuple(shape)} of {dtype} beside the other operands, got {tuple(t.shape)} of "
+                         f"{t.dtype} on {t.device}")
     return t
 
 
-def _same_device(device, *tensors):
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"operands on {device} and {t.device}")
-
-
 _CODES = {"int8": CF_I8, "e4m3": CF_FP8_E4M3}
+_RMSNORM_QUANT_SIZE, _GEMM_I8_SIZE, _PREFIX_SIZE = (C.sizeof(t) for t in (RmsnormQuantArgs, GemmI8Args, AttentionPrefixArgs))
 
 
-@_placed
 def rmsnorm_quant(X, R=None, gamma=None, *, eps=1e-5, norm=True, code="int8", residual=None, out=None, scale=None,
                   stream=None):
     """(Q, s, H): 8-bit codes and row scales of RMSNorm(X + R) * gamma, and H = X + R.
@@ -663,63 +668,77 @@ def rmsnorm_quant(X, R=None, gamma=None, *, eps=1e-5, norm=True, code="int8", re
     names the tensor it goes to, which may be R (in place).  `out` and `scale`
     take Q and s.  Q is what gemm_i8 takes as its tokens, s as sa.
     """
+    if not _here(X, stream):
+        return _elsewhere(rmsnorm_quant, X, stream, R, gamma, eps=eps, norm=norm, code=code, residual=residual, out=out,
+                          scale=scale)
     torch = _torch()
-    M, N = X.shape
-    dt, size = _dt(X), X.element_size()
-    _same_device(X.device, R, gamma, residual, out, scale)
-    for t, name in ((R, "R"), (residual, "residual")):
-        if t is not None and (t.dtype != X.dtype or t.shape != X.shape):
-            raise ValueError(f"{name}: expected {tuple(X.shape)} of {X.dtype}")
-    _vector(gamma, N, "gamma")
+    shape, dtype, device = X.shape, X.dtype, X.get_device()
+    M, N = shape
+    dt = _dt(X)
+    size = 4 if dt == CF_F32 else 2
     qdt = torch.int8 if code == "int8" else torch.uint8
-    Q = out if out is not None else _rows(M, N, qdt, X.device, 1)
-    s = scale if scale is not None else torch.empty((M,), dtype=torch.float32, device=X.device)
-    if Q.shape != X.shape or Q.dtype != qdt:
-        raise ValueError(f"out: expected {tuple(X.shape)} of {qdt}")
-    _vector(s, M, "scale")
-    H = residual if residual is not None else None if R is None else _rows(M, N, X.dtype, X.device, size)
-    a = RmsnormQuantArgs(C.sizeof(RmsnormQuantArgs), M, N, dt, X.data_ptr(), _row_ld(X, size),
-                         _ptr(R), 0 if R is None else _row_ld(R, size), _ptr(H), 0 if H is None else _row_ld(H, size),
-                         _ptr(gamma), 1 if norm else 0, eps, _CODES[code], Q.data_ptr(), _row_ld(Q, 1), s.data_ptr())
-    _check(cf_rmsnorm_quant(a, _stream(stream)))
+    if R is not None:
+        _like(R, shape, dtype, device, "R")
+    H = residual
+    if H is not None:
+        _like(H, shape, dtype, device, "residual")
+    elif R is not None:
+        H = _rows(M, N, dtype, X.device, size)
+    Q = _rows(M, N, qdt, X.device, 1) if out is None else _like(out, shape, qdt, device, "out")
+    s = torch.empty(M, dtype=torch.float32, device=X.device) if scale is None else scale
+    a = RmsnormQuantArgs(_RMSNORM_QUANT_SIZE, M, N, dt, X.data_ptr(), _row_ld(X, M, N, size),
+                         None if R is None else R.data_ptr(), 0 if R is None else _row_ld(R, M, N, size),
+                         None if H is None else H.data_ptr(), 0 if H is None else _row_ld(H, M, N, size),
+                         _vector(gamma, N, device, "gamma"), 1 if norm else 0, eps, _CODES[code], Q.data_ptr(),
+                         _row_ld(Q, M, N, 1), _vector(s, M, device, "scale"))
+    _check(cf_rmsnorm_quant(a, _raw_stream(device)))
     return Q, s, H
 
 
 _ACTS = {"none": CF_ACT_NONE, "gelu": CF_ACT_GELU, "gelu_tanh": CF_ACT_GELU_TANH, "relu": CF_ACT_RELU}
 
 
-@_placed
 def gemm_i8(A, B, sa=None, sb=None, *, bias=None, act="none", out_dtype=None, out=None, stream=None):
     """C = act((A . B^T) * sa[:, None] * sb + bias) of int8 A [M, K] and B [N, K].
 
     sa fp32 [M] (a scale per token), sb fp32 [N] (per channel), bias fp32 [N];
     act "none", "gelu", "gelu_tanh" or "relu"; C bf16 (or fp32) [M, N].
     """
+    if not _here(A, stream):
+        return _elsewhere(gemm_i8, A, stream, B, sa, sb, bias=bias, act=act, out_dtype=out_dtype, out=out)
     torch = _torch()
+    device = A.get_device()
     M, K = A.shape
-    N = B.shape[0]
-    if A.dtype != torch.int8 or B.dtype != torch.int8:
+    N = B.size(0)
+    if A.dtype is not torch.int8 or B.dtype is not torch.int8:
         raise TypeError(f"expected int8 operands, got {A.dtype} and {B.dtype}")
-    if B.shape != (N, K):
-        raise ValueError(f"B: expected [N, {K}], got {tuple(B.shape)}")
-    _same_device(A.device, B, sa, sb, bias, out)
-    _vector(sa, M, "sa")
-    _vector(sb, N, "sb")
-    _vector(bias, N, "bias")
+    _like(B, (N, K), torch.int8, device, "B")
     if out is None:
-        dt = out_dtype or torch.bfloat16
-        Cm = _rows(M, N, dt, A.device, 4 if dt == torch.float32 else 2)
+        dt = CF_F32 if out_dtype is torch.float32 else CF_BF16
+        if dt == CF_BF16 and out_dtype not in (None, torch.bfloat16):
+            raise TypeError(f"unsupported dtype {out_dtype}")
+        Cm = _rows(M, N, torch.float32 if dt == CF_F32 else torch.bfloat16, A.device, 4 if dt == CF_F32 else 2)
     else:
-        Cm = out
-        if Cm.shape != (M, N):
-            raise ValueError(f"out: expected {(M, N)}, got {tuple(Cm.shape)}")
-    a = GemmI8Args(C.sizeof(GemmI8Args), M, N, K, A.data_ptr(), _row_ld(A, 1), B.data_ptr(), _row_ld(B, 1),
-                   _ptr(sa), _ptr(sb), _ptr(bias), _ACTS[act], _dt(Cm), Cm.data_ptr(), _row_ld(Cm, Cm.element_size()))
-    _check(cf_gemm_i8(a, _stream(stream)))
+        dt, Cm = _dt(out), _like(out, (M, N), out_dtype or out.dtype, device, "out")
+    a = GemmI8Args(_GEMM_I8_SIZE, M, N, K, A.data_ptr(), _row_ld(A, M, K, 1), B.data_ptr(), _row_ld(B, N, K, 1),
+                   _vector(sa, M, device, "sa"), _vector(sb, N, device, "sb"), _vector(bias, N, device, "bias"),
+                   _ACTS[act], dt, Cm.data_ptr(), _row_ld(Cm, M, N, 4 if dt == CF_F32 else 2))
+    _check(cf_gemm_i8(a, _raw_stream(device)))
     return Cm
 
 
-@_placed
+def _prefix_workspace(need, device, index):
+    """workspace(need, device, kind="prefix") at less cost: cached per device and stream while nothing is captured."""
+    torch = _torch()
+    if torch._C._cuda_isCurrentStreamCapturing():
+        return workspace(need, device, None, kind="prefix")
+    key = (index, _raw_stream(index), "prefix")
+    ws = _ws_cache.get(key)
+    if ws is None or ws.numel() < need:
+        ws = _ws_cache[key] = torch.empty(need, dtype=torch.uint8, device=device)
+    return ws
+
+
 def attention_prefix(Q, Kp, Vp, Ks=None, Vs=None, lens=None, *, causal=False, scale=None, out=None, ws=None,
                      stream=None):
     """O = softmax(scale * Q [Kp; Ks]^T) [Vp; Vs] for sequences that share the prefix Kp, Vp.
@@ -729,36 +748,45 @@ def attention_prefix(Q, Kp, Vp, Ks=None, Vs=None, lens=None, *, causal=False, sc
     device; None: all S); bf16, d 64 or 128, H a multiple of Hk, any strides that
     are multiples of 8 elements with unit innermost stride (caches stored
     token-major are passed as transposed views).  causal: query i sees the own
-    keys j < lens[b] - (Lq - 1 - i).  A query that sees no key gets 0.
+    keys j < lens[b] - (Lq - 1 - i).  A query that sees no key gets 0.  ws: a
+    workspace of the caller's own (cf_attention_prefix_workspace bytes).
     """
+    if not _here(Q, stream):
+        return _elsewhere(attention_prefix, Q, stream, Kp, Vp, Ks, Vs, lens, causal=causal, scale=scale, out=out, ws=ws)
     torch = _torch()
-    B, H, Lq, d = Q.shape
-    Hk, P = Kp.shape[0], Kp.shape[1]
-    S = 0 if Ks is None else Ks.shape[2]
-    _same_device(Q.device, Kp, Vp, Ks, Vs, lens, out)
+    bf16, device = torch.bfloat16, Q.get_device()
+    shape = Q.shape
+    B, H, Lq, d = shape
+    Hk, P = Kp.size(0), Kp.size(1)
     if (Ks is None) != (Vs is None):
         raise ValueError("Ks and Vs come together")
-    for t, shape, name in ((Kp, (Hk, P, d), "Kp"), (Vp, (Hk, P, d), "Vp"), (Ks, (B, Hk, S, d), "Ks"),
-                           (Vs, (B, Hk, S, d), "Vs"), (out, (B, H, Lq, d), "out")):
-        if t is not None and t.shape != shape:
-            raise ValueError(f"{name}: expected {shape}, got {tuple(t.shape)}")
-    O = out if out is not None else torch.empty_like(Q)
-    for t in (Q, Kp, Vp, Ks, Vs, O):
-        if t is not None and (t.dtype != torch.bfloat16 or t.stride(-1) != 1):
-            raise ValueError("expected bf16 tensors with unit innermost stride")
-    if lens is not None and (lens.dtype != torch.int32 or lens.shape != (B,) or not lens.is_contiguous()):
-        raise ValueError(f"lens: expected a contiguous int32 vector of {B}")
-    ks = (0, 0, 0) if Ks is None else Ks.stride()
-    vs = (0, 0, 0) if Vs is None else Vs.stride()
+    S = 0 if Ks is None else Ks.size(2)
+    _like(Q, shape, bf16, device, "Q")
+    _like(Kp, (Hk, P, d), bf16, device, "Kp")
+    _like(Vp, (Hk, P, d), bf16, device, "Vp")
+    O = torch.empty_like(Q) if out is None else _like(out, shape, bf16, device, "out")
     q, o, kp, vpr = Q.stride(), O.stride(), Kp.stride(), Vp.stride()
-    a = AttentionPrefixArgs(C.sizeof(AttentionPrefixArgs), B, H, Hk, Lq, P, S, d, CF_BF16,
-                            Q.data_ptr(), q[0], q[1], q[2], Kp.data_ptr(), kp[0], kp[1], Vp.data_ptr(), vpr[0], vpr[1],
-                            _ptr(Ks), ks[0], ks[1], ks[2], _ptr(Vs), vs[0], vs[1], vs[2], _ptr(lens),
-                            1 if causal else 0, d ** -0.5 if scale is None else scale,
-                            O.data_ptr(), o[0], o[1], o[2])
+    ks = vs = (0, 0, 0, 1)
+    if Ks is not None:
+        _like(Ks, (B, Hk, S, d), bf16, device, "Ks")
+        _like(Vs, (B, Hk, S, d), bf16, device, "Vs")
+        ks, vs = Ks.stride(), Vs.stride()
+    if not q[3] == o[3] == kp[2] == vpr[2] == ks[3] == vs[3] == 1:
+        raise ValueError("expected unit innermost strides")
+    if lens is not None:
+        _like(lens, (B,), torch.int32, device, "lens")
+        if not lens.is_contiguous():
+            raise ValueError("lens: expected a contiguous vector")
+    a = AttentionPrefixArgs(_PREFIX_SIZE, B, H, Hk, Lq, P, S, d, CF_BF16, Q.data_ptr(), q[0], q[1], q[2],
+                            Kp.data_ptr(), kp[0], kp[1], Vp.data_ptr(), vpr[0], vpr[1],
+                            None if Ks is None else Ks.data_ptr(), ks[0], ks[1], ks[2],
+                            None if Vs is None else Vs.data_ptr(), vs[0], vs[1], vs[2],
+                            None if lens is None else lens.data_ptr(), 1 if causal else 0,
+                            d ** -0.5 if scale is None else scale, O.data_ptr(), o[0], o[1], o[2])
     if ws is None:
         need = cf_attention_prefix_workspace(a)
         if need:
-            ws = workspace(need, Q.device, stream, kind="prefix")
-    _check(cf_attention_prefix(a, _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
+            ws = _prefix_workspace(need, Q.device, device)
+    _check(cf_attention_prefix(a, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
+                               _raw_stream(device)))
     return O

@@ -19,21 +19,29 @@ namespace cf {
 
 namespace {
 
-// QG waves own 32 rows each; KS groups of QG waves share the rows and take the
-// key blocks (BK keys) in turn, each with a ring of two stages in LDS.
-template <int D, int QG_, int KS_, int BK_>
+// QG waves own 32 rows each; KS groups of QG waves share the rows and take the key blocks
+// (BK keys) in turn, each with an LDS ring of its own.  Two forms:
+//   QG = 4, KS = 1, two stages: the next block loads while one is multiplied; a
+//     barrier per block.  For many rows.
+//   QG = 1, KS = 4, one stage per wave: the next keys load as soon as S^T is done, the next
+//     values after P V.  No barrier until the end.  For few rows, where the keys' stream counts.
+// Both fit a CU twice, so that two waves share a SIMD, and a workgroup of one form can run
+// beside one of the other.
+template <int D, int QG_>
 struct PrefixShape {
-  static constexpr int QG = QG_, KS = KS_, NW = QG * KS, NT = 64 * NW, TM = 32 * QG, BK = BK_;
+  static constexpr int QG = QG_, KS = 4 / QG, NW = 4, NT = 256, TM = 32 * QG, BK = QG == 4 ? 64 : 4096 / D;
   static constexpr int NH = BK / 32;              // 32-key parts of a block
   static constexpr int ROW = D * 2, CH = ROW / 16;   // bytes and 16-byte chunks of a key or value row
-  static constexpr int KB = BK * ROW, STAGE = 2 * KB;
-  static constexpr int RING = KS * 2 * STAGE;
+  static constexpr int NS = QG == 1 ? 1 : 2;      // stages
+  static constexpr int KB = BK * ROW, STAGE = 2 * KB, RING = NS * STAGE;
   static constexpr int OROW = D * 4 + 16;         // merge of the groups: one row's fp32 O
   static constexpr int OUT = NW * 32 * (OROW + 8);
-  static constexpr int LDS = RING > OUT ? RING : OUT;
+  static constexpr int LDS = KS * RING > OUT ? KS * RING : OUT;
   static constexpr int DK = D / 16, BD = D / 32;  // MFMA steps over d, 32-wide blocks of d
   static constexpr int NSA = NH * DK, NSB = 2 * NH * BD;
-  static_assert(LDS <= 160 * 1024 && 2 * STAGE <= 65536, "LDS budget, ds offset field");
+  static constexpr int RPI = 64 / CH, NINS = BK / RPI / QG;   // rows of a wave-wide load; a wave's loads of K or V
+  static_assert(QG == 1 || QG == 2 || QG == 4, "forms");
+  static_assert(LDS <= 80 * 1024 && RING <= 65536, "two workgroups a CU, ds offset field");
 };
 
 // Own keys of sequence b, and how many of them query i sees.
@@ -44,49 +52,110 @@ __device__ __forceinline__ int own_seen(const PrefixParams& p, int len, int i) {
   return p.causal ? max(0, len - (p.Lq - 1 - i)) : len;
 }
 
-template <int D, int QG, int KS, int BK>
-__global__ __launch_bounds__(64 * QG * KS, 2) void prefix_kernel(PrefixParams p) {
-  using A = PrefixShape<D, QG, KS, BK>;
-  __shared__ __attribute__((aligned(16))) char smem[A::LDS];
+// 8 d of the output row of query i of head h: o / l, or 0 where the row sees no key.
+__device__ __forceinline__ void store_row(const PrefixParams& p, int b, int h, int i, int d0, const float (&o)[8], float l,
+                                          bool any) {
+  const float inv = any ? 1.0f / l : 0.0f;
+  const u32x4_t w = {pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv),
+                     pack_bf16x2(o[4] * inv, o[5] * inv), pack_bf16x2(o[6] * inv, o[7] * inv)};
+  __builtin_nontemporal_store(w, reinterpret_cast<u32x4_t*>(p.O + b * p.o_b + h * p.o_h + i * p.o_l + d0));
+}
+
+// What a launch computes: whole rows of (sequence, key head) pairs over the prefix
+// and their own keys, or a part of the prefix for the rows of all sequences, or a
+// part of the own keys; the parts' (m, l, O) meet in the workspace.
+enum Kind { WHOLE = 0, PREFIX = 1, OWN = 2 };
+
+// Partial results: fp32 O [slot][row][D], then (m, l) [slot][row]; row (b Hk + hk) R + m.
+struct PartRows {
+  int64_t rows;   // B Hk R
+  __device__ __host__ float* o(const PrefixParams& p, int slot, int64_t row) const {
+    return p.ws + (slot * rows + row) * p.d;
+  }
+  __device__ __host__ float* ml(const PrefixParams& p, int slots, int slot, int64_t row) const {
+    return p.ws + slots * rows * p.d + (slot * rows + row) * 2;
+  }
+};
+
+// Rows m0 .. of (b, hk), or with PREFIX of all sequences of hk, over part z of `parts` of their key
+// blocks.  slots = 0: the output rows; else partial results, this one at `slot`.
+template <int KIND, int D, int QG>
+__device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb, int b, int hk, int z, int parts, int slot,
+                                       int slots) {
+  using A = PrefixShape<D, QG>;
+  constexpr int KS = A::KS, BK = A::BK;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lg = lane >> 5;
-  const int wq = KS == 1 ? wave : wave % QG, grp = KS == 1 ? 0 : wave / QG;
-  const int G = p.H / p.Hk, R = G * p.Lq;
-  const int m0 = blockIdx.x * A::TM;
-  const int hk = blockIdx.y % p.Hk, b = blockIdx.y / p.Hk;
+  const int wq = wave % QG, grp = wave / QG;
+  const int G = p.H / p.Hk, R = G * p.Lq;             // rows of a sequence and key head
+  const int m0 = rb * A::TM, Rall = KIND == PREFIX ? p.B * R : R;
   const float sl2 = p.scale * 1.4426950408889634f;   // scale * log2(e), > 0
   constexpr float kLazy = 8.0f;                       // rescale threshold (log2 units)
 
   // Q fragments (B operand of S^T = K Q^T): this lane's row, 8 d per step.
-  const int m = min(m0 + wq * 32 + lr, R - 1), qi = m / G, qh = hk * G + m % G;
+  const int m = min(m0 + wq * 32 + lr, Rall - 1), qb = KIND == PREFIX ? m / R : b;
+  const int qm = KIND == PREFIX ? m % R : m, qi = qm / G, qh = hk * G + qm % G;
   u32x4_t qf[A::DK];
   {
-    const bf16_t* q = p.Q + b * p.q_b + qh * p.q_h + qi * p.q_l;
+    const bf16_t* q = p.Q + qb * p.q_b + qh * p.q_h + qi * p.q_l;
 #pragma unroll
     for (int ks = 0; ks < A::DK; ++ks) qf[ks] = gload16(q + ks * 16 + lg * 8);
   }
-  const int len = own_len(p, b);
+  const int len = KIND == PREFIX ? 0 : own_len(p, b);
+
+  // Key blocks: those of the prefix, then those of the own keys; [jb, NB) are this part's.
+  const int nbp = KIND == OWN ? 0 : (p.P + BK - 1) / BK;
+  const int last = KIND == PREFIX ? 0 : own_seen(p, len, (min(m0 + A::TM, R) - 1) / G);   // own keys that some row sees
+  const int first = KIND == PREFIX ? 0 : own_seen(p, len, m0 / G);                        // ... that every row sees
+  const int seen = KIND == PREFIX ? 0 : own_seen(p, len, qi);                             // ... that this lane's row sees
+  const int nball = nbp + (last + BK - 1) / BK;
+  // (blocks <= 2^26 and parts <= kMaxParts: the products fit 32 bits)
+  const int jb = (int)((uint32_t)nball * z / (uint32_t)parts), NB = (int)((uint32_t)nball * (z + 1) / (uint32_t)parts);
+  const bf16_t* const Kp = p.Kp + hk * p.kp_h;
+  const bf16_t* const Vp = p.Vp + hk * p.vp_h;
+  const bf16_t* const Ks = p.Ks + b * p.ks_b + hk * p.ks_h;
+  const bf16_t* const Vs = p.Vs + b * p.vs_b + hk * p.vs_h;
 
   // Swizzles of the 16-byte chunks of a row, for the fragment reads (K) and the
   // transposing reads (V); see b2b_attention_kernel.
   auto kswz = [](int row) { return A::CH == 16 ? (row & 15) : ((row >> 1) & 7); };
   auto vswz = [](int row) { return A::CH == 16 ? 4 * (row & 3) : 4 * ((row >> 1) & 1); };
-  constexpr int LPR = A::CH, RPI = 64 / LPR;      // lanes per row, rows per wave-wide load
-  constexpr int NINS = BK / RPI / QG;             // loads per wave for the K or V of a block
-  char* const ring = smem + grp * 2 * A::STAGE;
+  char* const ring = smem + grp * A::RING;
   const uint32_t s0 =
-      (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)smem) + grp * 2 * A::STAGE;
+      (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)smem) + grp * A::RING;
   uint32_t kbase[A::DK], vbase[A::BD];
   const int r16 = lane & 15, vrow = 4 * lg + (r16 >> 2);
 #pragma unroll
   for (int ks = 0; ks < A::DK; ++ks) kbase[ks] = s0 + lr * A::ROW + (((2 * ks + lg) ^ kswz(lr)) << 4);
 #pragma unroll
   for (int d = 0; d < A::BD; ++d)
-    vbase[d] = s0 + vrow * A::ROW + ((((32 * d + (lane & 16) + 4 * (r16 & 3)) >> 3) ^ vswz(vrow)) << 4) + 8 * (r16 & 1);
-  auto lds_sync = [] {
-    __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));
-    lds_barrier();
+    vbase[d] = s0 + A::KB + vrow * A::ROW + ((((32 * d + (lane & 16) + 4 * (r16 & 3)) >> 3) ^ vswz(vrow)) << 4) + 8 * (r16 & 1);
+  auto fence = [] {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // Load `ins` of this wave's share of the keys (or values) of block j.  Rows behind the
+  // last key that may be read are clamped here, masked in P and zeroed in V.
+  const int lrow = lane / A::CH, lch = lane % A::CH;
+  auto load = [&](int j, int stage, auto v_t, int ins) {
+    constexpr bool V = decltype(v_t)::value;
+    const bool own = j >= nbp;
+    const bf16_t* src = V ? (own ? Vs : Vp) : (own ? Ks : Kp);
+    const int64_t ld = V ? (own ? p.vs_l : p.vp_l) : (own ? p.ks_l : p.kp_l);
+    const int in = wq + QG * ins, row = in * A::RPI + lrow, nk = own ? len : p.P;
+    const int key = min((own ? j - nbp : j) * BK + row, nk - 1);
+    dma16(reinterpret_cast<const char*>(src + key * ld) + ((lch ^ (V ? vswz(row) : kswz(row))) << 4),
+          ring + stage * A::STAGE + (V ? A::KB : 0) + in * 1024);
+  };
+  auto load_k = [&](int j, int stage) {
+#pragma unroll
+    for (int i = 0; i < A::NINS; ++i) load(j, stage, std::false_type{}, i);
+  };
+  auto load_v = [&](int j, int stage) {
+#pragma unroll
+    for (int i = 0; i < A::NINS; ++i) load(j, stage, std::true_type{}, i);
   };
 
   f32x16_t O[A::BD];
@@ -96,145 +165,156 @@ __global__ __launch_bounds__(64 * QG * KS, 2) void prefix_kernel(PrefixParams p)
     for (int e = 0; e < 16; ++e) O[d][e] = 0.0f;
   float m_used = -INFINITY, lsum = 0.0f;
 
-  using S0_ = std::integral_constant<int, 0>;
-  using S1_ = std::integral_constant<int, 1>;
-  // The prefix, then the sequence's own keys.
-#pragma unroll 1
-  for (int seg = 0; seg < 2; ++seg) {
-    const bf16_t* Kb = seg == 0 ? p.Kp + hk * p.kp_h : p.Ks + b * p.ks_b + hk * p.ks_h;
-    const bf16_t* Vb = seg == 0 ? p.Vp + hk * p.vp_h : p.Vs + b * p.vs_b + hk * p.vs_h;
-    const int64_t ldk = seg == 0 ? p.kp_l : p.ks_l, ldv = seg == 0 ? p.vp_l : p.vs_l;
-    const int nk = seg == 0 ? p.P : len;                       // keys that may be read
-    const int lim = seg == 0 ? p.P : own_seen(p, len, qi);     // keys that this lane's row sees
-    const int first = seg == 0 ? p.P : own_seen(p, len, m0 / G);   // ... that every row sees
-    const int last = seg == 0 ? p.P : own_seen(p, len, (min(m0 + A::TM, R) - 1) / G);   // ... that some row sees
-    const int NB = (last + BK - 1) / BK;
-
-    auto issue_kv = [&](int j, auto stage_t) {
-      char* dst = ring + decltype(stage_t)::value * A::STAGE;
-#pragma unroll
-      for (int ins = 0; ins < NINS; ++ins) {
-        const int in = wq + QG * ins, row = in * RPI + lane / LPR;
-        const int key = min(j * BK + row, nk - 1);   // rows behind nk: clamped here, masked in P, zeroed in V
-        dma16(reinterpret_cast<const char*>(Kb + key * ldk) + (((lane % LPR) ^ kswz(row)) << 4), dst + in * 1024);
-        dma16(reinterpret_cast<const char*>(Vb + key * ldv) + (((lane % LPR) ^ vswz(row)) << 4),
-              dst + A::KB + in * 1024);
-      }
-    };
-    auto step = [&](int j, auto stage_t, auto next_t) {
-      constexpr int ST = decltype(stage_t)::value * A::STAGE;
+  auto step = [&](int j, auto stage_t) {
+    constexpr int SG = decltype(stage_t)::value, ST = SG * A::STAGE;
+    const bool own = j >= nbp, next = j + KS < NB;
+    const int k0 = (own ? j - nbp : j) * BK;
+    if constexpr (QG == 1) {
+      wait_vmcnt<A::NINS>();   // the keys; the values may be on their way
+      fence();
+    } else {
       wait_vmcnt<0>();
-      lds_sync();
-      if (j >= NB) return;
-      if (j + KS < NB) issue_kv(j + KS, next_t);
-      // S^T = K Q^T
-      f32x16_t S[A::NH];
-      {
-        constexpr int KLA = 4;
-        const f32x16_t zero = {};
-        auto kread = [&](auto i_t) {
-          constexpr int i = decltype(i_t)::value;
-          return ds_read_b128_at<ST + (i % A::NH) * 32 * A::ROW>(kbase[i / A::NH]);
-        };
-        u32x4_t kf[KLA];
-        static_for<0, KLA>([&](auto i_t) { kf[decltype(i_t)::value] = kread(i_t); });
-        static_for<0, A::NSA>([&](auto i_t) {
-          constexpr int i = decltype(i_t)::value, h = i % A::NH, ks = i / A::NH, rest = A::NSA - 1 - i;
-          lgkm_wait<(rest < KLA - 1 ? rest : KLA - 1)>(kf[i % KLA]);
-          S[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[i % KLA]),
-                                                         __builtin_bit_cast(bf16x8_t, qf[ks]), ks == 0 ? zero : S[h], 0,
-                                                         0, 0);
-          if constexpr (i + KLA < A::NSA) kf[(i + KLA) % KLA] = kread(std::integral_constant<int, i + KLA>{});
-          __builtin_amdgcn_sched_barrier(0);
-        });
-      }
-      const bool mask = (j + 1) * BK > first;   // some row of the workgroup does not see the whole block
-      if (mask) {
-#pragma unroll
-        for (int e = 0; e < 16 * A::NH; ++e) {
-          const int key = j * BK + (e >> 4) * 32 + acc_row(e & 15, lane);
-          if (key >= lim) S[e >> 4][e & 15] = -INFINITY;
-        }
-      }
-      // softmax of the block
-      float t = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < 16 * A::NH; ++e) t = fmaxf(t, S[e >> 4][e & 15]);
-      const float mnew = fmaxf(m_used, lane_pair_max(t) * sl2);
-      const bool need = mnew > m_used + kLazy;
-      const float m_eff = need ? mnew : m_used;
-      const float corr = need ? __builtin_amdgcn_exp2f(m_used - m_eff) : 1.0f;
-      m_used = m_eff;
-      const float nm = m_used == -INFINITY ? 0.0f : -m_used;   // nothing seen yet: P are 0
-      u32x4_t P[A::NH][2];
+      __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));   // this wave's LDS reads
+      lds_barrier();           // the block is in, and every wave is done with the other stage
+      if (KS > 1 && j >= NB) return;   // this group has no block in the last step
+    }
+    // S^T = K Q^T: one LDS read per MFMA, four ahead.  With two stages the next block's loads
+    // go between the MFMAs: in a row they would hold the wave up.
+    f32x16_t S[A::NH];
+    {
+      constexpr int KLA = 4;
+      constexpr int SPC = A::NSA / (2 * A::NINS) > 0 ? A::NSA / (2 * A::NINS) : 1;   // MFMAs per load
+      constexpr int LPM = 2 * A::NINS > A::NSA ? 2 * A::NINS / A::NSA : 1;          // loads per MFMA
+      const f32x16_t zero = {};
+      auto kread = [&](auto i_t) {
+        constexpr int i = decltype(i_t)::value;
+        return ds_read_b128_at<ST + (i % A::NH) * 32 * A::ROW>(kbase[i / A::NH]);
+      };
+      u32x4_t kf[KLA];
+      static_for<0, KLA>([&](auto i_t) { kf[decltype(i_t)::value] = kread(i_t); });
+      static_for<0, A::NSA>([&](auto i_t) {
+        constexpr int i = decltype(i_t)::value, h = i % A::NH, ks = i / A::NH, rest = A::NSA - 1 - i;
+        lgkm_wait<(rest < KLA - 1 ? rest : KLA - 1)>(kf[i % KLA]);
+        S[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[i % KLA]),
+                                                       __builtin_bit_cast(bf16x8_t, qf[ks]), ks == 0 ? zero : S[h], 0, 0,
+                                                       0);
+        if constexpr (i + KLA < A::NSA) kf[(i + KLA) % KLA] = kread(std::integral_constant<int, i + KLA>{});
+        if constexpr (A::NS == 2)
+          if (next)
+            static_for<0, LPM>([&](auto l_t) {
+              constexpr int q = i / SPC * LPM + decltype(l_t)::value;
+              if constexpr (i % SPC == SPC - 1 && q < 2 * A::NINS)
+                load(j + KS, 1 - SG, std::integral_constant<bool, (q >= A::NINS)>{}, q % A::NINS);
+            });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    }
+    if constexpr (QG == 1) {
+      fence();   // the last read of the keys has returned
+      if (next) load_k(j + KS, 0);
+    }
+    if (k0 + BK > (own ? first : p.P)) {   // some row of the workgroup does not see the whole block
+      const int lim = own ? seen : p.P;
 #pragma unroll
       for (int e = 0; e < 16 * A::NH; ++e)
-        S[e >> 4][e & 15] = __builtin_amdgcn_exp2f(fmaf(S[e >> 4][e & 15], sl2, nm));
-#pragma unroll
-      for (int h = 0; h < A::NH; ++h) {
-        P[h][0] = pack_step(S[h], 0);
-        P[h][1] = pack_step(S[h], 1);
-      }
-      if (__any(need)) {
-#pragma unroll
-        for (int d = 0; d < A::BD; ++d)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) O[d][e] *= corr;
-        lsum *= corr;
-      }
-      // O^T += V^T P^T; in a block that reaches behind nk the values there are
-      // zeroed (0 * NaN would not be 0)
-      auto pv = [&](auto mask_t) {
-        constexpr int VT = ST + A::KB;
-        auto vfrag = [&](auto i_t) {
-          constexpr int i = decltype(i_t)::value;
-          constexpr int d = i % A::BD, s = (i / A::BD) & 1, h = i / (2 * A::BD);
-          constexpr int off = VT + (32 * h + 16 * s) * A::ROW;
-          const u32x2_t lo = ds_read_tr_b64<off>(vbase[d]);
-          const u32x2_t hi = ds_read_tr_b64<off + 8 * A::ROW>(vbase[d]);
-          return u32x4_t{lo[0], lo[1], hi[0], hi[1]};
-        };
-        u32x4_t vf[3];
-        vf[0] = vfrag(std::integral_constant<int, 0>{});
-        vf[1] = vfrag(std::integral_constant<int, 1>{});
-        static_for<0, A::NSB>([&](auto i_t) {
-          constexpr int i = decltype(i_t)::value;
-          constexpr int d = i % A::BD, s = (i / A::BD) & 1, h = i / (2 * A::BD);
-          lgkm_wait<(i + 1 < A::NSB ? 2 : 0)>(vf[i % 3]);
-          u32x4_t v = vf[i % 3];
-          if constexpr (decltype(mask_t)::value) {
-            const int left = nk - (j * BK + 32 * h + 16 * s + 4 * lg);   // of the 4 keys of v[0..1]; v[2..3]: 8 on
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int l = left - (e < 2 ? 2 * e : 8 + 2 * (e - 2));
-              v[e] = l >= 2 ? v[e] : l == 1 ? v[e] & 0xFFFFu : 0u;
-            }
-          }
-          Mma<bf16_t>::run(O[d], v, P[h][s]);
-          if constexpr (i + 2 < A::NSB) vf[(i + 2) % 3] = vfrag(std::integral_constant<int, i + 2>{});
-          __builtin_amdgcn_sched_barrier(0);
-        });
-      };
-      if ((j + 1) * BK > nk) pv(std::true_type{});
-      else pv(std::false_type{});
-      // the row sum from the same bf16 P as the numerator
-      typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-      const bf16x2_t one2 = __builtin_bit_cast(bf16x2_t, 0x3F803F80u);
-#pragma unroll
-      for (int q = 0; q < 2 * A::NH; ++q)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t x = P[q >> 1][q & 1][e];
-          lsum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x), one2, lsum, false);
-        }
-    };
-    if (grp < NB) issue_kv(grp, S0_{});
-    for (int j = 0; j < NB; j += 2 * KS) {
-      step(j + grp, S0_{}, S1_{});
-      if (j + KS < NB) step(j + KS + grp, S1_{}, S0_{});
+        if (k0 + (e >> 4) * 32 + acc_row(e & 15, lane) >= lim) S[e >> 4][e & 15] = -INFINITY;
     }
-    __syncthreads();   // the rings are free for the next segment, or for the merge
+    // softmax of the block
+    float t = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16 * A::NH; ++e) t = fmaxf(t, S[e >> 4][e & 15]);
+    const float mnew = fmaxf(m_used, lane_pair_max(t) * sl2);
+    const bool need = mnew > m_used + kLazy;
+    const float m_eff = need ? mnew : m_used;
+    const float corr = need ? __builtin_amdgcn_exp2f(m_used - m_eff) : 1.0f;
+    m_used = m_eff;
+    const float nm = m_used == -INFINITY ? 0.0f : -m_used;   // nothing seen yet: P are 0
+    u32x4_t P[A::NH][2];
+#pragma unroll
+    for (int e = 0; e < 16 * A::NH; ++e)
+      S[e >> 4][e & 15] = __builtin_amdgcn_exp2f(fmaf(S[e >> 4][e & 15], sl2, nm));
+#pragma unroll
+    for (int h = 0; h < A::NH; ++h) {
+      P[h][0] = pack_step(S[h], 0);
+      P[h][1] = pack_step(S[h], 1);
+    }
+    if (__any(need)) {
+#pragma unroll
+      for (int d = 0; d < A::BD; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) O[d][e] *= corr;
+      lsum *= corr;
+    }
+    if constexpr (QG == 1) {   // the values; the next keys may be on their way
+      if (next) wait_vmcnt<A::NINS>();
+      else wait_vmcnt<0>();
+      fence();
+    }
+    // O^T += V^T P^T; in a block that reaches behind the last key the values there are
+    // zeroed (0 * NaN would not be 0)
+    const int nk = own ? len : p.P;
+    auto pv = [&](auto mask_t) {
+      auto vfrag = [&](auto i_t) {
+        constexpr int i = decltype(i_t)::value;
+        constexpr int d = i % A::BD, s = (i / A::BD) & 1, h = i / (2 * A::BD);
+        constexpr int off = ST + (32 * h + 16 * s) * A::ROW;
+        const u32x2_t lo = ds_read_tr_b64<off>(vbase[d]);
+        const u32x2_t hi = ds_read_tr_b64<off + 8 * A::ROW>(vbase[d]);
+        return u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+      };
+      u32x4_t vf[3];
+      vf[0] = vfrag(std::integral_constant<int, 0>{});
+      vf[1] = vfrag(std::integral_constant<int, 1>{});
+      static_for<0, A::NSB>([&](auto i_t) {
+        constexpr int i = decltype(i_t)::value;
+        constexpr int d = i % A::BD, s = (i / A::BD) & 1, h = i / (2 * A::BD);
+        lgkm_wait<(i + 1 < A::NSB ? 2 : 0)>(vf[i % 3]);
+        u32x4_t v = vf[i % 3];
+        if constexpr (decltype(mask_t)::value) {
+          const int left = nk - (k0 + 32 * h + 16 * s + 4 * lg);   // of the 4 keys of v[0..1]; v[2..3]: 8 on
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int l = left - (e < 2 ? 2 * e : 8 + 2 * (e - 2));
+            v[e] = l >= 2 ? v[e] : l == 1 ? v[e] & 0xFFFFu : 0u;
+          }
+        }
+        Mma<bf16_t>::run(O[d], v, P[h][s]);
+        if constexpr (i + 2 < A::NSB) vf[(i + 2) % 3] = vfrag(std::integral_constant<int, i + 2>{});
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+    if (k0 + BK > nk) pv(std::true_type{});
+    else pv(std::false_type{});
+    if constexpr (QG == 1) {
+      fence();   // the last read of the values has returned
+      if (next) load_v(j + KS, 0);
+    }
+    // the row sum from the same bf16 P as the numerator
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    const bf16x2_t one2 = __builtin_bit_cast(bf16x2_t, 0x3F803F80u);
+#pragma unroll
+    for (int q = 0; q < 2 * A::NH; ++q)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t x = P[q >> 1][q & 1][e];
+        lsum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x), one2, lsum, false);
+      }
+  };
+  using S0_ = std::integral_constant<int, 0>;
+  using S1_ = std::integral_constant<int, 1>;
+  if (jb + grp < NB) {
+    load_k(jb + grp, 0);
+    load_v(jb + grp, 0);
   }
+  if constexpr (QG == 1) {
+    for (int j = jb + grp; j < NB; j += KS) step(j, S0_{});
+  } else {
+    for (int j = jb; j < NB; j += 2 * KS) {   // every group runs the same number of steps (the barriers are the workgroup's)
+      step(j + grp, S0_{});
+      if (j + KS < NB) step(j + KS + grp, S1_{});
+    }
+  }
+  __syncthreads();   // the rings are free for the merge
 
   // Every wave leaves its O and (m, l) in LDS; thread t takes 8 d of a row and adds
   // the groups in order, scaled to the common maximum.
@@ -253,7 +333,8 @@ __global__ __launch_bounds__(64 * QG * KS, 2) void prefix_kernel(PrefixParams p)
   }
   __syncthreads();
   constexpr int TPR = D / 8;
-  const int rows = min(A::TM, R - m0), d0 = tid % TPR * 8;
+  const int rows = min(A::TM, Rall - m0), d0 = tid % TPR * 8;
+  const PartRows pr{(int64_t)p.B * p.Hk * R};
   for (int r = tid / TPR; r < rows; r += A::NT / TPR) {
     float mg[KS], M = -INFINITY, L = 0.0f, o[8] = {};
 #pragma unroll
@@ -271,31 +352,204 @@ __global__ __launch_bounds__(64 * QG * KS, 2) void prefix_kernel(PrefixParams p)
         o[4 + e] = fmaf(f, y[e], o[4 + e]);
       }
     }
-    const int i = (m0 + r) / G, h = hk * G + (m0 + r) % G;
-    const float inv = p.P + own_seen(p, len, i) > 0 ? 1.0f / L : 0.0f;   // a row without keys: 0
-    const u32x4_t w = {pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv),
-                       pack_bf16x2(o[4] * inv, o[5] * inv), pack_bf16x2(o[6] * inv, o[7] * inv)};
-    __builtin_nontemporal_store(w, reinterpret_cast<u32x4_t*>(p.O + b * p.o_b + h * p.o_h + i * p.o_l + d0));
+    const int ob = KIND == PREFIX ? (m0 + r) / R : b, om = KIND == PREFIX ? (m0 + r) % R : m0 + r;
+    if (KIND == WHOLE && slots == 0) {
+      const int i = om / G;
+      store_row(p, ob, hk * G + om % G, i, d0, o, L, p.P + own_seen(p, len, i) > 0);
+    } else {
+      const int64_t row = (int64_t)(ob * p.Hk + hk) * R + om;
+      float* dst = pr.o(p, slot, row) + d0;
+      *reinterpret_cast<f32x4_t*>(dst) = f32x4_t{o[0], o[1], o[2], o[3]};
+      *reinterpret_cast<f32x4_t*>(dst + 4) = f32x4_t{o[4], o[5], o[6], o[7]};
+      if (d0 == 0) {
+        float* to = pr.ml(p, slots, slot, row);
+        to[0] = M;
+        to[1] = L;
+      }
+    }
   }
 }
 
-template <int D, int QG, int KS, int BK>
-hipError_t launch_direct(const PrefixParams& p, hipStream_t st) {
-  using A = PrefixShape<D, QG, KS, BK>;
-  const int R = p.H / p.Hk * p.Lq;
-  hipLaunchKernelGGL((prefix_kernel<D, QG, KS, BK>), dim3((unsigned)((R + A::TM - 1) / A::TM), (unsigned)(p.B * p.Hk)),
-                     dim3(A::NT), 0, st, p);
+// Workgroup L of T runs on XCD L % 8; an XCD takes a contiguous range of tasks, so that
+// neighbouring ones share keys in its L2.
+__device__ __forceinline__ int xcd_task(int L, int T) {
+  const int x = L & 7, q = T >> 3, r = T & 7;
+  return x * q + min(x, r) + (L >> 3);
+}
+
+// One launch over (key head, sequence, part, row block).  Later row blocks first: with
+// causal they see more keys.
+template <int D, int QG>
+__global__ __launch_bounds__(256, 2) void prefix_whole_kernel(PrefixParams p, int nrb, int parts) {
+  __shared__ __attribute__((aligned(16))) char smem[PrefixShape<D, QG>::LDS];
+  int t = xcd_task(blockIdx.x, gridDim.x);
+  const int rb = nrb - 1 - t % nrb;
+  t /= nrb;
+  const int z = t % parts;
+  t /= parts;
+  attend<WHOLE, D, QG>(p, smem, rb, t % p.B, t / p.B, z, parts, z, parts > 1 ? parts : 0);
+}
+
+// The parts of the prefix, (key head, part, row block over all sequences), then those of the own
+// keys, (key head, sequence, part, row block).  The prefix's, bound by the MFMAs, run beside the
+// own keys', which memory bounds.
+template <int D, int PQ, int OQ>
+__global__ __launch_bounds__(256, 2) void prefix_split_kernel(PrefixParams p, int tp, int nrb_p, int np, int nrb_o, int ns) {
+  __shared__ __attribute__((aligned(16)))
+  char smem[PrefixShape<D, PQ>::LDS > PrefixShape<D, OQ>::LDS ? PrefixShape<D, PQ>::LDS : PrefixShape<D, OQ>::LDS];
+  if ((int)blockIdx.x < tp) {
+    int t = xcd_task(blockIdx.x, tp);
+    const int rb = t % nrb_p;
+    t /= nrb_p;
+    attend<PREFIX, D, PQ>(p, smem, rb, 0, t / np, t % np, np, t % np, np + ns);
+  } else {
+    int t = xcd_task(blockIdx.x - tp, gridDim.x - tp);
+    const int rb = nrb_o - 1 - t % nrb_o;
+    t /= nrb_o;
+    const int z = t % ns;
+    t /= ns;
+    attend<OWN, D, OQ>(p, smem, rb, t % p.B, t / p.B, z, ns, np + z, np + ns);
+  }
+}
+
+// The parts of every row: D / 8 threads for 8 d each, times WAYS that take the parts in
+// turn and join in LDS, so that few trips to memory follow one another.
+template <int D, int WAYS>
+__global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixParams p, int slots) {
+  constexpr int TPR = D / 8, ROWS = 256 / TPR / WAYS;
+  __shared__ __attribute__((aligned(16))) float so[WAYS][ROWS][D];
+  __shared__ float sml[WAYS][ROWS][2];
+  const int G = p.H / p.Hk, R = G * p.Lq;
+  const int rows = p.B * p.Hk * R;              // at most 2^30
+  const PartRows pr{rows};
+  const int way = threadIdx.x / TPR % WAYS, r = threadIdx.x / TPR / WAYS, d0 = threadIdx.x % TPR * 8;
+  const int row = min((int)blockIdx.x * ROWS + r, rows - 1);
+  const float* const o0 = pr.o(p, 0, row) + d0;
+  const float* const ml0 = pr.ml(p, slots, 0, row);
+  float M = -INFINITY, L = 0.0f, o[8] = {};
+  auto join = [&](float mz, float lz, const f32x4_t& x, const f32x4_t& y) {
+    const float mn = fmaxf(M, mz);
+    const float fo = M == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M - mn);
+    const float fz = mz == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mz - mn);
+    M = mn;
+    L = fmaf(fz, lz, fo * L);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      o[e] = fmaf(fz, x[e], fo * o[e]);
+      o[4 + e] = fmaf(fz, y[e], fo * o[4 + e]);
+    }
+  };
+  for (int s0 = way; s0 < slots; s0 += 4 * WAYS) {   // four parts' loads in flight
+    f32x4_t x[4], y[4];
+    float mz[4], lz[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t s = min(s0 + q * WAYS, slots - 1);
+      x[q] = *reinterpret_cast<const f32x4_t*>(o0 + s * rows * D);
+      y[q] = *reinterpret_cast<const f32x4_t*>(o0 + s * rows * D + 4);
+      mz[q] = ml0[s * rows * 2];
+      lz[q] = ml0[s * rows * 2 + 1];
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (s0 + q * WAYS < slots) join(mz[q], lz[q], x[q], y[q]);
+  }
+  const int m = row % R, bh = row / R, hk = bh % p.Hk, b = bh / p.Hk, i = m / G;
+  const bool any = p.P + own_seen(p, own_len(p, b), i) > 0;
+  if constexpr (WAYS > 1) {
+    *reinterpret_cast<f32x4_t*>(&so[way][r][d0]) = f32x4_t{o[0], o[1], o[2], o[3]};
+    *reinterpret_cast<f32x4_t*>(&so[way][r][d0 + 4]) = f32x4_t{o[4], o[5], o[6], o[7]};
+    if (d0 == 0) {
+      sml[way][r][0] = M;
+      sml[way][r][1] = L;
+    }
+    __syncthreads();
+    if (way != 0) return;
+#pragma unroll
+    for (int w = 1; w < WAYS; ++w)
+      join(sml[w][r][0], sml[w][r][1], *reinterpret_cast<const f32x4_t*>(&so[w][r][d0]),
+           *reinterpret_cast<const f32x4_t*>(&so[w][r][d0 + 4]));
+  }
+  if ((int)blockIdx.x * ROWS + r < rows) store_row(p, b, hk * G + m % G, i, d0, o, L, any);
+}
+
+// ---------------------------------------------------------------------------
+// How a call is cut.
+// ---------------------------------------------------------------------------
+struct PrefixPlan {
+  int pq, oq;   // 32-row waves of a workgroup: prefix parts, own parts or whole rows
+  int np, ns;   // split: parts of the prefix and of the own keys.  ns = 0: whole rows in np parts
+  int slots() const { return ns > 0 ? np + ns : np > 1 ? np : 0; }
+};
+constexpr int kCUs = 256, kMaxParts = 32;
+
+int query_waves(int64_t rows) { return rows <= 32 ? 1 : 4; }
+int64_t row_blocks(int64_t rows, int qg) { return (rows + 32 * qg - 1) / (32 * qg); }
+
+PrefixPlan make_plan(const PrefixParams& p) {
+  const int64_t R = (int64_t)(p.H / p.Hk) * p.Lq, Rall = p.B * R;
+  PrefixPlan pl{query_waves(Rall), query_waves(R), 1, 0};
+  const char* force = getenv("CF_PREFIX");
+  if (force && force[0] == '1') {
+    sscanf(force, "1,%d", &pl.np);
+    return pl;
+  }
+  const int64_t own = row_blocks(R, pl.oq) * p.B * p.Hk;
+  if ((R >= 64 && own >= kCUs) || p.P == 0 || p.S == 0) return pl;
+  {
+    const int64_t w = row_blocks(Rall, pl.pq) * p.Hk;
+    const int64_t per = 64 * 4;
+    pl.np = (int)std::max<int64_t>(1, std::min<int64_t>({(kCUs + w - 1) / w, p.P / per, 32}));
+  }
+  pl.ns = (int)std::max<int64_t>(1, std::min<int64_t>({kCUs / own, p.S / 256, 16}));
+  if (force) sscanf(force, "2,%d,%d,%d", &pl.np, &pl.ns, &pl.pq);
+  return pl;
+}
+
+template <int D, int QG>
+hipError_t launch_whole(const PrefixParams& p, int parts, hipStream_t st) {
+  const int64_t R = (int64_t)(p.H / p.Hk) * p.Lq, nrb = row_blocks(R, QG), wgs = nrb * parts * p.Hk * p.B;
+  hipLaunchKernelGGL((prefix_whole_kernel<D, QG>), dim3((unsigned)wgs), dim3(256), 0, st, p, (int)nrb, parts);
   return hipGetLastError();
+}
+
+template <int D, int PQ, int OQ>
+hipError_t launch_split(const PrefixParams& p, const PrefixPlan& pl, hipStream_t st) {
+  const int64_t R = (int64_t)(p.H / p.Hk) * p.Lq, nrb_p = row_blocks(p.B * R, PQ), nrb_o = row_blocks(R, OQ);
+  const int64_t tp = nrb_p * pl.np * p.Hk, to = nrb_o * pl.ns * p.Hk * p.B;
+  hipLaunchKernelGGL((prefix_split_kernel<D, PQ, OQ>), dim3((unsigned)(tp + to)), dim3(256), 0, st, p, (int)tp, (int)nrb_p,
+                     pl.np, (int)nrb_o, pl.ns);
+  return hipGetLastError();
+}
+
+template <int D, int WAYS>
+hipError_t launch_merge(const PrefixParams& p, int slots, hipStream_t st) {
+  const int64_t rows = (int64_t)p.B * p.H * p.Lq, per = 256 / (D / 8) / WAYS;
+  hipLaunchKernelGGL((prefix_merge_kernel<D, WAYS>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, p, slots);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_all(const PrefixParams& p, const PrefixPlan& pl, hipStream_t st) {
+  hipError_t e;
+  if (pl.ns == 0) e = pl.oq == 1 ? launch_whole<D, 1>(p, pl.np, st) : launch_whole<D, 4>(p, pl.np, st);
+  else if (pl.pq == 1) e = launch_split<D, 1, 1>(p, pl, st);
+  else if (pl.pq == 2) e = launch_split<D, 2, 1>(p, pl, st);
+  else e = pl.oq == 1 ? launch_split<D, 4, 1>(p, pl, st) : launch_split<D, 4, 4>(p, pl, st);
+  if (e != hipSuccess || pl.slots() == 0) return e;
+  return pl.slots() <= 4 ? launch_merge<D, 1>(p, pl.slots(), st)
+                         : pl.slots() <= 16 ? launch_merge<D, 4>(p, pl.slots(), st) : launch_merge<D, 8>(p, pl.slots(), st);
 }
 
 }  // namespace
 
-size_t prefix_workspace(const PrefixParams&) { return 0; }
+size_t prefix_workspace(const PrefixParams& p) {
+  return (size_t)make_plan(p).slots() * (size_t)p.B * (size_t)p.H * (size_t)p.Lq * (size_t)(p.d + 2) * 4;
+}
 
 hipError_t launch_prefix(const PrefixParams& p, hipStream_t st) {
-  const bool few = p.H / p.Hk * p.Lq <= 32;
-  if (p.d == 128) return few ? launch_direct<128, 1, 4, 32>(p, st) : launch_direct<128, 4, 1, 64>(p, st);
-  return few ? launch_direct<64, 1, 8, 32>(p, st) : launch_direct<64, 4, 1, 64>(p, st);
+  const PrefixPlan pl = make_plan(p);
+  return p.d == 128 ? launch_all<128>(p, pl, st) : launch_all<64>(p, pl, st);
 }
 
 }  // namespace cf

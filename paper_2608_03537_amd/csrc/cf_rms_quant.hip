@@ -24,34 +24,40 @@ constexpr float kSmall = 8.6736173798840355e-19f;                               
 template <typename T, int E>
 __device__ __forceinline__ void load_chunk(const T* p, int left, float (&v)[E]) {
   if (left >= E) {
+    const u32x4_t u = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
 #pragma unroll
-    for (int i = 0; i < E; i += 4) {
-      float q[4];
-      load4_once<T>(p + i, q);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[i + e] = q[e];
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        v[i] = __uint_as_float(u[i]);
+      } else {
+        v[2 * i] = bf16_to_f32(u[i] & 0xFFFFu);
+        v[2 * i + 1] = bf16_to_f32(u[i] >> 16);
+      }
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      v[i] = 0.0f;
+    for (int i = 0; i < E; ++i) v[i] = 0.0f;
+    if (left <= 0) return;
+#pragma unroll
+    for (int i = 0; i < E; ++i)
       if (i < left) {
         if constexpr (sizeof(T) == 4) v[i] = p[i];
         else v[i] = bf16_to_f32(p[i]);
       }
-    }
   }
 }
 
 template <typename T, int E>
 __device__ __forceinline__ void store_chunk(T* p, int left, const float (&v)[E]) {
   if (left >= E) {
+    u32x4_t u;
 #pragma unroll
-    for (int i = 0; i < E; i += 4) {
-      const float q[4] = {v[i], v[i + 1], v[i + 2], v[i + 3]};
-      store4(p, i, sizeof(T) == 4, q);
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) u[i] = __float_as_uint(v[i]);
+      else u[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
     }
-  } else {
+    __builtin_nontemporal_store(u, reinterpret_cast<u32x4_t*>(p));
+  } else if (left > 0) {
 #pragma unroll
     for (int i = 0; i < E; ++i)
       if (i < left) {
@@ -103,6 +109,7 @@ __global__ __launch_bounds__(NT) void rms_quant_kernel(RmsQuantParams p) {
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int n = (c * TPR + t) * E;
+    if (n >= p.N) break;
     if (p.H) store_chunk<T, E>(H + n, p.N - n, v[c]);
 #pragma unroll
     for (int e = 0; e < E; ++e) ss = fmaf(v[c][e], v[c][e], ss);
@@ -162,6 +169,7 @@ __global__ __launch_bounds__(NT) void rms_quant_kernel(RmsQuantParams p) {
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int n = (c * TPR + t) * E;
+    if (n >= p.N) break;
     uint32_t w[E / 4];
 #pragma unroll
     for (int i = 0; i < E; i += 4) {
@@ -185,25 +193,36 @@ __global__ __launch_bounds__(NT) void rms_quant_kernel(RmsQuantParams p) {
 template <typename T, int TPR, int C, int NT>
 hipError_t launch(const RmsQuantParams& p, hipStream_t st) {
   constexpr int ROWS = NT / TPR;
-  static_assert(TPR * C * (16 / sizeof(T)) <= kRmsQuantMaxN, "widest row");
   hipLaunchKernelGGL((rms_quant_kernel<T, TPR, C, NT>), dim3((unsigned)((p.M + ROWS - 1) / ROWS)), dim3(NT), 0, st, p);
   return hipGetLastError();
 }
 
 }  // namespace
 
+// The narrowest form that holds a row: chunks behind N cost their checks, and more threads a
+// row with fewer chunks keep more rows of loads in flight.  Measured (us; 16 bytes a thread and
+// chunk): 16384 x 4096 bf16 with residual 80 on 256 threads x 2 chunks, 86 on 512 x 2, 93 on 256 x 4, 115 on
+// 64 x 8; 4096 x 16384 bf16 without 39 on 1024 x 2, 46 on 512 x 4, 69 on 256 x 8; 65536 x 1024 77 on 64 x
+// 2, 117 on 256 x 2; 16384 x 2048 45 on 64 x 4; fp32 8192 x 4096 74 on 512 x 2, 777 x 5120 6.7 on 512 x 4 and 8.2
+// on 1024 x 2.  16384 x 4096 is 470 MB at 5.8 TB/s: with three sets of operands in turn part of it comes
+// from the last-level cache (a large copy reaches 4.8).  One row takes about 4 us, the launch.
 hipError_t launch_rms_quant(const RmsQuantParams& p, hipStream_t st) {
-  const int chunks = (p.N + (p.f32 ? 3 : 7)) / (p.f32 ? 4 : 8);
   if (p.f32) {
-    if (chunks <= 64) return launch<float, 64, 1, 256>(p, st);
-    if (chunks <= 256) return launch<float, 64, 4, 256>(p, st);
-    if (chunks <= 1024) return launch<float, 256, 4, 256>(p, st);
-    if (chunks <= 2048) return launch<float, 256, 8, 256>(p, st);
+    if (p.N <= 256) return launch<float, 64, 1, 256>(p, st);
+    if (p.N <= 512) return launch<float, 64, 2, 256>(p, st);
+    if (p.N <= 1024) return launch<float, 64, 4, 256>(p, st);
+    if (p.N <= 2048) return launch<float, 256, 2, 256>(p, st);
+    if (p.N <= 4096) return launch<float, 512, 2, 512>(p, st);
+    if (p.N <= 8192) return launch<float, 512, 4, 512>(p, st);
+    if (p.N <= 16384) return launch<float, 1024, 4, 1024>(p, st);
     return launch<float, 1024, 8, 1024>(p, st);
   }
-  if (chunks <= 64) return launch<bf16_t, 64, 1, 256>(p, st);
-  if (chunks <= 256) return launch<bf16_t, 64, 4, 256>(p, st);
-  if (chunks <= 1024) return launch<bf16_t, 256, 4, 256>(p, st);
+  if (p.N <= 512) return launch<bf16_t, 64, 1, 256>(p, st);
+  if (p.N <= 1024) return launch<bf16_t, 64, 2, 256>(p, st);
+  if (p.N <= 2048) return launch<bf16_t, 64, 4, 256>(p, st);
+  if (p.N <= 4096) return launch<bf16_t, 256, 2, 256>(p, st);
+  if (p.N <= 8192) return launch<bf16_t, 512, 2, 512>(p, st);
+  if (p.N <= 16384) return launch<bf16_t, 1024, 2, 1024>(p, st);
   return launch<bf16_t, 1024, 4, 1024>(p, st);
 }
 
