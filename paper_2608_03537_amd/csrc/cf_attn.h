@@ -59,4 +59,25 @@ __device__ __forceinline__ void static_for(F&& f) {
 __device__ __forceinline__ float lane_pair_sum(float v) { return v + __shfl_xor(v, 32); }
 __device__ __forceinline__ float lane_pair_max(float v) { return fmaxf(v, __shfl_xor(v, 32)); }
 
+// lane_pair_max without a trip through LDS: v_permlane32_swap exchanges the upper half of its first
+// operand with the lower half of its second, so of two copies every lane gets both halves' values.
+__device__ __forceinline__ float lane_pair_max_swap(float v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+#else
+  return v;
+#endif
+}
+
+// dma16 from base + lane_off + wave_off bytes (base and wave_off wave-uniform, offsets below 2^31): the
+// address takes no vector arithmetic beyond the lane's own offset.
+__device__ __forceinline__ void dma16_at(const char* base, uint32_t lane_off, uint32_t wave_off, char* lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, 0x7FFFFFFF, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)lds, 16, lane_off, wave_off, 0,
+                                           0);
+#endif
+}
+
 }  // namespace cf

@@ -11,6 +11,7 @@
 // owns 32 rows and keeps the running maximum m and sum l of each (fp32, raised
 // lazily).
 #include <algorithm>
+#include <cmath>
 
 #include "cf_attn.h"
 #include "cf_gemm_tile.h"
@@ -29,7 +30,7 @@ namespace {
 // beside one of the other.
 template <int D, int QG_>
 struct PrefixShape {
-  static constexpr int QG = QG_, KS = 4 / QG, NW = 4, NT = 256, TM = 32 * QG, BK = QG == 4 ? 64 : 4096 / D;
+  static constexpr int QG = QG_, KS = 4 / QG, NW = 4, NT = 256, TM = 32 * QG, BK = QG == 1 ? 4096 / D : 64;
   static constexpr int NH = BK / 32;              // 32-key parts of a block
   static constexpr int ROW = D * 2, CH = ROW / 16;   // bytes and 16-byte chunks of a key or value row
   static constexpr int NS = QG == 1 ? 1 : 2;      // stages
@@ -40,7 +41,7 @@ struct PrefixShape {
   static constexpr int DK = D / 16, BD = D / 32;  // MFMA steps over d, 32-wide blocks of d
   static constexpr int NSA = NH * DK, NSB = 2 * NH * BD;
   static constexpr int RPI = 64 / CH, NINS = BK / RPI / QG;   // rows of a wave-wide load; a wave's loads of K or V
-  static_assert(QG == 1 || QG == 2 || QG == 4, "forms");
+  static_assert(QG == 1 || QG == 4, "forms");
   static_assert(LDS <= 80 * 1024 && RING <= 65536, "two workgroups a CU, ds offset field");
 };
 
@@ -110,7 +111,7 @@ __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb
   const int first = KIND == PREFIX ? 0 : own_seen(p, len, m0 / G);                        // ... that every row sees
   const int seen = KIND == PREFIX ? 0 : own_seen(p, len, qi);                             // ... that this lane's row sees
   const int nball = nbp + (last + BK - 1) / BK;
-  // (blocks <= 2^26 and parts <= kMaxParts: the products fit 32 bits)
+  // (blocks <= 2^26 + 2^26 and parts <= kMaxParts: the products fit 32 bits)
   const int jb = (int)((uint32_t)nball * z / (uint32_t)parts), NB = (int)((uint32_t)nball * (z + 1) / (uint32_t)parts);
   const bf16_t* const Kp = p.Kp + hk * p.kp_h;
   const bf16_t* const Vp = p.Vp + hk * p.vp_h;
@@ -136,26 +137,50 @@ __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  // Load `ins` of this wave's share of the keys (or values) of block j.  Rows behind the
-  // last key that may be read are clamped here, masked in P and zeroed in V.
+  // Load `ins` of this wave's share of the keys (or values) of block j: rows in RPI .. + RPI - 1,
+  // in = wq + QG ins, a wave-uniform base and a lane's offset (row stride below 2^23 bytes).  The swizzle
+  // of a lane's chunk depends on `in` through in % 4 (d = 128) or in % 2 only, NP values over a
+  // wave's loads.  In a block that reaches behind the last key that may be read, rows are
+  // clamped; they are masked in P and zeroed in V.
+  constexpr int NP = A::CH == 16 ? 4 / QG : (QG == 1 ? 2 : 1);
   const int lrow = lane / A::CH, lch = lane % A::CH;
-  auto load = [&](int j, int stage, auto v_t, int ins) {
-    constexpr bool V = decltype(v_t)::value;
+  uint32_t kc[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) kc[i] = (lch ^ kswz((wq + QG * i) * A::RPI + lrow)) << 4;
+  const uint32_t vc = (lch ^ vswz(lrow)) << 4;
+  struct Block {   // where the keys and values of a block lie
+    const char *k, *v;
+    int ldk, ldv, left;   // bytes a row; rows that may be read from its first key on
+  };
+  auto block = [&](int j) {
     const bool own = j >= nbp;
-    const bf16_t* src = V ? (own ? Vs : Vp) : (own ? Ks : Kp);
-    const int64_t ld = V ? (own ? p.vs_l : p.vp_l) : (own ? p.ks_l : p.kp_l);
-    const int in = wq + QG * ins, row = in * A::RPI + lrow, nk = own ? len : p.P;
-    const int key = min((own ? j - nbp : j) * BK + row, nk - 1);
-    dma16(reinterpret_cast<const char*>(src + key * ld) + ((lch ^ (V ? vswz(row) : kswz(row))) << 4),
-          ring + stage * A::STAGE + (V ? A::KB : 0) + in * 1024);
+    const int k0 = (own ? j - nbp : j) * BK;
+    Block bl;
+    bl.ldk = (int)(own ? p.ks_l : p.kp_l) * 2;
+    bl.ldv = (int)(own ? p.vs_l : p.vp_l) * 2;
+    bl.k = reinterpret_cast<const char*>(own ? Ks : Kp) + (int64_t)k0 * bl.ldk;
+    bl.v = reinterpret_cast<const char*>(own ? Vs : Vp) + (int64_t)k0 * bl.ldv;
+    bl.left = (own ? len : p.P) - k0;
+    return bl;
   };
-  auto load_k = [&](int j, int stage) {
-#pragma unroll
-    for (int i = 0; i < A::NINS; ++i) load(j, stage, std::false_type{}, i);
+  auto load = [&](const Block& bl, int stage, auto v_t, auto full_t, int ins) {
+    constexpr bool V = decltype(v_t)::value, FULL = decltype(full_t)::value;
+    const int in = wq + QG * ins, ld = V ? bl.ldv : bl.ldk;
+    const char* src = V ? bl.v : bl.k;
+    const uint32_t c = V ? vc : kc[ins % NP];
+    char* dst = ring + stage * A::STAGE + (V ? A::KB : 0) + in * 1024;
+    if constexpr (FULL) dma16_at(src, __mul24(lrow, ld) + c, in * A::RPI * ld, dst);
+    else dma16_at(src, __mul24(min(in * A::RPI + lrow, bl.left - 1), ld) + c, 0, dst);
   };
-  auto load_v = [&](int j, int stage) {
+  // All of this wave's loads of the keys or of the values of a block.
+  auto load_all = [&](const Block& bl, int stage, auto v_t) {
+    if (bl.left >= BK) {
 #pragma unroll
-    for (int i = 0; i < A::NINS; ++i) load(j, stage, std::true_type{}, i);
+      for (int i = 0; i < A::NINS; ++i) load(bl, stage, v_t, std::true_type{}, i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < A::NINS; ++i) load(bl, stage, v_t, std::false_type{}, i);
+    }
   };
 
   f32x16_t O[A::BD];
@@ -176,12 +201,12 @@ __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb
       wait_vmcnt<0>();
       __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));   // this wave's LDS reads
       lds_barrier();           // the block is in, and every wave is done with the other stage
-      if (KS > 1 && j >= NB) return;   // this group has no block in the last step
     }
     // S^T = K Q^T: one LDS read per MFMA, four ahead.  With two stages the next block's loads
     // go between the MFMAs: in a row they would hold the wave up.
     f32x16_t S[A::NH];
-    {
+    const Block nb = block(next ? j + KS : j);
+    auto scores = [&](auto load_t, auto full_t) {
       constexpr int KLA = 4;
       constexpr int SPC = A::NSA / (2 * A::NINS) > 0 ? A::NSA / (2 * A::NINS) : 1;   // MFMAs per load
       constexpr int LPM = 2 * A::NINS > A::NSA ? 2 * A::NINS / A::NSA : 1;          // loads per MFMA
@@ -199,19 +224,21 @@ __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb
                                                        __builtin_bit_cast(bf16x8_t, qf[ks]), ks == 0 ? zero : S[h], 0, 0,
                                                        0);
         if constexpr (i + KLA < A::NSA) kf[(i + KLA) % KLA] = kread(std::integral_constant<int, i + KLA>{});
-        if constexpr (A::NS == 2)
-          if (next)
-            static_for<0, LPM>([&](auto l_t) {
-              constexpr int q = i / SPC * LPM + decltype(l_t)::value;
-              if constexpr (i % SPC == SPC - 1 && q < 2 * A::NINS)
-                load(j + KS, 1 - SG, std::integral_constant<bool, (q >= A::NINS)>{}, q % A::NINS);
-            });
+        if constexpr (decltype(load_t)::value)
+          static_for<0, LPM>([&](auto l_t) {
+            constexpr int q = i / SPC * LPM + decltype(l_t)::value;
+            if constexpr (i % SPC == SPC - 1 && q < 2 * A::NINS)
+              load(nb, 1 - SG, std::integral_constant<bool, (q >= A::NINS)>{}, full_t, q % A::NINS);
+          });
         __builtin_amdgcn_sched_barrier(0);
       });
-    }
+    };
+    if (A::NS == 1 || !next) scores(std::false_type{}, std::false_type{});
+    else if (nb.left >= BK) scores(std::integral_constant<bool, A::NS == 2>{}, std::true_type{});
+    else scores(std::integral_constant<bool, A::NS == 2>{}, std::false_type{});
     if constexpr (QG == 1) {
       fence();   // the last read of the keys has returned
-      if (next) load_k(j + KS, 0);
+      if (next) load_all(nb, 0, std::false_type{});
     }
     if (k0 + BK > (own ? first : p.P)) {   // some row of the workgroup does not see the whole block
       const int lim = own ? seen : p.P;
@@ -223,7 +250,7 @@ __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb
     float t = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 16 * A::NH; ++e) t = fmaxf(t, S[e >> 4][e & 15]);
-    const float mnew = fmaxf(m_used, lane_pair_max(t) * sl2);
+    const float mnew = fmaxf(m_used, lane_pair_max_swap(t) * sl2);
     const bool need = mnew > m_used + kLazy;
     const float m_eff = need ? mnew : m_used;
     const float corr = need ? __builtin_amdgcn_exp2f(m_used - m_eff) : 1.0f;
@@ -262,14 +289,14 @@ __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb
         const u32x2_t hi = ds_read_tr_b64<off + 8 * A::ROW>(vbase[d]);
         return u32x4_t{lo[0], lo[1], hi[0], hi[1]};
       };
-      u32x4_t vf[3];
-      vf[0] = vfrag(std::integral_constant<int, 0>{});
-      vf[1] = vfrag(std::integral_constant<int, 1>{});
+      constexpr int VLA = 2;
+      u32x4_t vf[VLA + 1];
+      static_for<0, VLA>([&](auto i_t) { vf[decltype(i_t)::value] = vfrag(i_t); });
       static_for<0, A::NSB>([&](auto i_t) {
-        constexpr int i = decltype(i_t)::value;
+        constexpr int i = decltype(i_t)::value, rest = A::NSB - 1 - i;
         constexpr int d = i % A::BD, s = (i / A::BD) & 1, h = i / (2 * A::BD);
-        lgkm_wait<(i + 1 < A::NSB ? 2 : 0)>(vf[i % 3]);
-        u32x4_t v = vf[i % 3];
+        lgkm_wait<2 * (rest < VLA - 1 ? rest : VLA - 1)>(vf[i % (VLA + 1)]);
+        u32x4_t v = vf[i % (VLA + 1)];
         if constexpr (decltype(mask_t)::value) {
           const int left = nk - (k0 + 32 * h + 16 * s + 4 * lg);   // of the 4 keys of v[0..1]; v[2..3]: 8 on
 #pragma unroll
@@ -279,7 +306,7 @@ __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb
           }
         }
         Mma<bf16_t>::run(O[d], v, P[h][s]);
-        if constexpr (i + 2 < A::NSB) vf[(i + 2) % 3] = vfrag(std::integral_constant<int, i + 2>{});
+        if constexpr (i + VLA < A::NSB) vf[(i + VLA) % (VLA + 1)] = vfrag(std::integral_constant<int, i + VLA>{});
         __builtin_amdgcn_sched_barrier(0);
       });
     };
@@ -287,7 +314,7 @@ __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb
     else pv(std::false_type{});
     if constexpr (QG == 1) {
       fence();   // the last read of the values has returned
-      if (next) load_v(j + KS, 0);
+      if (next) load_all(nb, 0, std::true_type{});
     }
     // the row sum from the same bf16 P as the numerator
     typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -303,15 +330,16 @@ __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb
   using S0_ = std::integral_constant<int, 0>;
   using S1_ = std::integral_constant<int, 1>;
   if (jb + grp < NB) {
-    load_k(jb + grp, 0);
-    load_v(jb + grp, 0);
+    const Block bl = block(jb + grp);
+    load_all(bl, 0, std::false_type{});
+    load_all(bl, 0, std::true_type{});
   }
   if constexpr (QG == 1) {
     for (int j = jb + grp; j < NB; j += KS) step(j, S0_{});
   } else {
-    for (int j = jb; j < NB; j += 2 * KS) {   // every group runs the same number of steps (the barriers are the workgroup's)
-      step(j + grp, S0_{});
-      if (j + KS < NB) step(j + KS + grp, S1_{});
+    for (int j = jb; j < NB; j += 2) {
+      step(j, S0_{});
+      if (j + 1 < NB) step(j + 1, S1_{});
     }
   }
   __syncthreads();   // the rings are free for the merge
@@ -474,36 +502,81 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixParams p, int s
 }
 
 // ---------------------------------------------------------------------------
-// How a call is cut.
+// How a call is cut: whole rows in one launch, in np parts of their keys and a
+// second launch that joins them, or split into prefix parts and own parts.
 // ---------------------------------------------------------------------------
 struct PrefixPlan {
   int pq, oq;   // 32-row waves of a workgroup: prefix parts, own parts or whole rows
   int np, ns;   // split: parts of the prefix and of the own keys.  ns = 0: whole rows in np parts
   int slots() const { return ns > 0 ? np + ns : np > 1 ? np : 0; }
 };
-constexpr int kCUs = 256, kMaxParts = 32;
+constexpr int kCUs = 256, kMaxParts = 32, kMaxOwnParts = 8;
 
 int query_waves(int64_t rows) { return rows <= 32 ? 1 : 4; }
-int64_t row_blocks(int64_t rows, int qg) { return (rows + 32 * qg - 1) / (32 * qg); }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t row_blocks(int64_t rows, int qg) { return ceil_div(rows, 32 * qg); }
+
+// The estimate (us).  A step is one key block of every group of a workgroup: alone on its CU,
+// and where two workgroups share the CU; a workgroup's start and merge; the joining launch, and
+// a partial result's write and read.  Fitted to 80 calls of 1 to 64 sequences, 1 to 500 queries and
+// 64 to 16000 prefix keys, each measured in 10 to 40 cuts: the cut that the estimate takes is
+// 2 % slower than the best one on average, 14 % at worst.  Some of them (us: whole rows; the best split):
+//     4 x 8 heads, 1 query, 128 + 64 keys, d 64                5.6     8.5
+//     64 x 8 heads, 1 query, 512 + 128, d 64                  10.7    12.5
+//     16 x 16 heads, 5 queries, 4095 + 333, d 64              22.6    15.5 (4 + 1 parts)
+//     1 x 32 heads of 8, 1 query, 8192 + 512, d 128             67    13.4 (16 + 2)
+//     64 x 32 heads of 8, 1 query, 8192 + 512, d 128           118    39.8 (8 + 2)
+constexpr double kStepFew = 0.95, kStepFew2 = 1.9, kStepMany = 1.6, kStepMany2 = 2.35;   // QG 1, QG 4; 2: two a CU
+constexpr double kStepMany64 = 0.62;              // QG 4 steps at d = 64 by those at d = 128
+constexpr double kStart = 6.6, kJoin = 3.3, kPartial = 1.9e-6, kStream = 4.8e6;   // kStream: bytes a us
+
+struct Task {   // one kind of workgroup of a launch
+  double steps, wgs;
+  int qg;
+  double us(bool shared) const {
+    return steps * (qg == 1 ? (shared ? kStepFew2 : kStepFew) : (shared ? kStepMany2 : kStepMany)) + kStart;
+  }
+};
 
 PrefixPlan make_plan(const PrefixParams& p) {
-  const int64_t R = (int64_t)(p.H / p.Hk) * p.Lq, Rall = p.B * R;
-  PrefixPlan pl{query_waves(Rall), query_waves(R), 1, 0};
-  const char* force = getenv("CF_PREFIX");
-  if (force && force[0] == '1') {
-    sscanf(force, "1,%d", &pl.np);
-    return pl;
+  const int64_t R = (int64_t)(p.H / p.Hk) * p.Lq, Rall = p.B * R, rows = p.Hk * Rall;
+  PrefixPlan best{query_waves(Rall), query_waves(R), 1, 0};
+  auto keys = [&](int qg) { return qg == 1 ? 4096 / p.d : 64; };              // of a block
+  auto blocks = [&](int64_t n, int qg) { return ceil_div(n, keys(qg)); };
+  auto task = [&](int64_t nb, int parts, int64_t wgs, int qg) {
+    const double scale = qg == 4 && p.d == 64 ? kStepMany64 : 1.0;
+    return Task{(double)ceil_div(ceil_div(nb, parts), 4 / qg) * scale, (double)wgs * parts, qg};
+  };
+  const int64_t wo = row_blocks(R, best.oq) * p.B * p.Hk, wp = row_blocks(Rall, best.pq) * p.Hk;
+  const int64_t bw = blocks(p.P, best.oq) + blocks(p.S, best.oq);
+  const double stream = 4.0 * p.Hk * p.d * (p.P + 0.8 * p.B * p.S) / kStream;
+  const double part = kPartial * (double)rows * p.d;
+  const int64_t most = ((int64_t)1 << 30) / std::max<int64_t>(1, rows * (p.d + 2) * 4);   // parts in 1 GiB
+  double least = 0;
+  auto take = [&](double us, int np, int ns) {
+    if (least == 0 || us < least) {
+      least = us;
+      best.np = np;
+      best.ns = ns;
+    }
+  };
+  for (int n = 1; n <= kMaxParts && (n == 1 || ((int64_t)n * 64 <= (int64_t)p.P + p.S && n <= most)); n *= 2) {
+    const Task t = task(bw, n, wo, best.oq);
+    const double us = t.wgs <= kCUs ? t.us(false) : std::ceil(t.wgs / (2 * kCUs)) * t.us(true);
+    take(std::max(us, stream) + (n > 1 ? kJoin + n * part : 0.0), n, 0);
   }
-  const int64_t own = row_blocks(R, pl.oq) * p.B * p.Hk;
-  if ((R >= 64 && own >= kCUs) || p.P == 0 || p.S == 0) return pl;
-  {
-    const int64_t w = row_blocks(Rall, pl.pq) * p.Hk;
-    const int64_t per = 64 * 4;
-    pl.np = (int)std::max<int64_t>(1, std::min<int64_t>({(kCUs + w - 1) / w, p.P / per, 32}));
-  }
-  pl.ns = (int)std::max<int64_t>(1, std::min<int64_t>({kCUs / own, p.S / 256, 16}));
-  if (force) sscanf(force, "2,%d,%d,%d", &pl.np, &pl.ns, &pl.pq);
-  return pl;
+  // whole rows of full workgroups on every CU: nothing to gain from parts
+  if (p.P == 0 || p.S == 0 || (R >= 64 && wo >= kCUs)) return best;
+  const int64_t bp = blocks(p.P, best.pq), bo = blocks(p.S, best.oq);
+  for (int n = 1; n <= kMaxParts && (n == 1 || (int64_t)n * 64 <= p.P); n *= 2)
+    for (int m = 1; m <= kMaxOwnParts && (m == 1 || (int64_t)m * 64 <= p.S) && n + m <= most; m *= 2) {
+      const Task a = task(bp, n, wp, best.pq), b = task(bo, m, wo, best.oq);
+      const bool shared = a.wgs + b.wgs > kCUs;
+      const double ua = a.us(shared), ub = b.us(shared);
+      const double us = std::max({ua, ub, 1.36 * (a.wgs * ua + b.wgs * ub) / (2 * kCUs)});
+      take(std::max(us, stream) + kJoin + (n + m) * part, n, m);
+    }
+  return best;
 }
 
 template <int D, int QG>
@@ -534,7 +607,6 @@ hipError_t launch_all(const PrefixParams& p, const PrefixPlan& pl, hipStream_t s
   hipError_t e;
   if (pl.ns == 0) e = pl.oq == 1 ? launch_whole<D, 1>(p, pl.np, st) : launch_whole<D, 4>(p, pl.np, st);
   else if (pl.pq == 1) e = launch_split<D, 1, 1>(p, pl, st);
-  else if (pl.pq == 2) e = launch_split<D, 2, 1>(p, pl, st);
   else e = pl.oq == 1 ? launch_split<D, 4, 1>(p, pl, st) : launch_split<D, 4, 4>(p, pl, st);
   if (e != hipSuccess || pl.slots() == 0) return e;
   return pl.slots() <= 4 ? launch_merge<D, 1>(p, pl.slots(), st)
