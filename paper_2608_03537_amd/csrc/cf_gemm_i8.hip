@@ -58,12 +58,13 @@ __device__ __forceinline__ void with_act(int act, F&& f) {
 // Output pass of a tile whose sums lie in LDS: KW planes of TM rows of TN int32 (pitch TN * 4 +
 // 16 bytes), added here.  A thread takes 8 columns of a row at a time, always the same columns.
 // Its scales and biases are loaded ahead (before the main loop, where registers allow: loaded
-// here, they add a trip to memory to every tile).
-template <int TM, int TN, int NT>
+// here, they add a trip to memory to every tile).  AHEAD = false: the rows' scales are loaded row by
+// row, and the rows not unrolled, for the 256 x 256 tiles, which have no registers to spare here.
+template <int TM, int TN, int NT, bool AHEAD>
 struct TileScales {
   static constexpr int CPR = TN / 8, STEP = NT / CPR, RPT = (TM + STEP - 1) / STEP;   // a thread's rows: STEP apart
   static_assert(NT % CPR == 0, "a thread keeps its columns");
-  float sa[RPT], sb[8], bias[8];
+  float sa[AHEAD ? RPT : 1], sb[8], bias[8];
   __device__ __forceinline__ void load(const GemmI8Params& p, int m0, int n0) {
     const int n = n0 + threadIdx.x % CPR * 8, r0 = threadIdx.x / CPR;
     auto eight = [&](const float* v, float none, float (&out)[8]) {
@@ -81,25 +82,24 @@ struct TileScales {
     };
     eight(p.sb, 1.0f, sb);
     eight(p.bias, 0.0f, bias);
+    if constexpr (AHEAD) {
 #pragma unroll
-    for (int i = 0; i < RPT; ++i) sa[i] = p.sa ? p.sa[min(m0 + r0 + i * STEP, p.M - 1)] : 1.0f;
+      for (int i = 0; i < RPT; ++i) sa[i] = p.sa ? p.sa[min(m0 + r0 + i * STEP, p.M - 1)] : 1.0f;
+    }
   }
 };
 
-template <int TM, int TN, int KW, int NT>
-__device__ __forceinline__ void finish_tile(const GemmI8Params& p, const TileScales<TM, TN, NT>& sc, const char* smem,
-                                            int m0, int n0) {
-  using Sc = TileScales<TM, TN, NT>;
+template <int TM, int TN, int KW, int NT, bool AHEAD>
+__device__ __forceinline__ void finish_tile(const GemmI8Params& p, const TileScales<TM, TN, NT, AHEAD>& sc,
+                                            const char* smem, int m0, int n0) {
+  using Sc = TileScales<TM, TN, NT, AHEAD>;
   constexpr int PITCH = TN * 4 + 16;
   const int tid = threadIdx.x, c8 = tid % Sc::CPR * 8, left = p.N - n0 - c8;
   if (left <= 0) return;
   const int rows = min(TM, p.M - m0);
   with_act(p.act, [&](auto act_t) {
     constexpr int ACT = decltype(act_t)::value;
-#pragma unroll
-    for (int i = 0; i < Sc::RPT; ++i) {
-      const int r = tid / Sc::CPR + i * Sc::STEP;
-      if (r >= rows) break;
+    auto row = [&](int r, float sa) {
       const char* src = smem + r * PITCH + c8 * 4;
       i32x4_t a = *reinterpret_cast<const i32x4_t*>(src), b = *reinterpret_cast<const i32x4_t*>(src + 16);
 #pragma unroll
@@ -110,7 +110,7 @@ __device__ __forceinline__ void finish_tile(const GemmI8Params& p, const TileSca
       float y[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        float x = (float)(e < 4 ? a[e] : b[e - 4]) * sc.sa[i] * sc.sb[e];
+        float x = (float)(e < 4 ? a[e] : b[e - 4]) * sa * sc.sb[e];
         if (p.bias) x += sc.bias[e];
         y[e] = act_i8<ACT>(x);
       }
@@ -133,6 +133,15 @@ __device__ __forceinline__ void finish_tile(const GemmI8Params& p, const TileSca
           else reinterpret_cast<bf16_t*>(p.C)[at + e] = (bf16_t)pack_bf16x2(y[e], 0.0f);
         }
       }
+    };
+    const int r0 = tid / Sc::CPR;
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int i = 0; i < Sc::RPT; ++i)
+        if (r0 + i * Sc::STEP < rows) row(r0 + i * Sc::STEP, sc.sa[i]);
+    } else {
+#pragma unroll 2
+      for (int r = r0; r < rows; r += Sc::STEP) row(r, p.sa ? p.sa[m0 + r] : 1.0f);
     }
   });
 }
@@ -170,7 +179,7 @@ __global__ __launch_bounds__(S::NT) void gemm_i8_tile_kernel(GemmI8Params p) {
   int rb, c;
   big_tile_order((p.M + S::TM - 1) / S::TM, (p.N + S::TN - 1) / S::TN, rb, c);
   const int m0 = rb * S::TM, n0 = c * S::TN;
-  TileScales<S::TM, S::TN, S::NT> sc;
+  TileScales<S::TM, S::TN, S::NT, true> sc;
   sc.load(p, m0, n0);
   char* const ring = smem + grp * S::RING;
   const int KT = p.K / 128, steps = grp < KT ? (KT - grp - 1) / S::KW + 1 : 0;   // whole steps; those of this group
@@ -320,7 +329,7 @@ void gemm_i8_big_kernel(GemmI8Params p) {
           *reinterpret_cast<i32x4_t*>(smem + (wm * 64 + b * 32 + lr) * kI8BigPitch + (nh * 128 + wn * 32 + 8 * g + 4 * lg) * 4) =
               i32x4_t{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
         }
-    TileScales<128, kBigT, 512> sc;
+    TileScales<128, kBigT, 512, false> sc;
     sc.load(p, m0 + h * 128, n0);
     __syncthreads();
     finish_tile<128, kBigT, 1, 512>(p, sc, smem, m0 + h * 128, n0);
