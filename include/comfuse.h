@@ -394,7 +394,7 @@ cf_status cf_gemm_i8(const cf_gemm_i8_args* a, void* hip_stream);
  *
  * Q, O: batch x H x Lq rows of d; Kp, Vp: Hk x P rows; Ks, Vs: batch x Hk x S
  * rows, all bf16, each matrix with its own strides (elements, multiples of 8; rows
- * have unit stride).  H is a multiple of Hk: query head h reads key head
+ * have unit stride; an input's batch or head stride may be 0).  H is a multiple of Hk: query head h reads key head
  * h / (H / Hk).  d in {64, 128}.  P >= 0, S >= 0; Kp and Vp (Ks and Vs) may be
  * NULL where P (S) is 0.  lens: int32 [batch] in device memory, or NULL for S
  * everywhere; values outside [0, S] are clamped.  causal = 1: query i sees the

@@ -611,19 +611,21 @@ def _elsewhere(call, X, stream, *args, **kw):
 
 
 def _here(X, stream):
-    """Whether the call can run on the current device and stream."""
-    return stream is None and X.is_cuda and X.get_device() == _torch()._C._cuda_getDevice()
+    """(library, torch, device index, raw stream) where the call can run on the current device and stream, else None."""
+    torch = _torch()
+    if stream is not None or not X.is_cuda:
+        return None
+    device = X.get_device()
+    if device != torch._C._cuda_getDevice():
+        return None
+    return _lib or lib(), torch, device, torch._C._cuda_getCurrentRawStream(device)
 
 
-def _raw_stream(device):
-    return _torch()._C._cuda_getCurrentRawStream(device)
-
-
-def _rows(M, N, dtype, device, size):
+def _rows(torch, M, N, dtype, device, size):
     """An [M, N] tensor whose rows start every multiple of 16 bytes (`size`: bytes of an element)."""
     per = 16 // size
     ld = -(-N // per) * per
-    t = _torch().empty(M, ld, dtype=dtype, device=device)
+    t = torch.empty(M, ld, dtype=dtype, device=device)
     return t if ld == N else t[:, :N]
 
 
@@ -654,6 +656,12 @@ def _like(t, shape, dtype, device, name):
     return t
 
 
+def _choice(table, key, name):
+    if key not in table:
+        raise ValueError(f"{name}: expected one of {', '.join(table)}, got {key!r}")
+    return table[key]
+
+
 _CODES = {"int8": CF_I8, "e4m3": CF_FP8_E4M3}
 _RMSNORM_QUANT_SIZE, _GEMM_I8_SIZE, _PREFIX_SIZE = (C.sizeof(t) for t in (RmsnormQuantArgs, GemmI8Args, AttentionPrefixArgs))
 
@@ -668,30 +676,34 @@ def rmsnorm_quant(X, R=None, gamma=None, *, eps=1e-5, norm=True, code="int8", re
     names the tensor it goes to, which may be R (in place).  `out` and `scale`
     take Q and s.  Q is what gemm_i8 takes as its tokens, s as sa.
     """
-    if not _here(X, stream):
+    here = _here(X, stream)
+    if here is None:
         return _elsewhere(rmsnorm_quant, X, stream, R, gamma, eps=eps, norm=norm, code=code, residual=residual, out=out,
                           scale=scale)
-    torch = _torch()
-    shape, dtype, device = X.shape, X.dtype, X.get_device()
+    L, torch, device, raw = here
+    shape, dtype, dev = X.shape, X.dtype, X.device
     M, N = shape
     dt = _dt(X)
     size = 4 if dt == CF_F32 else 2
-    qdt = torch.int8 if code == "int8" else torch.uint8
+    cdt = _choice(_CODES, code, "code")
+    qdt = torch.int8 if cdt == CF_I8 else torch.uint8
     if R is not None:
         _like(R, shape, dtype, device, "R")
     H = residual
     if H is not None:
         _like(H, shape, dtype, device, "residual")
     elif R is not None:
-        H = _rows(M, N, dtype, X.device, size)
-    Q = _rows(M, N, qdt, X.device, 1) if out is None else _like(out, shape, qdt, device, "out")
-    s = torch.empty(M, dtype=torch.float32, device=X.device) if scale is None else scale
+        H = _rows(torch, M, N, dtype, dev, size)
+    Q = _rows(torch, M, N, qdt, dev, 1) if out is None else _like(out, shape, qdt, device, "out")
+    s = torch.empty(M, dtype=torch.float32, device=dev) if scale is None else scale
     a = RmsnormQuantArgs(_RMSNORM_QUANT_SIZE, M, N, dt, X.data_ptr(), _row_ld(X, M, N, size),
                          None if R is None else R.data_ptr(), 0 if R is None else _row_ld(R, M, N, size),
                          None if H is None else H.data_ptr(), 0 if H is None else _row_ld(H, M, N, size),
-                         _vector(gamma, N, device, "gamma"), 1 if norm else 0, eps, _CODES[code], Q.data_ptr(),
+                         _vector(gamma, N, device, "gamma"), 1 if norm else 0, eps, cdt, Q.data_ptr(),
                          _row_ld(Q, M, N, 1), _vector(s, M, device, "scale"))
-    _check(cf_rmsnorm_quant(a, _raw_stream(device)))
+    status = L.cf_rmsnorm_quant(C.byref(a), raw)
+    if status:
+        _check(status)
     return Q, s, H
 
 
@@ -704,10 +716,10 @@ def gemm_i8(A, B, sa=None, sb=None, *, bias=None, act="none", out_dtype=None, ou
     sa fp32 [M] (a scale per token), sb fp32 [N] (per channel), bias fp32 [N];
     act "none", "gelu", "gelu_tanh" or "relu"; C bf16 (or fp32) [M, N].
     """
-    if not _here(A, stream):
+    here = _here(A, stream)
+    if here is None:
         return _elsewhere(gemm_i8, A, stream, B, sa, sb, bias=bias, act=act, out_dtype=out_dtype, out=out)
-    torch = _torch()
-    device = A.get_device()
+    L, torch, device, raw = here
     M, K = A.shape
     N = B.size(0)
     if A.dtype is not torch.int8 or B.dtype is not torch.int8:
@@ -717,22 +729,22 @@ def gemm_i8(A, B, sa=None, sb=None, *, bias=None, act="none", out_dtype=None, ou
         dt = CF_F32 if out_dtype is torch.float32 else CF_BF16
         if dt == CF_BF16 and out_dtype not in (None, torch.bfloat16):
             raise TypeError(f"unsupported dtype {out_dtype}")
-        Cm = _rows(M, N, torch.float32 if dt == CF_F32 else torch.bfloat16, A.device, 4 if dt == CF_F32 else 2)
+        Cm = _rows(torch, M, N, torch.float32 if dt == CF_F32 else torch.bfloat16, A.device, 4 if dt == CF_F32 else 2)
     else:
         dt, Cm = _dt(out), _like(out, (M, N), out_dtype or out.dtype, device, "out")
     a = GemmI8Args(_GEMM_I8_SIZE, M, N, K, A.data_ptr(), _row_ld(A, M, K, 1), B.data_ptr(), _row_ld(B, N, K, 1),
                    _vector(sa, M, device, "sa"), _vector(sb, N, device, "sb"), _vector(bias, N, device, "bias"),
-                   _ACTS[act], dt, Cm.data_ptr(), _row_ld(Cm, M, N, 4 if dt == CF_F32 else 2))
-    _check(cf_gemm_i8(a, _raw_stream(device)))
+                   _choice(_ACTS, act, "act"), dt, Cm.data_ptr(), _row_ld(Cm, M, N, 4 if dt == CF_F32 else 2))
+    status = L.cf_gemm_i8(C.byref(a), raw)
+    if status:
+        _check(status)
     return Cm
 
 
-def _prefix_workspace(need, device, index):
+def _prefix_workspace(torch, need, device, key):
     """workspace(need, device, kind="prefix") at less cost: cached per device and stream while nothing is captured."""
-    torch = _torch()
     if torch._C._cuda_isCurrentStreamCapturing():
         return workspace(need, device, None, kind="prefix")
-    key = (index, _raw_stream(index), "prefix")
     ws = _ws_cache.get(key)
     if ws is None or ws.numel() < need:
         ws = _ws_cache[key] = torch.empty(need, dtype=torch.uint8, device=device)
@@ -751,10 +763,11 @@ def attention_prefix(Q, Kp, Vp, Ks=None, Vs=None, lens=None, *, causal=False, sc
     keys j < lens[b] - (Lq - 1 - i).  A query that sees no key gets 0.  ws: a
     workspace of the caller's own (cf_attention_prefix_workspace bytes).
     """
-    if not _here(Q, stream):
+    here = _here(Q, stream)
+    if here is None:
         return _elsewhere(attention_prefix, Q, stream, Kp, Vp, Ks, Vs, lens, causal=causal, scale=scale, out=out, ws=ws)
-    torch = _torch()
-    bf16, device = torch.bfloat16, Q.get_device()
+    L, torch, device, raw = here
+    bf16 = torch.bfloat16
     shape = Q.shape
     B, H, Lq, d = shape
     Hk, P = Kp.size(0), Kp.size(1)
@@ -784,9 +797,10 @@ def attention_prefix(Q, Kp, Vp, Ks=None, Vs=None, lens=None, *, causal=False, sc
                             None if lens is None else lens.data_ptr(), 1 if causal else 0,
                             d ** -0.5 if scale is None else scale, O.data_ptr(), o[0], o[1], o[2])
     if ws is None:
-        need = cf_attention_prefix_workspace(a)
+        need = L.cf_attention_prefix_workspace(C.byref(a))
         if need:
-            ws = _prefix_workspace(need, Q.device, device)
-    _check(cf_attention_prefix(a, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
-                               _raw_stream(device)))
+            ws = _prefix_workspace(torch, need, Q.device, (device, raw, "prefix"))
+    status = L.cf_attention_prefix(C.byref(a), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), raw)
+    if status:
+        _check(status)
     return O

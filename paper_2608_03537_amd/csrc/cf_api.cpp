@@ -1170,9 +1170,10 @@ cf_status cf_gemm_i8(const cf_gemm_i8_args* a, void* hip_stream) {
 }
 
 // One operand of cf_attention_prefix: rows of d elements in up to two outer
-// dimensions (batch, head); strides that move nothing (size 1) are free.
+// dimensions (batch, head); strides that move nothing (size 1) are free.  An
+// input may be shared along an outer dimension (stride 0), the output may not.
 static cf_status check_rows(const char* name, const void* p, bool used, int64_t nb, int64_t sb, int64_t nh, int64_t sh,
-                            int64_t rows, int64_t sl, int64_t d) {
+                            int64_t rows, int64_t sl, int64_t d, bool output = false) {
   if (!used) return CF_OK;
   if (!p) return fail(CF_ERR_NULL, "%s is NULL", name);
   if (!aligned16(p)) return fail(CF_ERR_ALIGN, "%s is not 16-byte aligned", name);
@@ -1181,6 +1182,8 @@ static cf_status check_rows(const char* name, const void* p, bool used, int64_t 
     return fail(CF_ERR_LD, "%s: row stride of %lld bytes or more", name, (long long)kMaxRowPitch);
   if ((nb > 1 && (sb < 0 || sb % 8 != 0)) || (nh > 1 && (sh < 0 || sh % 8 != 0)) || (rows > 1 && sl % 8 != 0))
     return fail(CF_ERR_ALIGN, "%s: strides must be non-negative multiples of 8 elements", name);
+  if (output && ((nb > 1 && sb < d) || (nh > 1 && sh < d)))
+    return fail(CF_ERR_LD, "%s: outputs overlap (a stride below d = %lld)", name, (long long)d);
   return CF_OK;
 }
 
@@ -1229,7 +1232,7 @@ cf_status cf_attention_prefix(const cf_attention_prefix_args* a, void* workspace
     if (s != CF_OK) return s;
     const bool any = p.B > 0 && p.Lq > 0;
     if ((s = check_rows("Q", a->Q, any, p.B, a->q_b, p.H, a->q_h, p.Lq, a->q_l, p.d)) != CF_OK ||
-        (s = check_rows("O", a->O, any, p.B, a->o_b, p.H, a->o_h, p.Lq, a->o_l, p.d)) != CF_OK ||
+        (s = check_rows("O", a->O, any, p.B, a->o_b, p.H, a->o_h, p.Lq, a->o_l, p.d, true)) != CF_OK ||
         (s = check_rows("Kp", a->Kp, any && p.P > 0, 1, 0, p.Hk, a->kp_h, p.P, a->kp_l, p.d)) != CF_OK ||
         (s = check_rows("Vp", a->Vp, any && p.P > 0, 1, 0, p.Hk, a->vp_h, p.P, a->vp_l, p.d)) != CF_OK ||
         (s = check_rows("Ks", a->Ks, any && p.S > 0, p.B, a->ks_b, p.Hk, a->ks_h, p.S, a->ks_l, p.d)) != CF_OK ||

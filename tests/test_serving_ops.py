@@ -461,6 +461,80 @@ def test_repeatable_and_on_another_stream():
         assert torch.equal(o, first) and torch.equal(p, prod) and all(torch.equal(u, v) for u, v in zip(c, codes))
 
 
+@gpu
+def test_empty_batches():
+    x = torch.zeros((0, 64), dtype=BF16, device="cuda")
+    Q, s, H = cf.rmsnorm_quant(x, x)
+    assert Q.shape == (0, 64) and s.shape == (0,) and H.shape == (0, 64)
+    assert cf.gemm_i8(Q, torch.zeros((48, 64), dtype=torch.int8, device="cuda"), s).shape == (0, 48)
+
+
+@gpu
+def test_split_calls_captured_and_on_two_streams():
+    """Calls in parts use a workspace: each capture has its own, which eager calls of other sizes do not
+    disturb, and so has each stream."""
+    g = gen(5)
+    small = prefix_inputs(g, 4, 8, 2, 1, 3000, 200, 128)
+    large = prefix_inputs(g, 16, 16, 4, 2, 6000, 300, 64)
+    assert all(cf.cf_attention_prefix_workspace(prefix_args(batch=a[0].shape[0], H=a[0].shape[1], Hk=a[1].shape[0],
+                                                            Lq=a[0].shape[2], P=a[1].shape[1], S=a[3].shape[2],
+                                                            d=a[0].shape[3])) > 0 for a in (small, large))
+    want = [cf.attention_prefix(*a).clone() for a in (small, large)]
+    graphs, got = [], []
+    for a in (small, large):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got.append(cf.attention_prefix(*a))
+        graphs.append(graph)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for turn in range(4):
+        for t in got:
+            t.zero_()
+        torch.cuda.synchronize()
+        for graph, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+        eager = [cf.attention_prefix(*a, stream=s) for _ in range(3) for a, s in zip((large, small), streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want)), turn
+        assert all(torch.equal(x, want[1 - i % 2]) for i, x in enumerate(eager)), turn
+
+
+@gpu
+def test_offsets_past_32_bits():
+    """Rows, keys and tokens that lie more than 4 GiB behind their tensor's start."""
+    g = gen(11)
+    n, wide = 300000, 8192                           # 16 KB a row in bf16, 4.9 GB
+    big = torch.zeros((n, wide), dtype=BF16, device="cuda")
+    big[-70:] = torch.randn((70, wide), generator=g, device="cuda").to(BF16)
+    Q, s, _ = cf.rmsnorm_quant(big)
+    check_norm(Q[-70:], s[-70:], None, norm_ref(big[-70:], None, None, 1e-5, True, "int8"), "int8", BF16)
+    assert not Q[:-70].any() and not s[:-70].any()
+    W = i8(g, 24, wide)
+    C = cf.gemm_i8(Q, W, s)
+    check_gemm(C[-70:], Q[-70:], W, s[-70:], None, None, "none")
+    assert not C[:-70].any()
+    del Q, C
+    # keys and values: two heads of 128 in the rows; all but the last 70 keys are zero
+    d = 128
+    K, V = (big[:, i * d:(i + 2) * d].unflatten(-1, (2, d)).transpose(0, 1) for i in (0, 8))
+    q = (torch.randn((2, 4, 1, d), generator=g, device="cuda") * 4).to(BF16)
+    none = torch.zeros((2, 0, d), dtype=BF16, device="cuda")
+    own = [t[None].expand(2, -1, -1, -1) for t in (K, V)]
+    for args in ((K, V), (none, none, *own)):
+        O = cf.attention_prefix(q, *args)
+        x = torch.einsum("bghd,gkd->bghk", q.view(2, 2, 2, d).double(), K[:, -70:].double()) * d ** -0.5
+        m = x.amax(-1, keepdim=True).clamp(min=0)
+        w = torch.exp(x - m)
+        total = w.sum(-1, keepdim=True) + (n - 70) * torch.exp(-m)      # the zero keys score 0
+        ref = (torch.einsum("bghk,gkd->bghd", w, V[:, -70:].double()) / total).reshape(2, 4, 1, d)
+        size = (torch.einsum("bghk,gkd->bghd", w, V[:, -70:].double().abs()) / total).reshape(2, 4, 1, d)
+        # a weight, and the sum of n of them in fp32 (a lane adds up to 2^10 of them before they join): off by
+        # 2^-8 and 2^10 u beside the score's error (as in check_attention)
+        tol = (2 * 2.0 ** -8 * 1.01 + 2.0 ** 10 * U + 1e-4) * size + 2.0 ** -8 * 1.01 * ref.abs()
+        assert bool(((O.double() - ref).abs() <= tol).all())
+
+
 # ---------------------------------------------------------------- refusals (no GPU)
 A_, B_, C_, D_, E_ = (0x7F0000000000 + 0x100000 * i for i in range(5))
 
@@ -522,7 +596,7 @@ def prefix_args(**kw):
     (dict(Vs=None), "CF_ERR_NULL"), (dict(Ks=C_ + 8), "CF_ERR_ALIGN"), (dict(kp_l=60), "CF_ERR_LD"),
     (dict(ks_l=68), "CF_ERR_ALIGN"), (dict(vs_h=1004), "CF_ERR_ALIGN"), (dict(q_b=-256), "CF_ERR_ALIGN"),
     (dict(vp_l=1 << 22), "CF_ERR_LD"), (dict(lens=E_ + 2), "CF_ERR_ALIGN"), (dict(O=A_), "CF_ERR_ALIAS"),
-    (dict(O=C_), "CF_ERR_ALIAS")])
+    (dict(O=C_), "CF_ERR_ALIAS"), (dict(o_b=0), "CF_ERR_LD"), (dict(o_h=0), "CF_ERR_LD")])
 def test_prefix_refuses(kw, status):
     assert cf.STATUS[cf.cf_attention_prefix(prefix_args(**kw), None, 0, None)] == status, cf.cf_last_error()
 
@@ -557,8 +631,18 @@ def test_helpers_refuse():
                  lambda: cf.gemm_i8(q, q, out=x), lambda: cf.rmsnorm_quant(x.t())):
         with pytest.raises(ValueError):
             call()
+    for call in (lambda: cf.rmsnorm_quant(x, code="int4"), lambda: cf.gemm_i8(q, q, act="silu"),
+                 lambda: cf.gemm_i8(q, q[:, :0])):
+        with pytest.raises(ValueError):
+            call()
     with pytest.raises(TypeError):
         cf.gemm_i8(x, x)
+    with pytest.raises(cf.CfError, match="CF_ERR_ALIAS"):
+        cf.rmsnorm_quant(x, x.clone(), residual=x)
+    with pytest.raises(cf.CfError, match="CF_ERR_ALIGN"):
+        cf.rmsnorm_quant(torch.zeros((4, 30), dtype=BF16, device="cuda"))
+    with pytest.raises(cf.CfError, match="CF_ERR_SHAPE"):
+        cf.gemm_i8(q[:, :40].contiguous(), q[:, :40].contiguous())
     a = torch.zeros((2, 4, 1, 64), dtype=BF16, device="cuda")
     k = torch.zeros((2, 8, 64), dtype=BF16, device="cuda")
     for kw in (dict(Ks=a), dict(Ks=a, Vs=a), dict(lens=torch.zeros((2,), device="cuda")), dict(out=k)):
