@@ -638,13 +638,12 @@ def _row_ld(t, M, N, size):
     return s[0] if M > 1 else -(-N * size // 16) * 16 // size
 
 
-def _vector(t, n, device, name):
-    """The address of a contiguous fp32 vector of n on `device`, or None."""
+def _vector(t, n, f32, device, name):
+    """The address of n contiguous fp32 values on `device`, or None."""
     if t is None:
         return None
-    if t.dtype is not _torch().float32 or t.dim() != 1 or t.size(0) != n or not t.is_contiguous() or \
-            t.get_device() != device:
-        raise ValueError(f"{name}: expected a contiguous fp32 vector of {n} beside the other operands")
+    if t.dtype is not f32 or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{name}: expected {n} contiguous fp32 values beside the other operands")
     return t.data_ptr()
 
 
@@ -681,7 +680,7 @@ def rmsnorm_quant(X, R=None, gamma=None, *, eps=1e-5, norm=True, code="int8", re
         return _elsewhere(rmsnorm_quant, X, stream, R, gamma, eps=eps, norm=norm, code=code, residual=residual, out=out,
                           scale=scale)
     L, torch, device, raw = here
-    shape, dtype, dev = X.shape, X.dtype, X.device
+    shape, dtype, dev, f32 = X.shape, X.dtype, X.device, torch.float32
     M, N = shape
     dt = _dt(X)
     size = 4 if dt == CF_F32 else 2
@@ -695,12 +694,12 @@ def rmsnorm_quant(X, R=None, gamma=None, *, eps=1e-5, norm=True, code="int8", re
     elif R is not None:
         H = _rows(torch, M, N, dtype, dev, size)
     Q = _rows(torch, M, N, qdt, dev, 1) if out is None else _like(out, shape, qdt, device, "out")
-    s = torch.empty(M, dtype=torch.float32, device=dev) if scale is None else scale
+    s = torch.empty(M, dtype=f32, device=dev) if scale is None else scale
     a = RmsnormQuantArgs(_RMSNORM_QUANT_SIZE, M, N, dt, X.data_ptr(), _row_ld(X, M, N, size),
                          None if R is None else R.data_ptr(), 0 if R is None else _row_ld(R, M, N, size),
                          None if H is None else H.data_ptr(), 0 if H is None else _row_ld(H, M, N, size),
-                         _vector(gamma, N, device, "gamma"), 1 if norm else 0, eps, cdt, Q.data_ptr(),
-                         _row_ld(Q, M, N, 1), _vector(s, M, device, "scale"))
+                         _vector(gamma, N, f32, device, "gamma"), 1 if norm else 0, eps, cdt, Q.data_ptr(),
+                         _row_ld(Q, M, N, 1), _vector(s, M, f32, device, "scale"))
     status = L.cf_rmsnorm_quant(C.byref(a), raw)
     if status:
         _check(status)
@@ -713,27 +712,28 @@ _ACTS = {"none": CF_ACT_NONE, "gelu": CF_ACT_GELU, "gelu_tanh": CF_ACT_GELU_TANH
 def gemm_i8(A, B, sa=None, sb=None, *, bias=None, act="none", out_dtype=None, out=None, stream=None):
     """C = act((A . B^T) * sa[:, None] * sb + bias) of int8 A [M, K] and B [N, K].
 
-    sa fp32 [M] (a scale per token), sb fp32 [N] (per channel), bias fp32 [N];
+    sa fp32 [M] or [M, 1] (a scale per token), sb fp32 [N] (per channel), bias fp32 [N];
     act "none", "gelu", "gelu_tanh" or "relu"; C bf16 (or fp32) [M, N].
     """
     here = _here(A, stream)
     if here is None:
         return _elsewhere(gemm_i8, A, stream, B, sa, sb, bias=bias, act=act, out_dtype=out_dtype, out=out)
     L, torch, device, raw = here
+    i8, f32 = torch.int8, torch.float32
     M, K = A.shape
     N = B.size(0)
-    if A.dtype is not torch.int8 or B.dtype is not torch.int8:
+    if A.dtype is not i8 or B.dtype is not i8:
         raise TypeError(f"expected int8 operands, got {A.dtype} and {B.dtype}")
-    _like(B, (N, K), torch.int8, device, "B")
+    _like(B, (N, K), i8, device, "B")
     if out is None:
-        dt = CF_F32 if out_dtype is torch.float32 else CF_BF16
+        dt = CF_F32 if out_dtype is f32 else CF_BF16
         if dt == CF_BF16 and out_dtype not in (None, torch.bfloat16):
             raise TypeError(f"unsupported dtype {out_dtype}")
-        Cm = _rows(torch, M, N, torch.float32 if dt == CF_F32 else torch.bfloat16, A.device, 4 if dt == CF_F32 else 2)
+        Cm = _rows(torch, M, N, f32 if dt == CF_F32 else torch.bfloat16, A.device, 4 if dt == CF_F32 else 2)
     else:
         dt, Cm = _dt(out), _like(out, (M, N), out_dtype or out.dtype, device, "out")
     a = GemmI8Args(_GEMM_I8_SIZE, M, N, K, A.data_ptr(), _row_ld(A, M, K, 1), B.data_ptr(), _row_ld(B, N, K, 1),
-                   _vector(sa, M, device, "sa"), _vector(sb, N, device, "sb"), _vector(bias, N, device, "bias"),
+                   _vector(sa, M, f32, device, "sa"), _vector(sb, N, f32, device, "sb"), _vector(bias, N, f32, device, "bias"),
                    _choice(_ACTS, act, "act"), dt, Cm.data_ptr(), _row_ld(Cm, M, N, 4 if dt == CF_F32 else 2))
     status = L.cf_gemm_i8(C.byref(a), raw)
     if status:
