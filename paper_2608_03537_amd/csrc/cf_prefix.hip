@@ -383,7 +383,7 @@ __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb
     const int ob = KIND == PREFIX ? (m0 + r) / R : b, om = KIND == PREFIX ? (m0 + r) % R : m0 + r;
     if (KIND == WHOLE && slots == 0) {
       const int i = om / G;
-      store_row(p, ob, hk * G + om % G, i, d0, o, L, p.P + own_seen(p, len, i) > 0);
+      store_row(p, ob, hk * G + om % G, i, d0, o, L, p.P > 0 || own_seen(p, len, i) > 0);
     } else {
       const int64_t row = (int64_t)(ob * p.Hk + hk) * R + om;
       float* dst = pr.o(p, slot, row) + d0;
@@ -454,6 +454,8 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixParams p, int s
   const int row = min((int)blockIdx.x * ROWS + r, rows - 1);
   const float* const o0 = pr.o(p, 0, row) + d0;
   const float* const ml0 = pr.ml(p, slots, 0, row);
+  const int m = row % R, bh = row / R, hk = bh % p.Hk, b = bh / p.Hk, i = m / G;
+  const bool any = p.P > 0 || own_seen(p, own_len(p, b), i) > 0;
   float M = -INFINITY, L = 0.0f, o[8] = {};
   auto join = [&](float mz, float lz, const f32x4_t& x, const f32x4_t& y) {
     const float mn = fmaxf(M, mz);
@@ -482,8 +484,6 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixParams p, int s
     for (int q = 0; q < 4; ++q)
       if (s0 + q * WAYS < slots) join(mz[q], lz[q], x[q], y[q]);
   }
-  const int m = row % R, bh = row / R, hk = bh % p.Hk, b = bh / p.Hk, i = m / G;
-  const bool any = p.P + own_seen(p, own_len(p, b), i) > 0;
   if constexpr (WAYS > 1) {
     *reinterpret_cast<f32x4_t*>(&so[way][r][d0]) = f32x4_t{o[0], o[1], o[2], o[3]};
     *reinterpret_cast<f32x4_t*>(&so[way][r][d0 + 4]) = f32x4_t{o[4], o[5], o[6], o[7]};
@@ -512,7 +512,6 @@ struct PrefixPlan {
 };
 constexpr int kCUs = 256, kMaxParts = 32, kMaxOwnParts = 8;
 
-int query_waves(int64_t rows) { return rows <= 32 ? 1 : 4; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t row_blocks(int64_t rows, int qg) { return ceil_div(rows, 32 * qg); }
 
@@ -540,42 +539,46 @@ struct Task {   // one kind of workgroup of a launch
 
 PrefixPlan make_plan(const PrefixParams& p) {
   const int64_t R = (int64_t)(p.H / p.Hk) * p.Lq, Rall = p.B * R, rows = p.Hk * Rall;
-  PrefixPlan best{query_waves(Rall), query_waves(R), 1, 0};
-  auto keys = [&](int qg) { return qg == 1 ? 4096 / p.d : 64; };              // of a block
-  auto blocks = [&](int64_t n, int qg) { return ceil_div(n, keys(qg)); };
+  PrefixPlan best{1, R <= 32 ? 1 : 4, 1, 0};
+  auto blocks = [&](int64_t n, int qg) { return ceil_div(n, qg == 1 ? 4096 / p.d : 64); };   // of keys
   auto task = [&](int64_t nb, int parts, int64_t wgs, int qg) {
     const double scale = qg == 4 && p.d == 64 ? kStepMany64 : 1.0;
     return Task{(double)ceil_div(ceil_div(nb, parts), 4 / qg) * scale, (double)wgs * parts, qg};
   };
-  const int64_t wo = row_blocks(R, best.oq) * p.B * p.Hk, wp = row_blocks(Rall, best.pq) * p.Hk;
-  const int64_t bw = blocks(p.P, best.oq) + blocks(p.S, best.oq);
+  const int64_t wo = row_blocks(R, best.oq) * p.B * p.Hk;
   const double stream = 4.0 * p.Hk * p.d * (p.P + 0.8 * p.B * p.S) / kStream;
   const double part = kPartial * (double)rows * p.d;
   const int64_t most = ((int64_t)1 << 30) / std::max<int64_t>(1, rows * (p.d + 2) * 4);   // parts in 1 GiB
   double least = 0;
-  auto take = [&](double us, int np, int ns) {
+  auto take = [&](double us, int pq, int np, int ns) {
     if (least == 0 || us < least) {
       least = us;
+      best.pq = pq;
       best.np = np;
       best.ns = ns;
     }
   };
+  const int64_t bw = blocks(p.P, best.oq) + blocks(p.S, best.oq);
   for (int n = 1; n <= kMaxParts && (n == 1 || ((int64_t)n * 64 <= (int64_t)p.P + p.S && n <= most)); n *= 2) {
     const Task t = task(bw, n, wo, best.oq);
     const double us = t.wgs <= kCUs ? t.us(false) : std::ceil(t.wgs / (2 * kCUs)) * t.us(true);
-    take(std::max(us, stream) + (n > 1 ? kJoin + n * part : 0.0), n, 0);
+    take(std::max(us, stream) + (n > 1 ? kJoin + n * part : 0.0), 1, n, 0);
   }
   // whole rows of full workgroups on every CU: nothing to gain from parts
   if (p.P == 0 || p.S == 0 || (R >= 64 && wo >= kCUs)) return best;
-  const int64_t bp = blocks(p.P, best.pq), bo = blocks(p.S, best.oq);
-  for (int n = 1; n <= kMaxParts && (n == 1 || (int64_t)n * 64 <= p.P); n *= 2)
-    for (int m = 1; m <= kMaxOwnParts && (m == 1 || (int64_t)m * 64 <= p.S) && n + m <= most; m *= 2) {
-      const Task a = task(bp, n, wp, best.pq), b = task(bo, m, wo, best.oq);
-      const bool shared = a.wgs + b.wgs > kCUs;
-      const double ua = a.us(shared), ub = b.us(shared);
-      const double us = std::max({ua, ub, 1.36 * (a.wgs * ua + b.wgs * ub) / (2 * kCUs)});
-      take(std::max(us, stream) + kJoin + (n + m) * part, n, m);
-    }
+  // 32 rows a workgroup for the prefix read it more often, but start sooner: also where there are more rows
+  for (int pq : {1, 4}) {
+    if (pq == 4 ? Rall <= 32 : best.oq == 4) continue;
+    const int64_t bp = blocks(p.P, pq), bo = blocks(p.S, best.oq), wp = row_blocks(Rall, pq) * p.Hk;
+    for (int n = 1; n <= kMaxParts && (n == 1 || (int64_t)n * 64 <= p.P); n *= 2)
+      for (int m = 1; m <= kMaxOwnParts && (m == 1 || (int64_t)m * 64 <= p.S) && n + m <= most; m *= 2) {
+        const Task a = task(bp, n, wp, pq), b = task(bo, m, wo, best.oq);
+        const bool shared = a.wgs + b.wgs > kCUs;
+        const double ua = a.us(shared), ub = b.us(shared);
+        const double us = std::max({ua, ub, 1.36 * (a.wgs * ua + b.wgs * ub) / (2 * kCUs)});
+        take(std::max(us, stream) + kJoin + (n + m) * part, pq, n, m);
+      }
+  }
   return best;
 }
 
