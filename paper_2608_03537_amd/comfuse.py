@@ -622,11 +622,12 @@ def _here(X, stream):
 
 
 def _rows(torch, M, N, dtype, device, size):
-    """An [M, N] tensor whose rows start every multiple of 16 bytes (`size`: bytes of an element)."""
-    per = 16 // size
-    ld = -(-N // per) * per
-    t = torch.empty(M, ld, dtype=dtype, device=device)
-    return t if ld == N else t[:, :N]
+    """A new [M, N] tensor whose rows start every multiple of 16 bytes (`size`: bytes of an element), and its
+    leading dimension."""
+    if N * size % 16 == 0:
+        return torch.empty(M, N, dtype=dtype, device=device), N
+    ld = -(-N * size // 16) * 16 // size
+    return torch.empty(M, ld, dtype=dtype, device=device)[:, :N], ld
 
 
 def _row_ld(t, M, N, size):
@@ -639,9 +640,7 @@ def _row_ld(t, M, N, size):
 
 
 def _vector(t, n, f32, device, name):
-    """The address of n contiguous fp32 values on `device`, or None."""
-    if t is None:
-        return None
+    """The address of n contiguous fp32 values on `device`."""
     if t.dtype is not f32 or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
         raise ValueError(f"{name}: expected {n} contiguous fp32 values beside the other operands")
     return t.data_ptr()
@@ -686,20 +685,29 @@ def rmsnorm_quant(X, R=None, gamma=None, *, eps=1e-5, norm=True, code="int8", re
     size = 4 if dt == CF_F32 else 2
     cdt = _choice(_CODES, code, "code")
     qdt = torch.int8 if cdt == CF_I8 else torch.uint8
+    whole = N * size % 16 == 0    # rows of whole 16 bytes: a contiguous tensor's leading dimension is N
+    ldx = N if whole and X.is_contiguous() else _row_ld(X, M, N, size)
+    rp = hp = None
+    ldr = ldh = 0
+    H = residual
     if R is not None:
         _like(R, shape, dtype, device, "R")
-    H = residual
-    if H is not None:
+        rp, ldr = R.data_ptr(), N if whole and R.is_contiguous() else _row_ld(R, M, N, size)
+        if H is None:
+            H, ldh = _rows(torch, M, N, dtype, dev, size)
+            hp = H.data_ptr()
+    if residual is not None:
         _like(H, shape, dtype, device, "residual")
-    elif R is not None:
-        H = _rows(torch, M, N, dtype, dev, size)
-    Q = _rows(torch, M, N, qdt, dev, 1) if out is None else _like(out, shape, qdt, device, "out")
+        hp, ldh = H.data_ptr(), _row_ld(H, M, N, size)
+    if out is None:
+        Q, ldq = _rows(torch, M, N, qdt, dev, 1)
+    else:
+        Q = _like(out, shape, qdt, device, "out")
+        ldq = _row_ld(Q, M, N, 1)
     s = torch.empty(M, dtype=f32, device=dev) if scale is None else scale
-    a = RmsnormQuantArgs(_RMSNORM_QUANT_SIZE, M, N, dt, X.data_ptr(), _row_ld(X, M, N, size),
-                         None if R is None else R.data_ptr(), 0 if R is None else _row_ld(R, M, N, size),
-                         None if H is None else H.data_ptr(), 0 if H is None else _row_ld(H, M, N, size),
-                         _vector(gamma, N, f32, device, "gamma"), 1 if norm else 0, eps, cdt, Q.data_ptr(),
-                         _row_ld(Q, M, N, 1), _vector(s, M, f32, device, "scale"))
+    a = RmsnormQuantArgs(_RMSNORM_QUANT_SIZE, M, N, dt, X.data_ptr(), ldx, rp, ldr, hp, ldh,
+                         None if gamma is None else _vector(gamma, N, f32, device, "gamma"), 1 if norm else 0, eps, cdt,
+                         Q.data_ptr(), ldq, s.data_ptr() if scale is None else _vector(s, M, f32, device, "scale"))
     status = L.cf_rmsnorm_quant(C.byref(a), raw)
     if status:
         _check(status)
@@ -729,12 +737,18 @@ def gemm_i8(A, B, sa=None, sb=None, *, bias=None, act="none", out_dtype=None, ou
         dt = CF_F32 if out_dtype is f32 else CF_BF16
         if dt == CF_BF16 and out_dtype not in (None, torch.bfloat16):
             raise TypeError(f"unsupported dtype {out_dtype}")
-        Cm = _rows(torch, M, N, f32 if dt == CF_F32 else torch.bfloat16, A.device, 4 if dt == CF_F32 else 2)
+        Cm, ldc = _rows(torch, M, N, f32 if dt == CF_F32 else torch.bfloat16, A.device, 4 if dt == CF_F32 else 2)
     else:
         dt, Cm = _dt(out), _like(out, (M, N), out_dtype or out.dtype, device, "out")
-    a = GemmI8Args(_GEMM_I8_SIZE, M, N, K, A.data_ptr(), _row_ld(A, M, K, 1), B.data_ptr(), _row_ld(B, N, K, 1),
-                   _vector(sa, M, f32, device, "sa"), _vector(sb, N, f32, device, "sb"), _vector(bias, N, f32, device, "bias"),
-                   _choice(_ACTS, act, "act"), dt, Cm.data_ptr(), _row_ld(Cm, M, N, 4 if dt == CF_F32 else 2))
+        ldc = _row_ld(Cm, M, N, 4 if dt == CF_F32 else 2)
+    whole = K % 16 == 0
+    a = GemmI8Args(_GEMM_I8_SIZE, M, N, K,
+                   A.data_ptr(), K if whole and A.is_contiguous() else _row_ld(A, M, K, 1),
+                   B.data_ptr(), K if whole and B.is_contiguous() else _row_ld(B, N, K, 1),
+                   None if sa is None else _vector(sa, M, f32, device, "sa"),
+                   None if sb is None else _vector(sb, N, f32, device, "sb"),
+                   None if bias is None else _vector(bias, N, f32, device, "bias"),
+                   CF_ACT_NONE if act == "none" else _choice(_ACTS, act, "act"), dt, Cm.data_ptr(), ldc)
     status = L.cf_gemm_i8(C.byref(a), raw)
     if status:
         _check(status)
@@ -774,16 +788,21 @@ def attention_prefix(Q, Kp, Vp, Ks=None, Vs=None, lens=None, *, causal=False, sc
     if (Ks is None) != (Vs is None):
         raise ValueError("Ks and Vs come together")
     S = 0 if Ks is None else Ks.size(2)
-    _like(Q, shape, bf16, device, "Q")
-    _like(Kp, (Hk, P, d), bf16, device, "Kp")
-    _like(Vp, (Hk, P, d), bf16, device, "Vp")
+    # one condition where all is well; else _like names the operand
+    pshape, ks, vs = (Hk, P, d), (0, 0, 0, 1), (0, 0, 0, 1)
+    if not (Q.dtype is Kp.dtype is Vp.dtype is bf16 and Kp.shape == pshape and Vp.shape == pshape and
+            Kp.get_device() == Vp.get_device() == device):
+        for t, want, name in ((Q, shape, "Q"), (Kp, pshape, "Kp"), (Vp, pshape, "Vp")):
+            _like(t, want, bf16, device, name)
+    if Ks is not None:
+        oshape = (B, Hk, S, d)
+        if not (Ks.dtype is Vs.dtype is bf16 and Ks.shape == oshape and Vs.shape == oshape and
+                Ks.get_device() == Vs.get_device() == device):
+            _like(Ks, oshape, bf16, device, "Ks")
+            _like(Vs, oshape, bf16, device, "Vs")
+        ks, vs = Ks.stride(), Vs.stride()
     O = torch.empty_like(Q) if out is None else _like(out, shape, bf16, device, "out")
     q, o, kp, vpr = Q.stride(), O.stride(), Kp.stride(), Vp.stride()
-    ks = vs = (0, 0, 0, 1)
-    if Ks is not None:
-        _like(Ks, (B, Hk, S, d), bf16, device, "Ks")
-        _like(Vs, (B, Hk, S, d), bf16, device, "Vs")
-        ks, vs = Ks.stride(), Vs.stride()
     if not q[3] == o[3] == kp[2] == vpr[2] == ks[3] == vs[3] == 1:
         raise ValueError("expected unit innermost strides")
     if lens is not None:
