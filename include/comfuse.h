@@ -56,6 +56,7 @@ extern "C" {
 /* A workspace query that returns this size means an optional workspace: with it
    the call runs as row clusters, without it (NULL) on whole rows. */
 #define CF_WS_OPTIONAL_BYTES 8917008  /* CF_WS_HEADER_BYTES + 16 */
+#define CF_PREFIX_WS_HEADER_BYTES 262144  /* cf_attention_prefix arrival counters: 65536 words of 4 bytes */
 #define CF_B2B_WS_HEADER_BYTES 1048576  /* split-MLP arrival counters: 262144 words of 4 bytes */
 
 typedef enum {
@@ -404,9 +405,11 @@ cf_status cf_gemm_i8(const cf_gemm_i8_args* a, void* hip_stream);
  * NaN in a value row that causal hides from some queries of a call only reaches them too
  * (as 0 * NaN).  scale finite and > 0.  The softmax is exact (running maximum and sum in fp32);
  * P is rounded to bf16 for the second product, as in cf_b2bgemm.
- * Workspace: cf_attention_prefix_workspace() bytes (may be 0), 16-byte aligned,
- * no initial contents required; it holds partial results during the call
- * only.  Calls that share it must not overlap in time.
+ * Workspace: cf_attention_prefix_workspace() bytes (may be 0), 16-byte aligned:
+ * CF_PREFIX_WS_HEADER_BYTES of arrival counters, then partial results.  Zero-fill
+ * the header once before the first call; every call leaves it all zero again,
+ * so later calls of any shape find it valid.  Do not share the workspace with
+ * calls of another kind, and do not let calls that share it overlap in time.
  * ------------------------------------------------------------------------ */
 typedef struct {
   size_t struct_size;            /* = sizeof(cf_attention_prefix_args) */

@@ -29,6 +29,7 @@ CF_ACT_NONE, CF_ACT_GELU, CF_ACT_GELU_TANH, CF_ACT_RELU = 0, 1, 2, 3
 PATH_AUTO, PATH_WHOLE_ROW, PATH_CLUSTER, PATH_SPLIT = 0, 1, 2, 3
 CF_WS_HEADER_BYTES = 8916992       # zero-filled start of a row workspace
 CF_WS_OPTIONAL_BYTES = 8917008     # a workspace query's answer where the workspace may be left out
+CF_PREFIX_WS_HEADER_BYTES = 1 << 18   # arrival counters at the start of attention_prefix's workspace
 CF_B2B_WS_HEADER_BYTES = 1 << 20   # split-MLP arrival counters at the start of its workspace
 STATUS = {0: "CF_OK", 1: "CF_ERR_NULL", 2: "CF_ERR_SHAPE", 3: "CF_ERR_LD", 4: "CF_ERR_ALIGN",
           5: "CF_ERR_DTYPE", 6: "CF_ERR_WORKSPACE", 7: "CF_ERR_UNSUPPORTED", 8: "CF_ERR_ALIAS",
@@ -271,11 +272,10 @@ def _graph_workspace(nbytes, key, device, stream):
     capture = _capture_id(stream)
     have = _ws_graph.get(key)
     if have is None or capture is None or have[0] != capture or have[1].numel() < nbytes:
-        header = {"rows": CF_WS_HEADER_BYTES, "b2b": CF_B2B_WS_HEADER_BYTES}.get(key[2], 0)
+        header = {"rows": CF_WS_HEADER_BYTES, "b2b": CF_B2B_WS_HEADER_BYTES, "prefix": CF_PREFIX_WS_HEADER_BYTES}[key[2]]
         with torch.cuda.stream(stream):
             ws = torch.empty(max(nbytes, header), dtype=torch.uint8, device=device)
-            if header:
-                ws[:header].view(torch.int32).zero_()
+            ws[:header].view(torch.int32).zero_()
         have = _ws_graph[key] = (capture, ws)
     return have[1]
 
@@ -286,8 +286,8 @@ def workspace(nbytes, device, stream=None, kind="rows"):
     share it; calls on different streams get different workspaces (the
     row-cluster round counters live in it).  kind "b2b" is that of the split
     MLP and of attention with split keys (their arrival counters must not meet
-    another entry point's data); "prefix" that of attention_prefix, which needs no
-    initial contents.  Calls captured into a graph share one of the
+    another entry point's data), "prefix" that of attention_prefix, for the same
+    reason.  Calls captured into a graph share one of the
     capture's own, never an eager one: a graph outlives what the cache holds,
     and its replays may overlap eager calls or another graph."""
     torch = _torch()
@@ -761,7 +761,7 @@ def _prefix_workspace(torch, need, device, key):
         return workspace(need, device, None, kind="prefix")
     ws = _ws_cache.get(key)
     if ws is None or ws.numel() < need:
-        ws = _ws_cache[key] = torch.empty(need, dtype=torch.uint8, device=device)
+        ws = _ws_cache[key] = torch.zeros(need, dtype=torch.uint8, device=device)
     return ws
 
 
@@ -775,7 +775,8 @@ def attention_prefix(Q, Kp, Vp, Ks=None, Vs=None, lens=None, *, causal=False, sc
     are multiples of 8 elements with unit innermost stride (caches stored
     token-major are passed as transposed views).  causal: query i sees the own
     keys j < lens[b] - (Lq - 1 - i).  A query that sees no key gets 0.  ws: a
-    workspace of the caller's own (cf_attention_prefix_workspace bytes).
+    workspace of the caller's own (cf_attention_prefix_workspace bytes, its first
+    CF_PREFIX_WS_HEADER_BYTES zero before its first use).
     """
     here = _here(Q, stream)
     if here is None:

@@ -70,6 +70,33 @@ __device__ __forceinline__ float lane_pair_max_swap(float v) {
 #endif
 }
 
+// Accesses that are coherent between the XCDs (bytes `off` behind base, below 2^31), for data that
+// workgroups of one launch hand to each other.
+__device__ __forceinline__ void coherent_store16(float* base, uint32_t off, u32x4_t v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_raw_buffer_store_b128(v, __builtin_amdgcn_make_buffer_rsrc(base, 0, 0x7FFFFFFF, 0x00020000), off, 0, 16);
+#endif
+}
+__device__ __forceinline__ void coherent_store8(float* base, uint32_t off, u32x2_t v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_raw_buffer_store_b64(v, __builtin_amdgcn_make_buffer_rsrc(base, 0, 0x7FFFFFFF, 0x00020000), off, 0, 16);
+#endif
+}
+__device__ __forceinline__ u32x4_t coherent_load16(float* base, uint32_t off) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc(base, 0, 0x7FFFFFFF, 0x00020000), off, 0, 16);
+#else
+  return u32x4_t{};
+#endif
+}
+__device__ __forceinline__ u32x2_t coherent_load8(float* base, uint32_t off) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_raw_buffer_load_b64(__builtin_amdgcn_make_buffer_rsrc(base, 0, 0x7FFFFFFF, 0x00020000), off, 0, 16);
+#else
+  return u32x2_t{};
+#endif
+}
+
 // dma16 from base + lane_off + wave_off bytes (base and wave_off wave-uniform, offsets below 2^31): the
 // address takes no vector arithmetic beyond the lane's own offset.
 __device__ __forceinline__ void dma16_at(const char* base, uint32_t lane_off, uint32_t wave_off, char* lds) {

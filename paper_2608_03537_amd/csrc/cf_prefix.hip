@@ -15,6 +15,7 @@
 
 #include "cf_attn.h"
 #include "cf_gemm_tile.h"
+#include "comfuse.h"
 
 namespace cf {
 
@@ -78,11 +79,85 @@ struct PartRows {
   }
 };
 
+// Whole rows in parts, up to 32 rows of a (sequence, key head): the workgroup that finishes one last
+// joins its parts, which saves a launch (3 us of the host; 1 x 12 heads, 89 + 431 keys 14.3 -> 11.7 us a
+// call from Python).  Each has an arrival counter, zero between calls.  A workgroup of the prefix's
+// parts has rows of several sequences, and would join all of them if it came last (47 x 16 heads 17
+// -> 70 us): those keep the second launch.
+
+// The parts of the rows of (b, hk), by the whole workgroup: 8 rows at a time, 256 / D threads a part's
+// row beside each other, WAYS taking the parts in turn.  The grouping depends on the sizes only.
+template <int D>
+__device__ __forceinline__ void join_rows(const PrefixParams& p, char* smem, int b, int hk, int slots) {
+  constexpr int TPR = D / 8, RPP = 8, WAYS = 256 / TPR / RPP, AHEAD = 6;
+  const int tid = threadIdx.x, g = tid / TPR, r = g % RPP, way = g / RPP, d0 = tid % TPR * 8;
+  const int G = p.H / p.Hk, R = G * p.Lq;
+  const uint32_t rows = (uint32_t)(p.B * p.Hk * R), ml0 = (uint32_t)slots * rows * (D * 4);
+  float* const so = reinterpret_cast<float*>(smem);             // [WAYS][RPP][D + 2]
+  const int len = own_len(p, b);
+  for (int m0 = 0; m0 < R; m0 += RPP) {
+    const int m = min(m0 + r, R - 1);
+    const uint32_t row = (uint32_t)((b * p.Hk + hk) * R + m);
+    float M = -INFINITY, L = 0.0f, o[8] = {};
+    auto join = [&](float mz, float lz, const float (&x)[8]) {
+      const float mn = fmaxf(M, mz);
+      const float fo = M == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M - mn);
+      const float fz = mz == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mz - mn);
+      M = mn;
+      L = fmaf(fz, lz, fo * L);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = fmaf(fz, x[e], fo * o[e]);
+    };
+    for (int s0 = way; s0 < slots; s0 += AHEAD * WAYS) {
+      u32x4_t x[AHEAD], y[AHEAD];
+      u32x2_t v[AHEAD];
+#pragma unroll
+      for (int q = 0; q < AHEAD; ++q) {
+        const uint32_t at = (uint32_t)min(s0 + q * WAYS, slots - 1) * rows + row;
+        x[q] = coherent_load16(p.ws, at * (D * 4) + d0 * 4);
+        y[q] = coherent_load16(p.ws, at * (D * 4) + d0 * 4 + 16);
+        v[q] = coherent_load8(p.ws, ml0 + at * 8);
+      }
+#pragma unroll
+      for (int q = 0; q < AHEAD; ++q)
+        if (s0 + q * WAYS < slots) {
+          float f[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            f[e] = __uint_as_float(x[q][e]);
+            f[4 + e] = __uint_as_float(y[q][e]);
+          }
+          join(__uint_as_float(v[q][0]), __uint_as_float(v[q][1]), f);
+        }
+    }
+    float* const mine = so + (way * RPP + r) * (D + 4);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mine[d0 + e] = o[e];
+    if (d0 == 0) {
+      mine[D] = M;
+      mine[D + 1] = L;
+    }
+    __syncthreads();
+    if (way == 0 && m0 + r < R) {
+#pragma unroll
+      for (int w = 1; w < WAYS; ++w) {
+        const float* other = so + (w * RPP + r) * (D + 4);
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = other[d0 + e];
+        join(other[D], other[D + 1], f);
+      }
+      store_row(p, b, hk * G + m % G, m / G, d0, o, L, p.P > 0 || own_seen(p, len, m / G) > 0);
+    }
+    __syncthreads();
+  }
+}
+
 // Rows m0 .. of (b, hk), or with PREFIX of all sequences of hk, over part z of `parts` of their key
 // blocks.  slots = 0: the output rows; else partial results, this one at `slot`.
-template <int KIND, int D, int QG>
+template <int KIND, int D, int QG, bool JOIN>
 __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb, int b, int hk, int z, int parts, int slot,
-                                       int slots) {
+                                       int slots, unsigned* count) {
   using A = PrefixShape<D, QG>;
   constexpr int KS = A::KS, BK = A::BK;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -386,15 +461,38 @@ __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb
       store_row(p, ob, hk * G + om % G, i, d0, o, L, p.P > 0 || own_seen(p, len, i) > 0);
     } else {
       const int64_t row = (int64_t)(ob * p.Hk + hk) * R + om;
-      float* dst = pr.o(p, slot, row) + d0;
-      *reinterpret_cast<f32x4_t*>(dst) = f32x4_t{o[0], o[1], o[2], o[3]};
-      *reinterpret_cast<f32x4_t*>(dst + 4) = f32x4_t{o[4], o[5], o[6], o[7]};
-      if (d0 == 0) {
-        float* to = pr.ml(p, slots, slot, row);
-        to[0] = M;
-        to[1] = L;
+      if constexpr (JOIN) {   // the partial results take at most 1 GiB
+        const f32x4_t x = {o[0], o[1], o[2], o[3]}, y = {o[4], o[5], o[6], o[7]};
+        const uint32_t at = (uint32_t)(slot * pr.rows + row);
+        coherent_store16(p.ws, at * (D * 4) + d0 * 4, __builtin_bit_cast(u32x4_t, x));
+        coherent_store16(p.ws, at * (D * 4) + d0 * 4 + 16, __builtin_bit_cast(u32x4_t, y));
+        if (d0 == 0)
+          coherent_store8(p.ws, (uint32_t)(slots * pr.rows) * (D * 4) + at * 8, u32x2_t{__float_as_uint(M), __float_as_uint(L)});
+      } else {
+        float* dst = pr.o(p, slot, row) + d0;
+        *reinterpret_cast<f32x4_t*>(dst) = f32x4_t{o[0], o[1], o[2], o[3]};
+        *reinterpret_cast<f32x4_t*>(dst + 4) = f32x4_t{o[4], o[5], o[6], o[7]};
+        if (d0 == 0) {
+          float* to = pr.ml(p, slots, slot, row);
+          to[0] = M;
+          to[1] = L;
+        }
       }
     }
+  }
+  if constexpr (JOIN) {
+    static_assert(KIND == WHOLE && QG == 1, "the parts of one (sequence, key head)");
+    // Count the arrival; the last workgroup joins (the counter goes back to 0, ready for the next call).
+    wait_vmcnt<0>();          // this wave's partial results are written
+    __syncthreads();          // ... and every wave's; the LDS is free
+    int* const last = reinterpret_cast<int*>(smem + 16384);   // behind what join_rows uses
+    if (tid == 0) {
+      unsigned* const c = count + hk * p.B + b;
+      *last = __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)(slots - 1);
+      if (*last) __hip_atomic_store(c, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (*last) join_rows<D>(p, smem, b, hk, slots);
   }
 }
 
@@ -407,15 +505,16 @@ __device__ __forceinline__ int xcd_task(int L, int T) {
 
 // One launch over (key head, sequence, part, row block).  Later row blocks first: with
 // causal they see more keys.
-template <int D, int QG>
-__global__ __launch_bounds__(256, 2) void prefix_whole_kernel(PrefixParams p, int nrb, int parts) {
+// parts > 1: partial results, joined here (JOIN) or by prefix_merge_kernel.
+template <int D, int QG, bool JOIN>
+__global__ __launch_bounds__(256, 2) void prefix_whole_kernel(PrefixParams p, int nrb, int parts, unsigned* count) {
   __shared__ __attribute__((aligned(16))) char smem[PrefixShape<D, QG>::LDS];
   int t = xcd_task(blockIdx.x, gridDim.x);
   const int rb = nrb - 1 - t % nrb;
   t /= nrb;
   const int z = t % parts;
   t /= parts;
-  attend<WHOLE, D, QG>(p, smem, rb, t % p.B, t / p.B, z, parts, z, parts > 1 ? parts : 0);
+  attend<WHOLE, D, QG, JOIN>(p, smem, rb, t % p.B, t / p.B, z, parts, z, parts > 1 ? parts : 0, count);
 }
 
 // The parts of the prefix, (key head, part, row block over all sequences), then those of the own
@@ -429,14 +528,14 @@ __global__ __launch_bounds__(256, 2) void prefix_split_kernel(PrefixParams p, in
     int t = xcd_task(blockIdx.x, tp);
     const int rb = t % nrb_p;
     t /= nrb_p;
-    attend<PREFIX, D, PQ>(p, smem, rb, 0, t / np, t % np, np, t % np, np + ns);
+    attend<PREFIX, D, PQ, false>(p, smem, rb, 0, t / np, t % np, np, t % np, np + ns, nullptr);
   } else {
     int t = xcd_task(blockIdx.x - tp, gridDim.x - tp);
     const int rb = nrb_o - 1 - t % nrb_o;
     t /= nrb_o;
     const int z = t % ns;
     t /= ns;
-    attend<OWN, D, OQ>(p, smem, rb, t % p.B, t / p.B, z, ns, np + z, np + ns);
+    attend<OWN, D, OQ, false>(p, smem, rb, t % p.B, t / p.B, z, ns, np + z, np + ns, nullptr);
   }
 }
 
@@ -509,17 +608,19 @@ struct PrefixPlan {
   int pq, oq;   // 32-row waves of a workgroup: prefix parts, own parts or whole rows
   int np, ns;   // split: parts of the prefix and of the own keys.  ns = 0: whole rows in np parts
   int slots() const { return ns > 0 ? np + ns : np > 1 ? np : 0; }
+  bool joined() const { return ns == 0 && np > 1 && oq == 1; }   // by the last workgroup, without a second launch
 };
+constexpr size_t kCounterBytes = CF_PREFIX_WS_HEADER_BYTES;   // the counters of (sequence, key head); the partial results follow
 constexpr int kCUs = 256, kMaxParts = 32, kMaxOwnParts = 8;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t row_blocks(int64_t rows, int qg) { return ceil_div(rows, 32 * qg); }
 
 // The estimate (us).  A step is one key block of every group of a workgroup: alone on its CU,
-// and where two workgroups share the CU; a workgroup's start and merge; the joining launch, and
+// and where two workgroups share the CU; a workgroup's start and merge; the join, and
 // a partial result's write and read.  Fitted to 80 calls of 1 to 64 sequences, 1 to 500 queries and
 // 64 to 16000 prefix keys, each measured in 10 to 40 cuts: the cut that the estimate takes is
-// 2 % slower than the best one on average, 14 % at worst.  Some of them (us: whole rows; the best split):
+// 2 % slower on the device than the best one on average, 14 % at worst.  Some of them (us: whole rows; the best split):
 //     4 x 8 heads, 1 query, 128 + 64 keys, d 64                5.6     8.5
 //     64 x 8 heads, 1 query, 512 + 128, d 64                  10.7    12.5
 //     16 x 16 heads, 5 queries, 4095 + 333, d 64              22.6    15.5 (4 + 1 parts)
@@ -527,7 +628,9 @@ int64_t row_blocks(int64_t rows, int qg) { return ceil_div(rows, 32 * qg); }
 //     64 x 32 heads of 8, 1 query, 8192 + 512, d 128           118    39.8 (8 + 2)
 constexpr double kStepFew = 0.95, kStepFew2 = 1.9, kStepMany = 1.6, kStepMany2 = 2.35;   // QG 1, QG 4; 2: two a CU
 constexpr double kStepMany64 = 0.62;              // QG 4 steps at d = 64 by those at d = 128
-constexpr double kStart = 6.6, kJoin = 3.3, kPartial = 1.9e-6, kStream = 4.8e6;   // kStream: bytes a us
+constexpr double kStart = 6.6, kPartial = 1.9e-6, kStream = 4.8e6;   // kStream: bytes a us
+constexpr double kJoin = 4.8;                     // the joining launch, on the device and on the host
+constexpr double kJoinBy8 = 1.0, kJoinOwn = 2.3;  // joined by the last workgroup: every 8 rows, and besides
 
 struct Task {   // one kind of workgroup of a launch
   double steps, wgs;
@@ -562,7 +665,8 @@ PrefixPlan make_plan(const PrefixParams& p) {
   for (int n = 1; n <= kMaxParts && (n == 1 || ((int64_t)n * 64 <= (int64_t)p.P + p.S && n <= most)); n *= 2) {
     const Task t = task(bw, n, wo, best.oq);
     const double us = t.wgs <= kCUs ? t.us(false) : std::ceil(t.wgs / (2 * kCUs)) * t.us(true);
-    take(std::max(us, stream) + (n > 1 ? kJoin + n * part : 0.0), 1, n, 0);
+    const double join = best.oq == 1 ? kJoinOwn + kJoinBy8 * (double)ceil_div(R, 8) : kJoin;
+    take(std::max(us, stream) + (n > 1 ? join + n * part : 0.0), 1, n, 0);
   }
   // whole rows of full workgroups on every CU: nothing to gain from parts
   if (p.P == 0 || p.S == 0 || (R >= 64 && wo >= kCUs)) return best;
@@ -582,10 +686,10 @@ PrefixPlan make_plan(const PrefixParams& p) {
   return best;
 }
 
-template <int D, int QG>
-hipError_t launch_whole(const PrefixParams& p, int parts, hipStream_t st) {
+template <int D, int QG, bool JOIN>
+hipError_t launch_whole(const PrefixParams& p, int parts, unsigned* count, hipStream_t st) {
   const int64_t R = (int64_t)(p.H / p.Hk) * p.Lq, nrb = row_blocks(R, QG), wgs = nrb * parts * p.Hk * p.B;
-  hipLaunchKernelGGL((prefix_whole_kernel<D, QG>), dim3((unsigned)wgs), dim3(256), 0, st, p, (int)nrb, parts);
+  hipLaunchKernelGGL((prefix_whole_kernel<D, QG, JOIN>), dim3((unsigned)wgs), dim3(256), 0, st, p, (int)nrb, parts, count);
   return hipGetLastError();
 }
 
@@ -606,9 +710,12 @@ hipError_t launch_merge(const PrefixParams& p, int slots, hipStream_t st) {
 }
 
 template <int D>
-hipError_t launch_all(const PrefixParams& p, const PrefixPlan& pl, hipStream_t st) {
+hipError_t launch_all(PrefixParams p, const PrefixPlan& pl, hipStream_t st) {
+  unsigned* const count = reinterpret_cast<unsigned*>(p.ws);
+  if (pl.slots() > 0) p.ws += kCounterBytes / 4;
+  if (pl.joined()) return launch_whole<D, 1, true>(p, pl.np, count, st);
   hipError_t e;
-  if (pl.ns == 0) e = pl.oq == 1 ? launch_whole<D, 1>(p, pl.np, st) : launch_whole<D, 4>(p, pl.np, st);
+  if (pl.ns == 0) e = pl.oq == 1 ? launch_whole<D, 1, false>(p, 1, nullptr, st) : launch_whole<D, 4, false>(p, pl.np, nullptr, st);
   else if (pl.pq == 1) e = launch_split<D, 1, 1>(p, pl, st);
   else e = pl.oq == 1 ? launch_split<D, 4, 1>(p, pl, st) : launch_split<D, 4, 4>(p, pl, st);
   if (e != hipSuccess || pl.slots() == 0) return e;
@@ -619,7 +726,9 @@ hipError_t launch_all(const PrefixParams& p, const PrefixPlan& pl, hipStream_t s
 }  // namespace
 
 size_t prefix_workspace(const PrefixParams& p) {
-  return (size_t)make_plan(p).slots() * (size_t)p.B * (size_t)p.H * (size_t)p.Lq * (size_t)(p.d + 2) * 4;
+  const int slots = make_plan(p).slots();
+  if (slots == 0) return 0;
+  return kCounterBytes + (size_t)slots * (size_t)p.B * (size_t)p.H * (size_t)p.Lq * (size_t)(p.d + 2) * 4;
 }
 
 hipError_t launch_prefix(const PrefixParams& p, hipStream_t st) {

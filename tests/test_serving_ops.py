@@ -501,6 +501,36 @@ def test_split_calls_captured_and_on_two_streams():
 
 
 @gpu
+def test_one_workspace_for_calls_of_several_sizes():
+    """The counters at its start are zero again after every call, whatever its size and cut."""
+    g = gen(6)
+    ws = torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda")
+    head = ws[:cf.CF_PREFIX_WS_HEADER_BYTES].view(torch.int32)
+    head.zero_()
+    kinds = set()
+    for B, H, Hk, Lq, P, S, d in [(1, 8, 2, 1, 4000, 300, 128), (9, 14, 2, 1, 900, 700, 64), (3, 8, 1, 3, 5000, 40, 64),
+                                  (5, 4, 4, 7, 2000, 900, 128), (2, 6, 2, 16, 3000, 64, 64), (40, 8, 8, 1, 3000, 50, 128),
+                                  (1, 2, 2, 1, 0, 6000, 128), (2, 4, 1, 50, 9000, 100, 64), (11, 3, 3, 1, 2500, 33, 64)]:
+        a = prefix_inputs(g, B, H, Hk, Lq, P, S, d)
+        lens = torch.randint(0, S + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+        lens[0] = S
+        need = cf.cf_attention_prefix_workspace(prefix_args(batch=B, H=H, Hk=Hk, Lq=Lq, P=P, S=S, d=d))
+        kinds.add(need > 0)
+        for _ in range(2):
+            O = cf.attention_prefix(*a, lens, causal=Lq > 1, ws=ws)
+            check_attention(O, *a, lens, Lq > 1)
+            assert not head.any()
+        for _ in range(5):                           # the same bits, whichever workgroup joins
+            assert torch.equal(cf.attention_prefix(*a, lens, causal=Lq > 1, ws=ws), O)
+        if need:
+            with pytest.raises(cf.CfError, match="CF_ERR_WORKSPACE"):
+                cf.attention_prefix(*a, lens, ws=ws[:need - 16])
+            with pytest.raises(cf.CfError, match="CF_ERR_ALIGN"):
+                cf.attention_prefix(*a, lens, ws=ws[8:])
+    assert kinds == {True}
+
+
+@gpu
 def test_offsets_past_32_bits():
     """Rows, keys and tokens that lie more than 4 GiB behind their tensor's start."""
     g = gen(11)
