@@ -338,7 +338,8 @@ cf_status cf_rowop(int64_t batch, int64_t M, int64_t N, cf_dtype in,
  * (same pointer and ld): the residual stream is then updated in place.
  * A row whose t is all zero gets s = 0 and zero codes; a row in which some t
  * is NaN or infinite gets s = NaN and zero codes.  The mean of squares is held
- * in fp32: s is 0 where it overflows (|h| about 1.8e19 and more).
+ * in fp32: s is 0 where it overflows (|h| about 1.8e19 and more), and with eps = 0
+ * inexact, in the end infinite, where it underflows (|h| below 1e-19 throughout).
  * ------------------------------------------------------------------------ */
 typedef struct {
   size_t struct_size;            /* = sizeof(cf_rmsnorm_quant_args) */

@@ -191,10 +191,21 @@ __global__ __launch_bounds__(NT) void rms_quant_kernel(RmsQuantParams p) {
 }
 
 template <typename T, int TPR, int C, int NT>
-hipError_t launch(const RmsQuantParams& p, hipStream_t st) {
+hipError_t launch(RmsQuantParams p, hipStream_t st) {
   constexpr int ROWS = NT / TPR;
-  hipLaunchKernelGGL((rms_quant_kernel<T, TPR, C, NT>), dim3((unsigned)((p.M + ROWS - 1) / ROWS)), dim3(NT), 0, st, p);
-  return hipGetLastError();
+  constexpr int64_t kMost = ((int64_t)1 << 31) / NT * ROWS;   // rows a launch: a grid has less than 2^32 threads
+  hipError_t e = hipSuccess;
+  for (int64_t left = p.M; left > 0 && e == hipSuccess; left -= kMost) {
+    p.M = (int)std::min(left, kMost);
+    hipLaunchKernelGGL((rms_quant_kernel<T, TPR, C, NT>), dim3((unsigned)((p.M + ROWS - 1) / ROWS)), dim3(NT), 0, st, p);
+    e = hipGetLastError();
+    p.X = reinterpret_cast<const T*>(p.X) + p.M * p.ldx;
+    if (p.R) p.R = reinterpret_cast<const T*>(p.R) + p.M * p.ldr;
+    if (p.H) p.H = reinterpret_cast<T*>(p.H) + p.M * p.ldh;
+    p.Q = reinterpret_cast<uint8_t*>(p.Q) + p.M * p.ldq;
+    p.s += p.M;
+  }
+  return e;
 }
 
 }  // namespace

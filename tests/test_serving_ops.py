@@ -118,6 +118,20 @@ def test_norm_in_place_strides_and_padding(dtype):
     assert bool((full[:, N:] == 99).all()) and bool((R._base[:, N:] == 5.0).all())
 
 
+@gpu
+def test_norm_more_rows_than_a_grid():
+    """Four rows a workgroup of 256 threads: 2^26 + 5 rows are more than 2^32 threads."""
+    M, N = (1 << 26) + 5, 8
+    X = torch.zeros((M, N), dtype=BF16, device="cuda")
+    out = torch.full((M, 16), 77, dtype=torch.int8, device="cuda")[:, :N]
+    at = torch.tensor([0, 5, (1 << 25) - 1, 1 << 25, (1 << 26) - 1, 1 << 26, M - 1], device="cuda")
+    X[at] = torch.randn((7, N), generator=gen(12), device="cuda").to(BF16)
+    H = X.clone()
+    Q, s, _ = cf.rmsnorm_quant(X, H, residual=H, out=out)
+    check_norm(Q[at], s[at], H[at], norm_ref(X[at], X[at], None, 1e-5, True, "int8"), "int8", BF16)
+    assert int((s != 0).sum()) == 7 and int(Q.any(1).sum()) == 7 and int(H.any(1).sum()) == 7
+
+
 # ---------------------------------------------------------------- gemm_i8
 def act64(y, act):
     if act == "gelu":
