@@ -367,7 +367,7 @@ cf_status cf_rmsnorm_quant(const cf_rmsnorm_quant_args* a, void* hip_stream);
  * A M x K and B N x K (CF_LAYOUT_NK) of I8, sa fp32 [M], sb fp32 [N] (NULL: 1),
  * bias fp32 [N] or NULL, C M x N in out_dtype F32 or BF16.  The sum is exact (32-bit integers;
  * hence K <= 131056) and its conversion, the scales and act are fp32.
- * Shape rules: K % 16 == 0; 1 <= N <= 2^20, M * N <= 2^40; columns between N and ldc are left as
+ * Shape rules: K % 16 == 0; 1 <= N <= 2^20, M * N <= 2^37; columns between N and ldc are left as
  * they are.  act: none, GELU (erf), GELU_TANH or RELU.
  * ------------------------------------------------------------------------ */
 typedef enum { CF_ACT_NONE = 0, CF_ACT_GELU = 1, CF_ACT_GELU_TANH = 2, CF_ACT_RELU = 3 } cf_act;

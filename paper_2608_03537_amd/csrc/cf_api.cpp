@@ -1131,7 +1131,7 @@ cf_status cf_gemm_i8(const cf_gemm_i8_args* a, void* hip_stream) {
       return fail(CF_ERR_STRUCT, "struct_size %zu != %zu", a->struct_size, sizeof(cf_gemm_i8_args));
     if (a->M < 0 || a->M > (int64_t)1 << 30 || a->N <= 0 || a->N > (int64_t)1 << 20)
       return fail(CF_ERR_SHAPE, "need 0 <= M <= 2^30, 0 < N <= 2^20");
-    if (a->M * a->N > (int64_t)1 << 40) return fail(CF_ERR_SHAPE, "M * N exceeds 2^40");
+    if (a->M * a->N > (int64_t)1 << 37) return fail(CF_ERR_SHAPE, "M * N exceeds 2^37");
     if (a->K <= 0 || a->K > kGemmI8MaxK || a->K % 16 != 0)
       return fail(CF_ERR_SHAPE, "K = %lld must be a multiple of 16 up to %lld", (long long)a->K, (long long)kGemmI8MaxK);
     if (a->out_dtype != CF_F32 && a->out_dtype != CF_BF16) return fail(CF_ERR_DTYPE, "out_dtype must be F32 or BF16");

@@ -362,20 +362,24 @@ hipError_t launch_big(const GemmI8Params& p, hipStream_t st) {
 //     4096 x 4096 x 4096     285  187  199  141  133  100   77 64.8
 //     8192 x 1024 x 1024      82   52   55   37   29   22 17.5   24
 struct Form {
-  int tm, tn, per;
+  int tm, tn, threads, per;
   double step, start;
   hipError_t (*launch)(const GemmI8Params&, hipStream_t);
 };
 constexpr int kCUs = 256;
+template <class S>
+constexpr Form tile_form(int per, double step, double start) {
+  return {S::TM, S::TN, S::NT, per, step, start, launch_tile<S>};
+}
 const Form kForms[] = {
-    {32, 32, kCUs, 0.09, 1.7, launch_tile<I8Tile<1, 1, 1, 1, 4, 4>>},
-    {64, 32, kCUs, 0.13, 1.9, launch_tile<I8Tile<2, 1, 1, 1, 4, 3>>},
-    {32, 64, kCUs, 0.12, 2.2, launch_tile<I8Tile<1, 2, 1, 1, 6, 2>>},
-    {64, 64, kCUs, 0.19, 2.6, launch_tile<I8Tile<2, 2, 1, 1, 4, 2>>},
-    {64, 128, kCUs, 0.40, 3.6, launch_tile<I8Tile<2, 2, 1, 2, 2, 3>>},
-    {128, 128, kCUs, 0.64, 4.6, launch_tile<I8Tile<2, 2, 2, 2, 1, 4>>},
-    {128, 128, 2 * kCUs, 1.06, 4.2, launch_tile<I8Tile<2, 2, 2, 2, 1, 2>>},
-    {kBigT, kBigT, kCUs, 0.88, 14.3, launch_big},
+    tile_form<I8Tile<1, 1, 1, 1, 4, 4>>(kCUs, 0.09, 1.7),
+    tile_form<I8Tile<2, 1, 1, 1, 4, 3>>(kCUs, 0.13, 1.9),
+    tile_form<I8Tile<1, 2, 1, 1, 6, 2>>(kCUs, 0.12, 2.2),
+    tile_form<I8Tile<2, 2, 1, 1, 4, 2>>(kCUs, 0.19, 2.6),
+    tile_form<I8Tile<2, 2, 1, 2, 2, 3>>(kCUs, 0.40, 3.6),
+    tile_form<I8Tile<2, 2, 2, 2, 1, 4>>(kCUs, 0.64, 4.6),
+    tile_form<I8Tile<2, 2, 2, 2, 1, 2>>(2 * kCUs, 1.06, 4.2),
+    {kBigT, kBigT, 512, kCUs, 0.88, 14.3, launch_big},
 };
 constexpr double kBigBusy = 0.62;   // added to the step of 256 x 256 tiles times the share of CUs at work (clocks)
 
@@ -386,7 +390,7 @@ const Form& choose_form(int64_t M, int64_t N, int64_t K) {
   for (const Form& f : kForms) {
     if (f.tm == kBigT && K < 256) continue;   // its loop needs two whole steps
     const int64_t wgs = ((M + f.tm - 1) / f.tm) * ((N + f.tn - 1) / f.tn), rounds = (wgs + f.per - 1) / f.per;
-    if (wgs > INT32_MAX / 2) continue;
+    if (wgs * f.threads > UINT32_MAX) continue;   // a grid has less than 2^32 threads; 128 x 128 tiles of M N <= 2^37 fit
     double step = f.step;
     if (f.tm == kBigT) step += kBigBusy * std::min(1.0, (double)wgs / kCUs);
     const double t = (double)rounds * (step * kt + f.start);

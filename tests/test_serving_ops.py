@@ -176,6 +176,20 @@ def test_gemm_i8_sizes(M, N, K):
 
 
 @gpu
+def test_gemm_i8_more_tokens_than_a_grid_of_small_tiles():
+    """2^29 + 40 rows and one column: tiles of 32 rows and 256 threads would be 2^32 threads."""
+    M = (1 << 29) + 40
+    A = torch.zeros((M, 16), dtype=torch.int8, device="cuda")
+    at = torch.tensor([0, 1, (1 << 28) + 3, (1 << 29) - 1, 1 << 29, M - 1], device="cuda")
+    A[at] = i8(gen(13), 6, 16)
+    B = torch.ones((1, 16), dtype=torch.int8, device="cuda")
+    C = cf.gemm_i8(A, B)                             # rows of 16 bytes: 8 GiB
+    want = A[at].to(F64).sum(-1, keepdim=True)
+    assert bool(((C[at].to(F64) - want).abs() <= 2.0 ** -8 * want.abs()).all())
+    assert int((C != 0).sum()) == int((want != 0).sum())
+
+
+@gpu
 @pytest.mark.parametrize("act", ["none", "gelu", "gelu_tanh", "relu"])
 @pytest.mark.parametrize("M", [1, 20, 90, 600])
 def test_gemm_i8_epilogues(M, act):
@@ -612,6 +626,7 @@ def gemm_args(**kw):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(struct_size=8), "CF_ERR_STRUCT"), (dict(M=-1), "CF_ERR_SHAPE"), (dict(N=0), "CF_ERR_SHAPE"),
+    (dict(M=(1 << 30) + 1), "CF_ERR_SHAPE"), (dict(M=1 << 30, N=129, ldc=136), "CF_ERR_SHAPE"),
     (dict(K=0), "CF_ERR_SHAPE"), (dict(K=40), "CF_ERR_SHAPE"), (dict(K=131072, lda=131072, ldb=131072), "CF_ERR_SHAPE"),
     (dict(A=None), "CF_ERR_NULL"), (dict(B=None), "CF_ERR_NULL"), (dict(C=None), "CF_ERR_NULL"), (dict(lda=48), "CF_ERR_LD"),
     (dict(ldc=96), "CF_ERR_LD"), (dict(lda=72), "CF_ERR_ALIGN"), (dict(ldc=100), "CF_ERR_ALIGN"),
