@@ -755,6 +755,9 @@ def gemm_i8(A, B, sa=None, sb=None, *, bias=None, act="none", out_dtype=None, ou
     return Cm
 
 
+_prefix_lock = threading.Lock()   # threads that share a stream share its workspace: a call's launches stay together
+
+
 def _prefix_workspace(torch, need, device, key):
     """workspace(need, device, kind="prefix") at less cost: cached per device and stream while nothing is captured."""
     if torch._C._cuda_isCurrentStreamCapturing():
@@ -816,11 +819,17 @@ def attention_prefix(Q, Kp, Vp, Ks=None, Vs=None, lens=None, *, causal=False, sc
                             None if Vs is None else Vs.data_ptr(), vs[0], vs[1], vs[2],
                             None if lens is None else lens.data_ptr(), 1 if causal else 0,
                             d ** -0.5 if scale is None else scale, O.data_ptr(), o[0], o[1], o[2])
-    if ws is None:
-        need = L.cf_attention_prefix_workspace(C.byref(a))
-        if need:
+    need = 0 if ws is not None else L.cf_attention_prefix_workspace(C.byref(a))
+    if need:
+        with _prefix_lock:
             ws = _prefix_workspace(torch, need, Q.device, (device, raw, "prefix"))
-    status = L.cf_attention_prefix(C.byref(a), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), raw)
+            status = L.cf_attention_prefix(C.byref(a), ws.data_ptr(), ws.numel(), raw)
+    elif ws is None:
+        status = L.cf_attention_prefix(C.byref(a), None, 0, raw)
+    else:
+        if ws.dtype is not torch.uint8 or not ws.is_contiguous() or ws.get_device() != device:
+            raise ValueError("ws: expected a contiguous uint8 tensor beside the other operands")
+        status = L.cf_attention_prefix(C.byref(a), ws.data_ptr(), ws.numel(), raw)
     if status:
         _check(status)
     return O

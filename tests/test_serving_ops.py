@@ -2,6 +2,7 @@
 8-bit codes, the int8 product, attention over a shared prefix, and a layer's run
 of all three.  u is fp32's half step; each bound counts roundings."""
 import math
+import threading
 
 import pytest
 import torch
@@ -529,6 +530,28 @@ def test_split_calls_captured_and_on_two_streams():
 
 
 @gpu
+def test_threads_share_a_stream():
+    """Calls in parts from two threads, on the same stream and so in one workspace."""
+    args = [prefix_inputs(gen(s), 6 + 3 * s, 8, 2, 1, 3000 + 500 * s, 200, 64) for s in (1, 2)]
+    want = [cf.attention_prefix(*a) for a in args]
+    torch.cuda.synchronize()
+    bad, stream = [], torch.cuda.Stream()
+
+    def run(i):
+        with torch.cuda.stream(stream):
+            for _ in range(200):
+                if not torch.equal(cf.attention_prefix(*args[i]), want[i]):
+                    bad.append(i)
+
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(60)
+    assert not bad and not any(t.is_alive() for t in threads)
+
+
+@gpu
 def test_one_workspace_for_calls_of_several_sizes():
     """The counters at its start are zero again after every call, whatever its size and cut."""
     g = gen(6)
@@ -704,6 +727,7 @@ def test_helpers_refuse():
         cf.gemm_i8(q[:, :40].contiguous(), q[:, :40].contiguous())
     a = torch.zeros((2, 4, 1, 64), dtype=BF16, device="cuda")
     k = torch.zeros((2, 8, 64), dtype=BF16, device="cuda")
-    for kw in (dict(Ks=a), dict(Ks=a, Vs=a), dict(lens=torch.zeros((2,), device="cuda")), dict(out=k)):
+    for kw in (dict(Ks=a), dict(Ks=a, Vs=a), dict(lens=torch.zeros((2,), device="cuda")), dict(out=k),
+               dict(ws=torch.zeros((1 << 18,), device="cuda")), dict(ws=torch.zeros((1 << 20,), dtype=torch.uint8))):
         with pytest.raises(ValueError):
             cf.attention_prefix(a, k, k, **kw)
