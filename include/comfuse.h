@@ -396,15 +396,16 @@ cf_status cf_gemm_i8(const cf_gemm_i8_args* a, void* hip_stream);
  *
  * Q, O: batch x H x Lq rows of d; Kp, Vp: Hk x P rows; Ks, Vs: batch x Hk x S
  * rows, all bf16, each matrix with its own strides (elements, multiples of 8; rows
- * have unit stride; an input's batch or head stride may be 0).  H is a multiple of Hk: query head h reads key head
+ * have unit stride; an input's batch or head stride may be 0,
+ * O's strides nest without overlap).  H is a multiple of Hk: query head h reads key head
  * h / (H / Hk).  d in {64, 128}.  P >= 0, S >= 0; Kp and Vp (Ks and Vs) may be
  * NULL where P (S) is 0.  lens: int32 [batch] in device memory, or NULL for S
  * everywhere; values outside [0, S] are clamped.  causal = 1: query i sees the
  * own keys j < lens[b] - (Lq - 1 - i) (the queries are the sequence's last Lq
  * tokens); the prefix is visible to all.  A query that sees no key gets O = 0.
  * Own rows at and behind lens[b] are not used, whatever they hold; an infinity or
- * NaN in a value row that causal hides from some queries of a call only reaches them too
- * (as 0 * NaN).  scale finite and > 0.  The softmax is exact (running maximum and sum in fp32);
+ * NaN in a value row that causal hides from some queries of a call only may reach those of
+ * them that see other keys (as 0 * NaN).  scale finite and > 0.  The softmax is exact (running maximum and sum in fp32);
  * P is rounded to bf16 for the second product, as in cf_b2bgemm.
  * Workspace: cf_attention_prefix_workspace() bytes (may be 0), 16-byte aligned:
  * CF_PREFIX_WS_HEADER_BYTES of arrival counters, then partial results.  Zero-fill

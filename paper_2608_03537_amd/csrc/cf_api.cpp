@@ -1182,8 +1182,17 @@ static cf_status check_rows(const char* name, const void* p, bool used, int64_t 
     return fail(CF_ERR_LD, "%s: row stride of %lld bytes or more", name, (long long)kMaxRowPitch);
   if ((nb > 1 && (sb < 0 || sb % 8 != 0)) || (nh > 1 && (sh < 0 || sh % 8 != 0)) || (rows > 1 && sl % 8 != 0))
     return fail(CF_ERR_ALIGN, "%s: strides must be non-negative multiples of 8 elements", name);
-  if (output && ((nb > 1 && sb < d) || (nh > 1 && sh < d)))
-    return fail(CF_ERR_LD, "%s: outputs overlap (a stride below d = %lld)", name, (long long)d);
+  if (output) {   // the dimensions nest: each one's stride is at least the extent of those with smaller strides
+    constexpr int64_t kFar = (int64_t)1 << 44;   // the extents stay below 2^62
+    std::pair<int64_t, int64_t> dims[3] = {{std::min(sb, kFar), nb}, {std::min(sh, kFar), nh}, {std::min(sl, kFar), rows}};
+    std::sort(dims, dims + 3);
+    int64_t extent = d;
+    for (const auto& [stride, n] : dims) {
+      if (n <= 1) continue;
+      if (stride < extent) return fail(CF_ERR_LD, "%s: outputs overlap (strides below the extent of what they step over)", name);
+      extent += stride * (n - 1);
+    }
+  }
   return CF_OK;
 }
 

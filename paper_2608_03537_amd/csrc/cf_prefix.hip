@@ -54,12 +54,14 @@ __device__ __forceinline__ int own_seen(const PrefixParams& p, int len, int i) {
   return p.causal ? max(0, len - (p.Lq - 1 - i)) : len;
 }
 
-// 8 d of the output row of query i of head h: o / l, or 0 where the row sees no key.
+// 8 d of the output row of query i of head h: o / l, or 0 where the row sees no key (o may be NaN
+// there: 0 times what a value row that it does not see holds).
 __device__ __forceinline__ void store_row(const PrefixParams& p, int b, int h, int i, int d0, const float (&o)[8], float l,
                                           bool any) {
-  const float inv = any ? 1.0f / l : 0.0f;
-  const u32x4_t w = {pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv),
-                     pack_bf16x2(o[4] * inv, o[5] * inv), pack_bf16x2(o[6] * inv, o[7] * inv)};
+  const float inv = 1.0f / l;
+  u32x4_t w = {pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv),
+               pack_bf16x2(o[4] * inv, o[5] * inv), pack_bf16x2(o[6] * inv, o[7] * inv)};
+  if (!any) w = u32x4_t{};
   __builtin_nontemporal_store(w, reinterpret_cast<u32x4_t*>(p.O + b * p.o_b + h * p.o_h + i * p.o_l + d0));
 }
 
@@ -482,14 +484,13 @@ __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb
   }
   if constexpr (JOIN) {
     static_assert(KIND == WHOLE && QG == 1, "the parts of one (sequence, key head)");
-    // Count the arrival; the last workgroup joins (the counter goes back to 0, ready for the next call).
+    // Count the arrival; the last workgroup joins.
     wait_vmcnt<0>();          // this wave's partial results are written
     __syncthreads();          // ... and every wave's; the LDS is free
     int* const last = reinterpret_cast<int*>(smem + 16384);   // behind what join_rows uses
     if (tid == 0) {
       unsigned* const c = count + hk * p.B + b;
-      *last = __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)(slots - 1);
-      if (*last) __hip_atomic_store(c, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      *last = atomicInc(c, (unsigned)(slots - 1)) == (unsigned)(slots - 1);   // the last one wraps it to 0
     }
     __syncthreads();
     if (*last) join_rows<D>(p, smem, b, hk, slots);

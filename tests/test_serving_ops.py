@@ -334,6 +334,19 @@ def test_prefix_rows_without_keys_and_stale_cache(d, Lq, S):
 
 
 @gpu
+@pytest.mark.parametrize("d,H,Lq", [(64, 4, 5), (128, 8, 3), (64, 16, 40)])
+def test_prefix_rows_without_keys_beside_nan_values(d, H, Lq):
+    """A query that sees no key gets 0, also where the keys of the later queries hold values that are not finite."""
+    Q, Kp, Vp, Ks, Vs = prefix_inputs(gen(14), 3, H, 2, Lq, 0, 300, d)
+    lens = torch.tensor([1, 0, 2], dtype=torch.int32, device="cuda")
+    Vs[0, :, 0] = float("nan")
+    Vs[2, :, 1] = math.inf
+    O = cf.attention_prefix(Q, Kp, Vp, Ks, Vs, lens, causal=True)
+    assert not O[0, :, :-1].any() and not O[1].any() and not O[2, :, :-2].any()
+    assert bool(O[0, :, -1].isnan().all()) and not bool(O[2, :, -1].isfinite().any())
+
+
+@gpu
 @pytest.mark.parametrize("Lq", [1, 48])
 def test_prefix_special_scores(Lq):
     """Infinite values stay in their own column; rows whose scores are all -infinity and scores with a
@@ -678,7 +691,9 @@ def prefix_args(**kw):
     (dict(Vs=None), "CF_ERR_NULL"), (dict(Ks=C_ + 8), "CF_ERR_ALIGN"), (dict(kp_l=60), "CF_ERR_LD"),
     (dict(ks_l=68), "CF_ERR_ALIGN"), (dict(vs_h=1004), "CF_ERR_ALIGN"), (dict(q_b=-256), "CF_ERR_ALIGN"),
     (dict(vp_l=1 << 22), "CF_ERR_LD"), (dict(lens=E_ + 2), "CF_ERR_ALIGN"), (dict(O=A_), "CF_ERR_ALIAS"),
-    (dict(O=C_), "CF_ERR_ALIAS"), (dict(o_b=0), "CF_ERR_LD"), (dict(o_h=0), "CF_ERR_LD")])
+    (dict(O=C_), "CF_ERR_ALIAS"), (dict(o_b=0), "CF_ERR_LD"), (dict(o_h=0), "CF_ERR_LD"),
+    (dict(o_b=64), "CF_ERR_LD"), (dict(o_b=192), "CF_ERR_LD"), (dict(Lq=3, o_l=64), "CF_ERR_LD"),
+    (dict(Lq=3, o_l=256, o_b=512), "CF_ERR_LD")])
 def test_prefix_refuses(kw, status):
     assert cf.STATUS[cf.cf_attention_prefix(prefix_args(**kw), None, 0, None)] == status, cf.cf_last_error()
 
