@@ -706,6 +706,13 @@ def test_empty_calls_do_nothing():
         assert cf.cf_attention_prefix_workspace(prefix_args(**kw)) == 0
 
 
+def test_packed_arguments():
+    """The helpers pack their arguments as the structures lay them out."""
+    for t, pack in ((cf.RmsnormQuantArgs, cf._RMSNORM_QUANT), (cf.GemmI8Args, cf._GEMM_I8), (cf.AttentionPrefixArgs, cf._PREFIX)):
+        values = [i + 0.5 if f is cf.C.c_float else 3 * i + 1 for i, (_, f) in enumerate(t._fields_)]
+        assert bytes(t(*values)) == pack.pack(*values)
+
+
 def test_helpers_refuse_host_tensors():
     x = torch.zeros((4, 16), dtype=BF16)
     with pytest.raises(ValueError, match="GPU"):
