@@ -170,7 +170,8 @@ __device__ __forceinline__ void read_blocks(u32x4_t (&f)[NB][4], const uint32_t 
   else read_w_half_nk<0>(f[0], a);
 }
 
-template <class S>
+// CUT: K ends inside a step (a kernel of its own: looking for that step costs whole K 0.3 us).
+template <class S, bool CUT>
 __global__ __launch_bounds__(S::NT) void gemm_i8_tile_kernel(GemmI8Params p) {
   __shared__ __attribute__((aligned(16))) char smem[S::LDS];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -182,7 +183,8 @@ __global__ __launch_bounds__(S::NT) void gemm_i8_tile_kernel(GemmI8Params p) {
   TileScales<S::TM, S::TN, S::NT, true> sc;
   sc.load(p, m0, n0);
   char* const ring = smem + grp * S::RING;
-  const int KT = p.K / 128, steps = grp < KT ? (KT - grp - 1) / S::KW + 1 : 0;   // whole steps; those of this group
+  const int KT = (p.K + 127) / 128, steps = grp < KT ? (KT - grp - 1) / S::KW + 1 : 0;   // steps; those of this group
+  const int rem = p.K % 128, cut = (KT - 1) % S::KW == grp ? steps - 1 : -1;      // CUT: the group's step that K ends in
 
   // Stage rows 0 .. TM - 1 are tokens, then TN channels; load i of a wave fills rows
   // 8 (i GW + gw) .. + 7.  Rows past M and N are clamped (they feed nothing that is stored).
@@ -194,8 +196,20 @@ __global__ __launch_bounds__(S::NT) void gemm_i8_tile_kernel(GemmI8Params p) {
                           : reinterpret_cast<const char*>(p.B) + (int64_t)min(n0 + row - S::TM, p.N - 1) * p.ldb) +
              ch * 16 + grp * 128;
   }
-  auto load = [&](int s, int i) {   // load i of the group's step s, into stage s % NS
-    dma16(src[i] + (int64_t)s * (S::KW * 128), ring + s % S::NS * S::STAGE + gw * 1024 + i * S::GW * 1024);
+  auto load = [&](int s, auto cut_t) {   // the group's step s, into stage s % NS
+#pragma unroll
+    for (int i = 0; i < S::LPW; ++i) {
+      const char* from = src[i] + (int64_t)s * (S::KW * 128);
+      if constexpr (decltype(cut_t)::value) {   // chunks behind K: the step's first one, cleared when read
+        const int ch = ((lane & 7) ^ ((4 * (i * S::GW + gw) + (lane >> 4)) & 7)) * 16;
+        if (ch >= rem) from -= ch;
+      }
+      dma16(from, ring + s % S::NS * S::STAGE + gw * 1024 + i * S::GW * 1024);
+    }
+  };
+  auto load_step = [&](int s) {
+    if (CUT && s == cut) load(s, std::true_type{});
+    else load(s, std::false_type{});
   };
   const uint32_t s0 =
       (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)smem) + grp * S::RING;
@@ -216,10 +230,7 @@ __global__ __launch_bounds__(S::NT) void gemm_i8_tile_kernel(GemmI8Params p) {
   };
 #pragma unroll
   for (int s = 0; s < S::NS - 1; ++s)
-    if (s < steps) {
-#pragma unroll
-      for (int i = 0; i < S::LPW; ++i) load(s, i);
-    }
+    if (s < steps) load_step(s);
   const int all = (KT + S::KW - 1) / S::KW;   // every group passes every barrier
   for (int s = 0; s < all; ++s) {
     if (s + S::NS - 2 < steps) wait_vmcnt<S::LPW*(S::NS - 2)>();
@@ -232,37 +243,22 @@ __global__ __launch_bounds__(S::NT) void gemm_i8_tile_kernel(GemmI8Params p) {
     // The loads of a later step go between the MFMAs: in front of the reads they would hold them up.
     read_blocks<S::BM>(xf, x);
     read_blocks<S::BN>(wf, w);
+    if (CUT && s == cut) {   // one operand's zeros do for both
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+        if (ks * 32 + lg * 16 >= rem)
+#pragma unroll
+          for (int b = 0; b < S::BM; ++b) xf[b][ks] = u32x4_t{};
+    }
     __builtin_amdgcn_sched_barrier(0);
     mma(0);
     __builtin_amdgcn_sched_barrier(0);
-    if (s + S::NS - 1 < steps) {
-#pragma unroll
-      for (int i = 0; i < S::LPW; ++i) load(s + S::NS - 1, i);
-    }
+    if (s + S::NS - 1 < steps) load_step(s + S::NS - 1);
     __builtin_amdgcn_sched_barrier(0);
     mma(1);
     mma(2);
     mma(3);
     __builtin_amdgcn_sched_barrier(0);
-  }
-  // k behind the last whole step, straight from memory; the last group takes it
-  if (grp == S::KW - 1 && KT * 128 < p.K) {
-    auto frag = [&](const int8_t* row, int ks) {
-      const int k = KT * 128 + ks * 32 + lg * 16;
-      u32x4_t v = {};
-      if (k < p.K) v = gload16(row + k);
-      return v;
-    };
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-#pragma unroll
-      for (int b = 0; b < S::BM; ++b)
-        xf[b][ks] = frag(p.A + (int64_t)min(m0 + (wm * S::BM + b) * 32 + lr, p.M - 1) * p.lda, ks);
-#pragma unroll
-      for (int b = 0; b < S::BN; ++b)
-        wf[b][ks] = frag(p.B + (int64_t)min(n0 + (wn * S::BN + b) * 32 + lr, p.N - 1) * p.ldb, ks);
-      mma(ks);
-    }
   }
   __syncthreads();
   constexpr int PITCH = S::TN * 4 + 16;
@@ -340,7 +336,8 @@ void gemm_i8_big_kernel(GemmI8Params p) {
 template <class S>
 hipError_t launch_tile(const GemmI8Params& p, hipStream_t st) {
   const int64_t wgs = (int64_t)((p.M + S::TM - 1) / S::TM) * ((p.N + S::TN - 1) / S::TN);
-  hipLaunchKernelGGL((gemm_i8_tile_kernel<S>), dim3((unsigned)wgs), dim3(S::NT), 0, st, p);
+  if (p.K % 128 == 0) hipLaunchKernelGGL((gemm_i8_tile_kernel<S, false>), dim3((unsigned)wgs), dim3(S::NT), 0, st, p);
+  else hipLaunchKernelGGL((gemm_i8_tile_kernel<S, true>), dim3((unsigned)wgs), dim3(S::NT), 0, st, p);
   return hipGetLastError();
 }
 hipError_t launch_big(const GemmI8Params& p, hipStream_t st) {
