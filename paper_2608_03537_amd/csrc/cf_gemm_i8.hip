@@ -6,14 +6,17 @@
 //
 // An MFMA covers 32 bytes of k per operand row in 32 cycles, as the bf16 one does,
 // so in bytes these loops are those of a bf16 product with half the k.  Tiles:
-//   wave tiles   32 x 32 to 64 x 64, a ring of LDS stages per wave (or per pair of
-//                waves); the waves or pairs of a workgroup split K and their sums meet in LDS.
-//   128 x 128    four waves of 64 x 64 share a ring, one or two workgroups a CU.
+//   32 x 32 to 64 x 64   a wave each, with a ring of LDS stages of its own; the waves of a workgroup
+//                split K and their sums meet in LDS.
+//   64 x 128, 128 x 128  four waves share a tile and a ring; two such groups split K, one multiplying while
+//                the other reads (1024 x 4096 x 4096 24.5 -> 22.7 us against one group of four waves,
+//                512 x 4096 x 4096 17.7 -> 15.8 against two pairs, all in step).
+//   128 x 128    four waves, two workgroups a CU, where there are more than 256 tiles.
 //   256 x 256    big_product in cf_gemm_big.h.
-// What bounds them: a CU's direct loads into LDS take about 32 cycles per KB (64 x 64
-// tiles reach 60 GB/s a CU with all CUs busy), so a tile's time is its operand bytes
-// over that rate, and few tokens are the weights' stream.  256 x 256 tiles run
-// 16384 x 4096 x 4096 in 262 us, 2.1 POP/s; with operands of zeros, whose MFMAs draw
+// What bounds them: a CU's direct loads into LDS reach 90 to 100 GB/s with all CUs busy, so few tokens
+// are the weights' stream.  In between it is how well a step's loads, LDS reads and MFMAs overlap (1024 x 4096
+// x 4096 on 128 x 128 tiles: 13, 9 and 9 us by themselves, 18 together, and 5 of start and output).  256 x 256
+// tiles run 16384 x 4096 x 4096 in 247 us, 2.2 POP/s; with operands of zeros, whose MFMAs draw
 // less power, in 184: the clock that full power leaves bounds them.  kForms has
 // the measurements of all.  A form that loads fragments straight into registers
 // was slower from 16 tokens on (48 x 12288 x 4096 29 us against 12.8: rows of a power
@@ -149,11 +152,12 @@ __device__ __forceinline__ void finish_tile(const GemmI8Params& p, const TileSca
 // ---------------------------------------------------------------------------
 // Tile.  A group of WM x WN waves (32 BM tokens x 32 BN channels each) shares a ring of
 // NS stages of 128 bytes of k; KW groups take the stages in turn.  A group of one wave
-// needs no barrier until the end.  The 16-byte chunk ch of row r of
-// a stage sits at position ch ^ ((r >> 1) & 7), as in big_product.
+// needs no barrier until the end.  ALT: two groups of four waves that read and multiply by turns
+// (below).  The 16-byte chunk ch of row r of a stage sits at position ch ^ ((r >> 1) & 7), as in big_product.
 // ---------------------------------------------------------------------------
-template <int BM_, int BN_, int WM_, int WN_, int KW_, int NS_>
+template <int BM_, int BN_, int WM_, int WN_, int KW_, int NS_, bool ALT_ = false>
 struct I8Tile {
+  static constexpr bool ALT = ALT_;
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KW = KW_, NS = NS_;
   static constexpr int GW = WM * WN, NW = GW * KW, NT = 64 * NW;
   static constexpr int TM = 32 * BM * WM, TN = 32 * BN * WN, STAGE = (TM + TN) * 128;
@@ -161,6 +165,7 @@ struct I8Tile {
   static constexpr int LDS = KW * RING > OUT ? KW * RING : OUT;
   static constexpr int LPW = (TM + TN) / 8 / GW;   // wave-wide loads of a stage per wave
   static_assert(LDS <= 160 * 1024 && LPW * NS < 64, "LDS budget, vmcnt range");
+  static_assert(!ALT || (KW == 2 && NW == 8), "two waves a SIMD");
 };
 
 // Fragments of a stage's four k steps of NB 32-row blocks at a[0..3], complete.
@@ -196,20 +201,18 @@ __global__ __launch_bounds__(S::NT) void gemm_i8_tile_kernel(GemmI8Params p) {
                           : reinterpret_cast<const char*>(p.B) + (int64_t)min(n0 + row - S::TM, p.N - 1) * p.ldb) +
              ch * 16 + grp * 128;
   }
-  auto load = [&](int s, auto cut_t) {   // the group's step s, into stage s % NS
+  // Loads i0 .. i1 - 1 of the group's step s, into stage s % NS; of the step that K ends in, a lane whose
+  // chunk lies behind K takes the step's first one (cleared when read).
+  auto load = [&](int s, int i0, int i1) {
 #pragma unroll
-    for (int i = 0; i < S::LPW; ++i) {
+    for (int i = i0; i < i1; ++i) {
       const char* from = src[i] + (int64_t)s * (S::KW * 128);
-      if constexpr (decltype(cut_t)::value) {   // chunks behind K: the step's first one, cleared when read
+      if (CUT && s == cut) {
         const int ch = ((lane & 7) ^ ((4 * (i * S::GW + gw) + (lane >> 4)) & 7)) * 16;
         if (ch >= rem) from -= ch;
       }
       dma16(from, ring + s % S::NS * S::STAGE + gw * 1024 + i * S::GW * 1024);
     }
-  };
-  auto load_step = [&](int s) {
-    if (CUT && s == cut) load(s, std::true_type{});
-    else load(s, std::false_type{});
   };
   const uint32_t s0 =
       (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)smem) + grp * S::RING;
@@ -228,19 +231,10 @@ __global__ __launch_bounds__(S::NT) void gemm_i8_tile_kernel(GemmI8Params p) {
 #pragma unroll
       for (int bn = 0; bn < S::BN; ++bn) MmaI8::run(acc[bm][bn], wf[bn][ks], xf[bm][ks]);
   };
-#pragma unroll
-  for (int s = 0; s < S::NS - 1; ++s)
-    if (s < steps) load_step(s);
-  const int all = (KT + S::KW - 1) / S::KW;   // every group passes every barrier
-  for (int s = 0; s < all; ++s) {
-    if (s + S::NS - 2 < steps) wait_vmcnt<S::LPW*(S::NS - 2)>();
-    else wait_vmcnt<0>();
-    if constexpr (S::GW > 1) lds_barrier();   // every wave's loads of step s are in, and step s - 1 has been read
-    if (s >= steps) continue;
+  auto read = [&](int s) {
     const uint32_t at = s % S::NS * S::STAGE;
     const uint32_t x[4] = {xa[0] + at, xa[1] + at, xa[2] + at, xa[3] + at};
     const uint32_t w[4] = {wa[0] + at, wa[1] + at, wa[2] + at, wa[3] + at};
-    // The loads of a later step go between the MFMAs: in front of the reads they would hold them up.
     read_blocks<S::BM>(xf, x);
     read_blocks<S::BN>(wf, w);
     if (CUT && s == cut) {   // one operand's zeros do for both
@@ -250,15 +244,53 @@ __global__ __launch_bounds__(S::NT) void gemm_i8_tile_kernel(GemmI8Params p) {
 #pragma unroll
           for (int b = 0; b < S::BM; ++b) xf[b][ks] = u32x4_t{};
     }
+  };
+  // The MFMAs of a step; the loads of a later one go between them (in front of the reads they would hold
+  // them up): a wave on its own issues them at once, waves that share a step in three parts, since together they
+  // fill the load path (512 x 4096 x 4096 on 64 x 128 tiles without ALT 18.2 -> 16.8 us; 64 x 64 11.8 -> 12.2).
+  auto multiply = [&](int later) {
+    constexpr int PARTS = S::GW > 1 ? 3 : 1;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      __builtin_amdgcn_sched_barrier(0);
+      mma(ks);
+      __builtin_amdgcn_sched_barrier(0);
+      if (ks < PARTS && later < steps) load(later, ks * S::LPW / PARTS, (ks + 1) * S::LPW / PARTS);
+    }
     __builtin_amdgcn_sched_barrier(0);
-    mma(0);
-    __builtin_amdgcn_sched_barrier(0);
-    if (s + S::NS - 1 < steps) load_step(s + S::NS - 1);
-    __builtin_amdgcn_sched_barrier(0);
-    mma(1);
-    mma(2);
-    mma(3);
-    __builtin_amdgcn_sched_barrier(0);
+  };
+  const int all = (KT + S::KW - 1) / S::KW;   // every group passes every barrier
+  constexpr int FIRST = S::ALT ? S::NS : S::NS - 1;   // steps loaded ahead
+#pragma unroll
+  for (int s = 0; s < FIRST; ++s)
+    if (s < steps) load(s, 0, S::LPW);
+  if constexpr (S::ALT) {
+    // Read and MFMA sections with a barrier behind each; group 1 is one section behind, and its waves share the
+    // SIMDs with those of group 0, so one of the two multiplies while the other reads.  In front of the
+    // barrier that ends a read section a wave waits for its loads of the next step (one section later the
+    // group reads them); a step's stage is free once that barrier is passed.
+    if (S::NS <= steps) wait_vmcnt<S::LPW*(S::NS - 1)>();
+    else wait_vmcnt<0>();
+    lds_barrier();
+    if (grp == 1) lds_barrier();
+    for (int s = 0; s < all; ++s) {
+      if (s < steps) read(s);
+      if (s + S::NS - 1 < steps) wait_vmcnt<S::LPW*(S::NS - 2)>();
+      else wait_vmcnt<0>();
+      lds_barrier();
+      if (s < steps) multiply(s + S::NS);
+      lds_barrier();
+    }
+    if (grp == 0) lds_barrier();
+  } else {
+    for (int s = 0; s < all; ++s) {
+      if (s + S::NS - 2 < steps) wait_vmcnt<S::LPW*(S::NS - 2)>();
+      else wait_vmcnt<0>();
+      if constexpr (S::GW > 1) lds_barrier();   // every wave's loads of step s are in, and step s - 1 has been read
+      if (s >= steps) continue;
+      read(s);
+      multiply(s + S::NS - 1);
+    }
   }
   __syncthreads();
   constexpr int PITCH = S::TN * 4 + 16;
@@ -348,16 +380,17 @@ hipError_t launch_big(const GemmI8Params& p, hipStream_t st) {
 
 // The tiles and their estimated time: rounds of `per` workgroups, each `step` us for
 // every 128 bytes of k and `start` us besides.  Fitted to M x N of 1 to 16384 with K of 512
-// to 16384; for instance (us, in this order, - not run):
-//     1 x 4096 x 4096        5.8  7.1  7.6  9.8   16   21    -    -
-//     16 x 12288 x 4096     12.5 14.0 11.0 11.6   16   22    -    -
-//     48 x 12288 x 4096     16.9 15.2 15.6 12.8   18   23    -    -
-//     128 x 4096 x 4096     11.2  8.2  8.5 10.7   17   24   30   42
-//     512 x 4096 x 4096       38   25   27 20.0 18.2   24   30   45
-//     1024 x 4096 x 4096      73   49   52   37   35 25.9   31   45
-//     2048 x 4096 x 4096     144   95  101   73   68   51 38.8   46
-//     4096 x 4096 x 4096     285  187  199  141  133  100   77 64.8
-//     8192 x 1024 x 1024      82   52   55   37   29   22 17.5   24
+// to 16384; for instance (us, in this order):
+//     1 x 4096 x 4096        5.9  7.2  7.4  9.8   13   15   27   36
+//     16 x 12288 x 4096     12.3 14.0 10.7 11.5   13   16   28   36
+//     48 x 12288 x 4096     15.6 14.3 14.6 12.0 13.5   16   28   37
+//     128 x 4096 x 4096     11.2  8.4  8.6 10.7   14   17   30   38
+//     512 x 4096 x 4096       38   27   26 19.8 15.8   18   30   42
+//     1024 x 4096 x 4096      73   49   49   36   30 22.7   31   43
+//     2048 x 4096 x 4096     141   94   95   69   57   43 37.7   48
+//     4096 x 4096 x 4096     282  184  187  135  111   82   75 63.9
+//     8192 x 1024 x 1024      77   51   49   34   25   23 16.0   22
+// Over 36 such calls the form that the estimate takes is 0.7 % slower than the best one on average, 16 % at worst.
 struct Form {
   int tm, tn, threads, per;
   double step, start;
@@ -369,16 +402,16 @@ constexpr Form tile_form(int per, double step, double start) {
   return {S::TM, S::TN, S::NT, per, step, start, launch_tile<S>};
 }
 const Form kForms[] = {
-    tile_form<I8Tile<1, 1, 1, 1, 4, 4>>(kCUs, 0.09, 1.7),
-    tile_form<I8Tile<2, 1, 1, 1, 4, 3>>(kCUs, 0.13, 1.9),
-    tile_form<I8Tile<1, 2, 1, 1, 6, 2>>(kCUs, 0.12, 2.2),
-    tile_form<I8Tile<2, 2, 1, 1, 4, 2>>(kCUs, 0.19, 2.6),
-    tile_form<I8Tile<2, 2, 1, 2, 2, 3>>(kCUs, 0.40, 3.6),
-    tile_form<I8Tile<2, 2, 2, 2, 1, 4>>(kCUs, 0.64, 4.6),
-    tile_form<I8Tile<2, 2, 2, 2, 1, 2>>(2 * kCUs, 1.06, 4.2),
-    {kBigT, kBigT, 512, kCUs, 0.88, 14.3, launch_big},
+    tile_form<I8Tile<1, 1, 1, 1, 4, 4>>(kCUs, 0.08, 2.2),
+    tile_form<I8Tile<2, 1, 1, 1, 4, 3>>(kCUs, 0.11, 2.8),
+    tile_form<I8Tile<1, 2, 1, 1, 6, 2>>(kCUs, 0.12, 2.4),
+    tile_form<I8Tile<2, 2, 1, 1, 4, 2>>(kCUs, 0.20, 2.9),
+    tile_form<I8Tile<1, 2, 2, 2, 2, 3, true>>(kCUs, 0.31, 3.5),
+    tile_form<I8Tile<2, 2, 2, 2, 2, 2, true>>(kCUs, 0.43, 4.7),
+    tile_form<I8Tile<2, 2, 2, 2, 1, 2>>(2 * kCUs, 1.02, 4.2),
+    {kBigT, kBigT, 512, kCUs, 0.88, 10.5, launch_big},
 };
-constexpr double kBigBusy = 0.62;   // added to the step of 256 x 256 tiles times the share of CUs at work (clocks)
+constexpr double kBigBusy = 0.65;   // added to the step of 256 x 256 tiles times the share of CUs at work (clocks)
 
 const Form& choose_form(int64_t M, int64_t N, int64_t K) {
   const Form* best = nullptr;
