@@ -32,6 +32,7 @@ namespace {
 
 typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4_t;
 typedef __attribute__((__vector_size__(16 * sizeof(int)))) int i32x16_t;
+typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2_t;
 
 // D (32 n x 32 m) += W (32 n x 32 k) X (32 k x 32 m): lane l gives 16 k of row l % 32 of
 // either operand, k group l / 32; layout of D as for the bf16 atom (acc_row).
@@ -128,13 +129,22 @@ __device__ __forceinline__ void finish_tile(const GemmI8Params& p, const TileSca
                              pack_bf16x2(y[6], y[7])};
           __builtin_nontemporal_store(w, reinterpret_cast<u32x4_t*>(reinterpret_cast<bf16_t*>(p.C) + at));
         }
+      } else if (p.c_f32) {   // 4, 2 and 1 columns by the bits of `left` (one by one: 1699 x 5327 x 896 24.4 us, so 21.7)
+        float* c = reinterpret_cast<float*>(p.C) + at;
+        const bool h = left & 4;
+        if (h) *reinterpret_cast<f32x4_t*>(c) = f32x4_t{y[0], y[1], y[2], y[3]};
+        c += left & 4;
+        const float z[3] = {h ? y[4] : y[0], h ? y[5] : y[1], h ? y[6] : y[2]};
+        if (left & 2) *reinterpret_cast<f32x2_t*>(c) = f32x2_t{z[0], z[1]};
+        if (left & 1) c[left & 2] = left & 2 ? z[2] : z[0];
       } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if (e >= left) break;
-          if (p.c_f32) reinterpret_cast<float*>(p.C)[at + e] = y[e];
-          else reinterpret_cast<bf16_t*>(p.C)[at + e] = (bf16_t)pack_bf16x2(y[e], 0.0f);
-        }
+        bf16_t* c = reinterpret_cast<bf16_t*>(p.C) + at;
+        const bool h = left & 4;
+        if (h) *reinterpret_cast<u32x2_t*>(c) = u32x2_t{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+        c += left & 4;
+        const uint32_t z[2] = {pack_bf16x2(h ? y[4] : y[0], h ? y[5] : y[1]), pack_bf16x2(h ? y[6] : y[2], 0.0f)};
+        if (left & 2) *reinterpret_cast<uint32_t*>(c) = z[0];
+        if (left & 1) c[left & 2] = (bf16_t)(left & 2 ? z[1] : z[0]);
       }
     };
     const int r0 = tid / Sc::CPR;
