@@ -626,7 +626,7 @@ def _rows(torch, M, N, dtype, device, size):
     if N * size % 16 == 0:
         return torch.empty(M, N, dtype=dtype, device=device), N
     ld = -(-N * size // 16) * 16 // size
-    return torch.empty(M, ld, dtype=dtype, device=device)[:, :N], ld
+    return torch.empty_strided((M, N), (ld, 1), dtype=dtype, device=device), ld
 
 
 def _row_ld(t, M, N, size):

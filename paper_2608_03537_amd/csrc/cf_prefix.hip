@@ -608,8 +608,9 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(PrefixParams p, int s
 struct PrefixPlan {
   int pq, oq;   // 32-row waves of a workgroup: prefix parts, own parts or whole rows
   int np, ns;   // split: parts of the prefix and of the own keys.  ns = 0: whole rows in np parts
+  bool few;     // at most 32 rows of a (sequence, key head)
   int slots() const { return ns > 0 ? np + ns : np > 1 ? np : 0; }
-  bool joined() const { return ns == 0 && np > 1 && oq == 1; }   // by the last workgroup, without a second launch
+  bool joined() const { return ns == 0 && np > 1 && few; }   // by the last workgroup, without a second launch
 };
 constexpr size_t kCounterBytes = CF_PREFIX_WS_HEADER_BYTES;   // the counters of (sequence, key head); the partial results follow
 constexpr int kCUs = 256, kMaxParts = 32, kMaxOwnParts = 8;
@@ -619,19 +620,22 @@ int64_t row_blocks(int64_t rows, int qg) { return ceil_div(rows, 32 * qg); }
 
 // The estimate (us).  A step is one key block of every group of a workgroup: alone on its CU,
 // and where two workgroups share the CU; a workgroup's start and merge; the join, and
-// a partial result's write and read.  Fitted to 80 calls of 1 to 64 sequences, 1 to 500 queries and
-// 64 to 16000 prefix keys, each measured in 10 to 40 cuts: the cut that the estimate takes is
-// 2 % slower on the device than the best one on average, 14 % at worst.  Some of them (us: whole rows; the best split):
+// a partial result's write and read.  Fitted to 400 calls of 1 to 64 sequences, 1 to 500 queries and
+// 64 to 16000 prefix keys, each measured in up to 80 cuts, at the time that a caller in Python sees (a second
+// launch costs the host 4 us): the cut that the estimate takes is 2 % slower than the best one on
+// average, 25 % at worst; with powers of two only 3 %, with 128 rows a workgroup for all calls
+// of more than 32 rows 4 %.  Some of them (us: whole rows; the best split):
 //     4 x 8 heads, 1 query, 128 + 64 keys, d 64                5.6     8.5
 //     64 x 8 heads, 1 query, 512 + 128, d 64                  10.7    12.5
 //     16 x 16 heads, 5 queries, 4095 + 333, d 64              22.6    15.5 (4 + 1 parts)
 //     1 x 32 heads of 8, 1 query, 8192 + 512, d 128             67    13.4 (16 + 2)
 //     64 x 32 heads of 8, 1 query, 8192 + 512, d 128           118    39.8 (8 + 2)
-constexpr double kStepFew = 0.95, kStepFew2 = 1.9, kStepMany = 1.6, kStepMany2 = 2.35;   // QG 1, QG 4; 2: two a CU
-constexpr double kStepMany64 = 0.62;              // QG 4 steps at d = 64 by those at d = 128
-constexpr double kStart = 6.6, kPartial = 1.9e-6, kStream = 4.8e6;   // kStream: bytes a us
+constexpr double kStepFew = 0.95, kStepFew2 = 1.88, kStepMany = 1.35, kStepMany2 = 2.13;   // QG 1, QG 4; 2: two a CU
+constexpr double kStepMany64 = 0.59;              // QG 4 steps at d = 64 by those at d = 128
+constexpr double kStart = 6.5, kPartial = 1.8e-6, kStream = 5.8e6;   // kStream: bytes a us
 constexpr double kJoin = 4.8;                     // the joining launch, on the device and on the host
-constexpr double kJoinBy8 = 1.0, kJoinOwn = 2.3;  // joined by the last workgroup: every 8 rows, and besides
+constexpr double kJoinBy8 = 1.44, kJoinOwn = 1.5; // joined by the last workgroup: every 8 rows, and besides
+constexpr double kUneven = 1.3;                   // what workgroups of two kinds leave unused
 
 struct Task {   // one kind of workgroup of a launch
   double steps, wgs;
@@ -641,48 +645,63 @@ struct Task {   // one kind of workgroup of a launch
   }
 };
 
+// Calls f with the numbers of parts from 1 to `most` that are tried: powers of two, and `fill` and
+// `fill2` (those that just occupy the CUs once and twice).
+template <typename F>
+void try_parts(int64_t most, int64_t fill, int64_t fill2, F&& f) {
+  for (int64_t n = 1; n <= most; n *= 2) f((int)n);
+  for (int64_t n : {fill, fill2})
+    if (n >= 3 && n <= most && (n & (n - 1)) != 0) f((int)n);
+}
+
 PrefixPlan make_plan(const PrefixParams& p) {
   const int64_t R = (int64_t)(p.H / p.Hk) * p.Lq, Rall = p.B * R, rows = p.Hk * Rall;
-  PrefixPlan best{1, R <= 32 ? 1 : 4, 1, 0};
+  PrefixPlan best{1, R <= 32 ? 1 : 4, 1, 0, R <= 32};
   auto blocks = [&](int64_t n, int qg) { return ceil_div(n, qg == 1 ? 4096 / p.d : 64); };   // of keys
   auto task = [&](int64_t nb, int parts, int64_t wgs, int qg) {
     const double scale = qg == 4 && p.d == 64 ? kStepMany64 : 1.0;
     return Task{(double)ceil_div(ceil_div(nb, parts), 4 / qg) * scale, (double)wgs * parts, qg};
   };
-  const int64_t wo = row_blocks(R, best.oq) * p.B * p.Hk;
   const double stream = 4.0 * p.Hk * p.d * (p.P + 0.8 * p.B * p.S) / kStream;
   const double part = kPartial * (double)rows * p.d;
-  const int64_t most = ((int64_t)1 << 30) / std::max<int64_t>(1, rows * (p.d + 2) * 4);   // parts in 1 GiB
+  const int64_t gib = ((int64_t)1 << 30) / std::max<int64_t>(1, rows * (p.d + 2) * 4);   // parts in 1 GiB
   double least = 0;
-  auto take = [&](double us, int pq, int np, int ns) {
+  auto take = [&](double us, int pq, int oq, int np, int ns) {
     if (least == 0 || us < least) {
       least = us;
       best.pq = pq;
+      best.oq = oq;
       best.np = np;
       best.ns = ns;
     }
   };
-  const int64_t bw = blocks(p.P, best.oq) + blocks(p.S, best.oq);
-  for (int n = 1; n <= kMaxParts && (n == 1 || ((int64_t)n * 64 <= (int64_t)p.P + p.S && n <= most)); n *= 2) {
-    const Task t = task(bw, n, wo, best.oq);
-    const double us = t.wgs <= kCUs ? t.us(false) : std::ceil(t.wgs / (2 * kCUs)) * t.us(true);
-    const double join = best.oq == 1 ? kJoinOwn + kJoinBy8 * (double)ceil_div(R, 8) : kJoin;
-    take(std::max(us, stream) + (n > 1 ? join + n * part : 0.0), 1, n, 0);
-  }
-  // whole rows of full workgroups on every CU: nothing to gain from parts
-  if (p.P == 0 || p.S == 0 || (R >= 64 && wo >= kCUs)) return best;
-  // 32 rows a workgroup for the prefix read it more often, but start sooner: also where there are more rows
-  for (int pq : {1, 4}) {
-    if (pq == 4 ? Rall <= 32 : best.oq == 4) continue;
-    const int64_t bp = blocks(p.P, pq), bo = blocks(p.S, best.oq), wp = row_blocks(Rall, pq) * p.Hk;
-    for (int n = 1; n <= kMaxParts && (n == 1 || (int64_t)n * 64 <= p.P); n *= 2)
-      for (int m = 1; m <= kMaxOwnParts && (m == 1 || (int64_t)m * 64 <= p.S) && n + m <= most; m *= 2) {
-        const Task a = task(bp, n, wp, pq), b = task(bo, m, wo, best.oq);
-        const bool shared = a.wgs + b.wgs > kCUs;
-        const double ua = a.us(shared), ub = b.us(shared);
-        const double us = std::max({ua, ub, 1.36 * (a.wgs * ua + b.wgs * ub) / (2 * kCUs)});
-        take(std::max(us, stream) + kJoin + (n + m) * part, pq, n, m);
-      }
+  // 32 or 128 rows a workgroup: up to 96 rows of a (sequence, key head) three of 32 may waste less than one of 128
+  for (int oq : {1, 4}) {
+    if (oq == 1 ? R > 96 : R <= 32) continue;
+    const int64_t wo = row_blocks(R, oq) * p.B * p.Hk, bw = blocks(p.P, oq) + blocks(p.S, oq);
+    try_parts(std::max<int64_t>(1, std::min({(int64_t)kMaxParts, ((int64_t)p.P + p.S) / 64, gib})), kCUs / wo, 2 * kCUs / wo,
+              [&](int n) {
+                const Task t = task(bw, n, wo, oq);
+                const double us = t.wgs <= kCUs ? t.us(false) : std::ceil(t.wgs / (2 * kCUs)) * t.us(true);
+                const double join = best.few ? kJoinOwn + kJoinBy8 * (double)ceil_div(R, 8) : kJoin;
+                take(std::max(us, stream) + (n > 1 ? join + n * part : 0.0), 1, oq, n, 0);
+              });
+    // whole rows of full workgroups on every CU: nothing to gain from parts
+    if (p.P == 0 || p.S == 0 || (R >= 64 && wo >= kCUs)) continue;
+    // 32 rows a workgroup for the prefix read it more often, but start sooner: also where there are more rows
+    for (int pq : {1, 4}) {
+      if (pq == 4 ? Rall <= 32 : oq == 4) continue;
+      const int64_t bp = blocks(p.P, pq), bo = blocks(p.S, oq), wp = row_blocks(Rall, pq) * p.Hk;
+      for (int m = 1; m <= kMaxOwnParts && (m == 1 || (int64_t)m * 64 <= p.S) && m < gib; m *= 2)
+        try_parts(std::max<int64_t>(1, std::min({(int64_t)kMaxParts, (int64_t)p.P / 64, gib - m})), (kCUs - wo * m) / wp,
+                  (2 * kCUs - wo * m) / wp, [&](int n) {
+                    const Task a = task(bp, n, wp, pq), b = task(bo, m, wo, oq);
+                    const bool shared = a.wgs + b.wgs > kCUs;
+                    const double ua = a.us(shared), ub = b.us(shared);
+                    const double us = std::max({ua, ub, kUneven * (a.wgs * ua + b.wgs * ub) / (2 * kCUs)});
+                    take(std::max(us, stream) + kJoin + (n + m) * part, pq, oq, n, m);
+                  });
+    }
   }
   return best;
 }
@@ -716,7 +735,7 @@ hipError_t launch_all(PrefixParams p, const PrefixPlan& pl, hipStream_t st) {
   if (pl.slots() > 0) p.ws += kCounterBytes / 4;
   if (pl.joined()) return launch_whole<D, 1, true>(p, pl.np, count, st);
   hipError_t e;
-  if (pl.ns == 0) e = pl.oq == 1 ? launch_whole<D, 1, false>(p, 1, nullptr, st) : launch_whole<D, 4, false>(p, pl.np, nullptr, st);
+  if (pl.ns == 0) e = pl.oq == 1 ? launch_whole<D, 1, false>(p, pl.np, nullptr, st) : launch_whole<D, 4, false>(p, pl.np, nullptr, st);
   else if (pl.pq == 1) e = launch_split<D, 1, 1>(p, pl, st);
   else e = pl.oq == 1 ? launch_split<D, 4, 1>(p, pl, st) : launch_split<D, 4, 4>(p, pl, st);
   if (e != hipSuccess || pl.slots() == 0) return e;

@@ -334,6 +334,20 @@ def test_prefix_rows_without_keys_and_stale_cache(d, Lq, S):
 
 
 @gpu
+@pytest.mark.parametrize("B,H,Hk,Lq,P,S,d", [
+    (3, 8, 8, 39, 409, 443, 128), (2, 8, 1, 12, 900, 19, 64), (1, 8, 8, 49, 2300, 51, 64), (1, 4, 4, 33, 0, 700, 128),
+    (5, 14, 2, 12, 1500, 70, 128), (1, 2, 2, 65, 1100, 65, 64), (6, 8, 8, 30, 1700, 30, 128), (3, 6, 2, 150, 1200, 160, 64)])
+def test_prefix_in_uneven_parts(B, H, Hk, Lq, P, S, d):
+    """Between 33 and 96 rows of a (sequence, key head), and numbers of parts that are no power of two."""
+    g = gen(B + Lq + P)
+    a = prefix_inputs(g, B, H, Hk, Lq, P, S, d)
+    lens = torch.randint(0, S + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    lens[0] = S
+    for causal in (False, True):
+        check_attention(cf.attention_prefix(*a, lens, causal=causal), *a, lens, causal)
+
+
+@gpu
 @pytest.mark.parametrize("d,H,Lq", [(64, 4, 5), (128, 8, 3), (64, 16, 40)])
 def test_prefix_rows_without_keys_beside_nan_values(d, H, Lq):
     """A query that sees no key gets 0, also where the keys of the later queries hold values that are not finite."""
