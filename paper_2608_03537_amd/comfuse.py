@@ -683,19 +683,19 @@ def rmsnorm_quant(X, R=None, gamma=None, *, eps=1e-5, norm=True, code="int8", re
     L, torch, device, raw = here
     shape, dtype, dev, f32 = X.shape, X.dtype, X.device, torch.float32
     M, N = shape
-    dt = _dt(X)
-    size = 4 if dt == CF_F32 else 2
-    cdt = _choice(_CODES, code, "code")
-    qdt = torch.int8 if cdt == CF_I8 else torch.uint8
+    dt, size = (CF_BF16, 2) if dtype is torch.bfloat16 else (_dt(X), 4)
+    cdt, qdt = (CF_I8, torch.int8) if code == "int8" else (_choice(_CODES, code, "code"), torch.uint8)
     whole = N * size % 16 == 0    # rows of whole 16 bytes: a contiguous tensor's leading dimension is N
-    ldx = N if whole and X.is_contiguous() else _row_ld(X, M, N, size)
+    plain = whole and X.is_contiguous()
+    ldx = N if plain else _row_ld(X, M, N, size)
     rp = hp = ldr = ldh = 0
     H = residual
     if R is not None:
-        _like(R, shape, dtype, device, "R")
+        if R.dtype is not dtype or R.shape != shape or R.get_device() != device:
+            _like(R, shape, dtype, device, "R")
         rp, ldr = R.data_ptr(), N if whole and R.is_contiguous() else _row_ld(R, M, N, size)
         if H is None:
-            H, ldh = _rows(torch, M, N, dtype, dev, size)
+            H, ldh = (torch.empty_like(X), N) if plain else _rows(torch, M, N, dtype, dev, size)
             hp = H.data_ptr()
     if residual is not None:
         _like(H, shape, dtype, device, "residual")
