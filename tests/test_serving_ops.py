@@ -177,6 +177,19 @@ def test_gemm_i8_sizes(M, N, K):
 
 
 @gpu
+@pytest.mark.parametrize("M,N,K", [
+    (128, 4096, 4112), (20, 12200, 560), (60, 9000, 720), (40, 9000, 1232), (300, 2000, 6032), (500, 3900, 16), (500, 3900, 112),
+    (500, 3900, 240), (500, 3900, 400), (130, 9000, 720), (1000, 4000, 144), (1000, 4000, 272), (130, 11000, 80),
+    (1000, 4000, 1008), (5000, 1000, 4176), (1900, 4000, 16), (1900, 4000, 160), (2500, 8100, 48), (4090, 4081, 4112),
+    (16300, 4090, 304)])
+def test_gemm_i8_ends_of_k(M, N, K):
+    """K that ends inside a step, with few steps, on every shape of tile."""
+    g = gen(M + N + K)
+    A, B = i8(g, M, K), i8(g, N, K)
+    check_gemm(cf.gemm_i8(A, B, out_dtype=F32), A, B, None, None, None, "none")
+
+
+@gpu
 def test_gemm_i8_more_tokens_than_a_grid_of_small_tiles():
     """2^29 + 40 rows and one column: tiles of 32 rows and 256 threads would be 2^32 threads."""
     M = (1 << 29) + 40
