@@ -62,13 +62,14 @@ __device__ __forceinline__ void with_act(int act, F&& f) {
 // Output pass of a tile whose sums lie in LDS: KW planes of TM rows of TN int32 (pitch TN * 4 +
 // 16 bytes), added here.  A thread takes 8 columns of a row at a time, always the same columns.
 // Its scales and biases are loaded ahead (before the main loop, where registers allow: loaded
-// here, they add a trip to memory to every tile).  AHEAD = false: the rows' scales are loaded row by
-// row, and the rows not unrolled, for the 256 x 256 tiles, which have no registers to spare here.
+// here, they add a trip to memory to every tile).  AHEAD = false: all of the tile's lie in LDS (stage_scales),
+// and the rows are not unrolled, for the 256 x 256 tiles, which have no registers to spare here.
 template <int TM, int TN, int NT, bool AHEAD>
 struct TileScales {
   static constexpr int CPR = TN / 8, STEP = NT / CPR, RPT = (TM + STEP - 1) / STEP;   // a thread's rows: STEP apart
   static_assert(NT % CPR == 0, "a thread keeps its columns");
   float sa[AHEAD ? RPT : 1], sb[8], bias[8];
+  const float* rows;   // AHEAD = false: the rows' scales in LDS
   __device__ __forceinline__ void load(const GemmI8Params& p, int m0, int n0) {
     const int n = n0 + threadIdx.x % CPR * 8, r0 = threadIdx.x / CPR;
     auto eight = [&](const float* v, float none, float (&out)[8]) {
@@ -86,9 +87,17 @@ struct TileScales {
     };
     eight(p.sb, 1.0f, sb);
     eight(p.bias, 0.0f, bias);
-    if constexpr (AHEAD) {
 #pragma unroll
-      for (int i = 0; i < RPT; ++i) sa[i] = p.sa ? p.sa[min(m0 + r0 + i * STEP, p.M - 1)] : 1.0f;
+    for (int i = 0; i < RPT; ++i) sa[i] = p.sa ? p.sa[min(m0 + r0 + i * STEP, p.M - 1)] : 1.0f;
+  }
+  // From LDS: sa of the rows, and sb and bias of the tile's columns (only those that the call has).
+  __device__ __forceinline__ void load_staged(const GemmI8Params& p, const float* la, const float* lb, const float* lbias) {
+    const int c = threadIdx.x % CPR * 8;
+    rows = la;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      sb[e] = p.sb ? lb[c + e] : 1.0f;
+      bias[e] = p.bias ? lbias[c + e] : 0.0f;
     }
   }
 };
@@ -154,7 +163,7 @@ __device__ __forceinline__ void finish_tile(const GemmI8Params& p, const TileSca
         if (r0 + i * Sc::STEP < rows) row(r0 + i * Sc::STEP, sc.sa[i]);
     } else {
 #pragma unroll 2
-      for (int r = r0; r < rows; r += Sc::STEP) row(r, p.sa ? p.sa[m0 + r] : 1.0f);
+      for (int r = r0; r < rows; r += Sc::STEP) row(r, p.sa ? sc.rows[r] : 1.0f);
     }
   });
 }
@@ -324,7 +333,18 @@ __global__ __launch_bounds__(S::NT) void gemm_i8_tile_kernel(GemmI8Params p) {
 // Big.
 // ---------------------------------------------------------------------------
 constexpr int kI8BigPitch = kBigT * 4 + 16;
-constexpr int kI8BigLds = 128 * kI8BigPitch > 2 * kBigStep ? 128 * kI8BigPitch : 2 * kBigStep;
+constexpr int kI8BigVec = 128 * kI8BigPitch > 2 * kBigStep ? 128 * kI8BigPitch : 2 * kBigStep;   // sa, sb and bias of the tile
+constexpr int kI8BigLds = kI8BigVec + 3 * kBigT * 4;
+
+// Values at .. at + 63 of v (clamped to n) into LDS, by direct loads: no registers are held while the product
+// runs, whose waits cover them.
+__device__ __forceinline__ void stage_scales(const float* v, int at, int n, char* lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  if (v)
+    __builtin_amdgcn_global_load_lds(v + min(at + (int)(threadIdx.x & 63), n - 1),
+                                     (__attribute__((address_space(3))) void*)lds, 4, 0, 0);
+#endif
+}
 
 __global__ __launch_bounds__(512, 1) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void gemm_i8_big_kernel(GemmI8Params p) {
@@ -334,6 +354,10 @@ void gemm_i8_big_kernel(GemmI8Params p) {
   int rb, c;
   big_tile_order((p.M + kBigT - 1) / kBigT, (p.N + kBigT - 1) / kBigT, rb, c);
   const int m0 = rb * kBigT, n0 = c * kBigT, KT = p.K / 128;
+  float* const vec = reinterpret_cast<float*>(smem + kI8BigVec);   // sa [256], sb [256], bias [256]
+  if (wave < 4) stage_scales(p.sa, m0 + 64 * wave, p.M, smem + kI8BigVec + 256 * wave);
+  else stage_scales(p.sb, n0 + 64 * (wave - 4), p.N, smem + kI8BigVec + 256 * wave);
+  if (wave < 4) stage_scales(p.bias, n0 + 64 * wave, p.N, smem + kI8BigVec + 2048 + 256 * wave);
   i32x16_t acc[2][2][2] = {};   // [token half][32-token block][channel half]
   big_product<false, MmaI8>(acc, reinterpret_cast<const char*>(p.A) + (int64_t)m0 * p.lda, p.lda, p.M - m0,
                             reinterpret_cast<const char*>(p.B) + (int64_t)n0 * p.ldb, p.ldb, p.N - n0, KT, smem);
@@ -368,7 +392,7 @@ void gemm_i8_big_kernel(GemmI8Params p) {
               i32x4_t{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
         }
     TileScales<128, kBigT, 512, false> sc;
-    sc.load(p, m0 + h * 128, n0);
+    sc.load_staged(p, vec + h * 128, vec + 256, vec + 512);
     __syncthreads();
     finish_tile<128, kBigT, 1, 512>(p, sc, smem, m0 + h * 128, n0);
     __syncthreads();
