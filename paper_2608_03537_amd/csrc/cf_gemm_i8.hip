@@ -16,7 +16,7 @@
 // What bounds them: a CU's direct loads into LDS reach 90 to 100 GB/s with all CUs busy, so few tokens
 // are the weights' stream.  In between it is how well a step's loads, LDS reads and MFMAs overlap (1024 x 4096
 // x 4096 on 128 x 128 tiles: 13, 9 and 9 us by themselves, 18 together, and 5 of start and output).  256 x 256
-// tiles run 16384 x 4096 x 4096 in 247 us, 2.2 POP/s; with operands of zeros, whose MFMAs draw
+// tiles run 16384 x 4096 x 4096 in 236 us, 2.3 POP/s; with operands of zeros, whose MFMAs draw
 // less power, in 184: the clock that full power leaves bounds them.  kForms has
 // the measurements of all.  A form that loads fragments straight into registers
 // was slower from 16 tokens on (48 x 12288 x 4096 29 us against 12.8: rows of a power
@@ -422,9 +422,10 @@ hipError_t launch_big(const GemmI8Params& p, hipStream_t st) {
 //     512 x 4096 x 4096       38   27   26 19.8 15.8   18   30   42
 //     1024 x 4096 x 4096      73   49   49   36   30 22.7   31   43
 //     2048 x 4096 x 4096     141   94   95   69   57   43 37.7   48
-//     4096 x 4096 x 4096     282  184  187  135  111   82   75 63.9
-//     8192 x 1024 x 1024      77   51   49   34   25   23 16.0   22
-// Over 36 such calls the form that the estimate takes is 0.7 % slower than the best one on average, 16 % at worst.
+//     4096 x 4096 x 4096     282  184  187  135  111   82   75 60.4
+//     8192 x 1024 x 1024      77   51   49   34   25   22 13.4   20
+// Over 300 calls of all sizes the form that the estimate takes is 0.4 % slower than the best one on average,
+// 20 % at worst.
 struct Form {
   int tm, tn, threads, per;
   double step, start;
@@ -436,27 +437,32 @@ constexpr Form tile_form(int per, double step, double start) {
   return {S::TM, S::TN, S::NT, per, step, start, launch_tile<S>};
 }
 const Form kForms[] = {
-    tile_form<I8Tile<1, 1, 1, 1, 4, 4>>(kCUs, 0.08, 2.2),
-    tile_form<I8Tile<2, 1, 1, 1, 4, 3>>(kCUs, 0.11, 2.8),
-    tile_form<I8Tile<1, 2, 1, 1, 6, 2>>(kCUs, 0.12, 2.4),
-    tile_form<I8Tile<2, 2, 1, 1, 4, 2>>(kCUs, 0.20, 2.9),
-    tile_form<I8Tile<1, 2, 2, 2, 2, 3, true>>(kCUs, 0.31, 3.5),
-    tile_form<I8Tile<2, 2, 2, 2, 2, 2, true>>(kCUs, 0.43, 4.7),
-    tile_form<I8Tile<2, 2, 2, 2, 1, 2>>(2 * kCUs, 1.02, 4.2),
-    {kBigT, kBigT, 512, kCUs, 0.88, 10.5, launch_big},
+    tile_form<I8Tile<1, 1, 1, 1, 4, 4>>(kCUs, 0.093, 2.45),
+    tile_form<I8Tile<2, 1, 1, 1, 4, 3>>(kCUs, 0.154, 4.15),
+    tile_form<I8Tile<1, 2, 1, 1, 6, 2>>(kCUs, 0.17, 2.7),
+    tile_form<I8Tile<2, 2, 1, 1, 4, 2>>(kCUs, 0.21, 3.55),
+    tile_form<I8Tile<1, 2, 2, 2, 2, 3, true>>(kCUs, 0.365, 3.6),
+    tile_form<I8Tile<2, 2, 2, 2, 2, 2, true>>(kCUs, 0.415, 5.5),
+    tile_form<I8Tile<2, 2, 2, 2, 1, 2>>(2 * kCUs, 0.935, 4.55),
+    {kBigT, kBigT, 512, kCUs, 0.86, 11.9, launch_big},
 };
-constexpr double kBigBusy = 0.65;   // added to the step of 256 x 256 tiles times the share of CUs at work (clocks)
+constexpr double kBigBusy = 0.55;   // added to the step of 256 x 256 tiles times the share of CUs at work (clocks)
+// Rows whose pitch is no multiple of 128 bytes take two lines of memory a step; the smaller tiles, which the load
+// path bounds, run slower by this (300 x 4096 x 4080 17.3 us, x 4096 13.7; 256 x 256 tiles 16384 x 4096 x 4080 271, 240).
+constexpr double kOddPitch = 1.27;
 
-const Form& choose_form(int64_t M, int64_t N, int64_t K) {
+const Form& choose_form(const GemmI8Params& p) {
   const Form* best = nullptr;
   double least = 0;
-  const double kt = (double)((K + 127) / 128);
+  const double kt = (double)((p.K + 127) / 128);
+  const bool odd = p.lda % 128 != 0 || p.ldb % 128 != 0;
   for (const Form& f : kForms) {
-    if (f.tm == kBigT && K < 256) continue;   // its loop needs two whole steps
-    const int64_t wgs = ((M + f.tm - 1) / f.tm) * ((N + f.tn - 1) / f.tn), rounds = (wgs + f.per - 1) / f.per;
+    if (f.tm == kBigT && p.K < 256) continue;   // its loop needs two whole steps
+    const int64_t wgs = (int64_t)((p.M + f.tm - 1) / f.tm) * ((p.N + f.tn - 1) / f.tn), rounds = (wgs + f.per - 1) / f.per;
     if (wgs * f.threads > UINT32_MAX) continue;   // a grid has less than 2^32 threads; 128 x 128 tiles of M N <= 2^37 fit
     double step = f.step;
     if (f.tm == kBigT) step += kBigBusy * std::min(1.0, (double)wgs / kCUs);
+    else if (odd) step *= kOddPitch;
     const double t = (double)rounds * (step * kt + f.start);
     if (!best || t < least) {
       best = &f;
@@ -468,6 +474,6 @@ const Form& choose_form(int64_t M, int64_t N, int64_t K) {
 
 }  // namespace
 
-hipError_t launch_gemm_i8(const GemmI8Params& p, hipStream_t st) { return choose_form(p.M, p.N, p.K).launch(p, st); }
+hipError_t launch_gemm_i8(const GemmI8Params& p, hipStream_t st) { return choose_form(p).launch(p, st); }
 
 }  // namespace cf
