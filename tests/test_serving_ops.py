@@ -181,7 +181,7 @@ def test_gemm_i8_sizes(M, N, K):
     (128, 4096, 4112), (20, 12200, 560), (60, 9000, 720), (40, 9000, 1232), (300, 2000, 6032), (500, 3900, 16), (500, 3900, 112),
     (500, 3900, 240), (500, 3900, 400), (130, 9000, 720), (1000, 4000, 144), (1000, 4000, 272), (130, 11000, 80),
     (1000, 4000, 1008), (5000, 1000, 4176), (1900, 4000, 16), (1900, 4000, 160), (2500, 8100, 48), (4090, 4081, 4112),
-    (16300, 4090, 304), (13079, 16, 3664), (8500, 17, 48)])
+    (16300, 4090, 304), (16000, 4090, 1040), (4090, 4000, 2160), (4000, 4081, 1984), (8000, 3900, 1936), (13079, 16, 3664), (8500, 17, 48)])
 def test_gemm_i8_ends_of_k(M, N, K):
     """K that ends inside a step, with few steps, on every shape of tile."""
     g = gen(M + N + K)
