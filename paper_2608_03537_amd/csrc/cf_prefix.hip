@@ -87,71 +87,88 @@ struct PartRows {
 // parts has rows of several sequences, and would join all of them if it came last (47 x 16 heads 17
 // -> 70 us): those keep the second launch.
 
-// The parts of the rows of (b, hk), by the whole workgroup: 8 rows at a time, 256 / D threads a part's
-// row beside each other, WAYS taking the parts in turn.  The grouping depends on the sizes only.
-template <int D>
+// The parts of the rows of (b, hk), by the whole workgroup: RPP rows at a time, D / 8 threads a part's row beside
+// each other.  Of 8 rows, others take the parts in turn (WAYS); of 32, each thread takes all parts, at d = 128 of
+// two rows (2 x 32 heads of 8, 2 queries, 1500 + 100 keys, d 64: 8 rows at a time 9.4 us a call, so 8.5).
+// The grouping depends on the sizes only.
+template <int D, int RPP>
 __device__ __forceinline__ void join_rows(const PrefixParams& p, char* smem, int b, int hk, int slots) {
-  constexpr int TPR = D / 8, RPP = 8, WAYS = 256 / TPR / RPP, AHEAD = 6;
-  const int tid = threadIdx.x, g = tid / TPR, r = g % RPP, way = g / RPP, d0 = tid % TPR * 8;
+  constexpr int TPR = D / 8, SETS = 256 / TPR, RS = RPP < SETS ? RPP : SETS;   // rows beside each other
+  constexpr int WAYS = SETS / RS, RT = RPP / RS, AHEAD = RT == 2 ? 4 : 6;
+  const int tid = threadIdx.x, g = tid / TPR, r = g % RS, way = g / RS, d0 = tid % TPR * 8;
   const int G = p.H / p.Hk, R = G * p.Lq;
   const uint32_t rows = (uint32_t)(p.B * p.Hk * R), ml0 = (uint32_t)slots * rows * (D * 4);
-  float* const so = reinterpret_cast<float*>(smem);             // [WAYS][RPP][D + 2]
+  float* const so = reinterpret_cast<float*>(smem);             // [WAYS][RS][D + 4]
   const int len = own_len(p, b);
-  for (int m0 = 0; m0 < R; m0 += RPP) {
-    const int m = min(m0 + r, R - 1);
-    const uint32_t row = (uint32_t)((b * p.Hk + hk) * R + m);
-    float M = -INFINITY, L = 0.0f, o[8] = {};
-    auto join = [&](float mz, float lz, const float (&x)[8]) {
-      const float mn = fmaxf(M, mz);
-      const float fo = M == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M - mn);
-      const float fz = mz == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mz - mn);
-      M = mn;
-      L = fmaf(fz, lz, fo * L);
+  float M[RT], L[RT], o[RT][8];
+  uint32_t row[RT];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = fmaf(fz, x[e], fo * o[e]);
-    };
-    for (int s0 = way; s0 < slots; s0 += AHEAD * WAYS) {
-      u32x4_t x[AHEAD], y[AHEAD];
-      u32x2_t v[AHEAD];
+  for (int k = 0; k < RT; ++k) {
+    row[k] = (uint32_t)((b * p.Hk + hk) * R + min(r + k * RS, R - 1));
+    M[k] = -INFINITY;
+    L[k] = 0.0f;
 #pragma unroll
-      for (int q = 0; q < AHEAD; ++q) {
-        const uint32_t at = (uint32_t)min(s0 + q * WAYS, slots - 1) * rows + row;
-        x[q] = coherent_load16(p.ws, at * (D * 4) + d0 * 4);
-        y[q] = coherent_load16(p.ws, at * (D * 4) + d0 * 4 + 16);
-        v[q] = coherent_load8(p.ws, ml0 + at * 8);
+    for (int e = 0; e < 8; ++e) o[k][e] = 0.0f;
+  }
+  auto join = [&](int k, float mz, float lz, const float (&x)[8]) {
+    const float mn = fmaxf(M[k], mz);
+    const float fo = M[k] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M[k] - mn);
+    const float fz = mz == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mz - mn);
+    M[k] = mn;
+    L[k] = fmaf(fz, lz, fo * L[k]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[k][e] = fmaf(fz, x[e], fo * o[k][e]);
+  };
+  for (int s0 = way; s0 < slots; s0 += AHEAD * WAYS) {
+    u32x4_t x[AHEAD][RT], y[AHEAD][RT];
+    u32x2_t v[AHEAD][RT];
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q)
+#pragma unroll
+      for (int k = 0; k < RT; ++k) {
+        const uint32_t at = (uint32_t)min(s0 + q * WAYS, slots - 1) * rows + row[k];
+        x[q][k] = coherent_load16(p.ws, at * (D * 4) + d0 * 4);
+        y[q][k] = coherent_load16(p.ws, at * (D * 4) + d0 * 4 + 16);
+        v[q][k] = coherent_load8(p.ws, ml0 + at * 8);
       }
 #pragma unroll
-      for (int q = 0; q < AHEAD; ++q)
-        if (s0 + q * WAYS < slots) {
+    for (int q = 0; q < AHEAD; ++q)
+      if (s0 + q * WAYS < slots) {
+#pragma unroll
+        for (int k = 0; k < RT; ++k) {
           float f[8];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            f[e] = __uint_as_float(x[q][e]);
-            f[4 + e] = __uint_as_float(y[q][e]);
+            f[e] = __uint_as_float(x[q][k][e]);
+            f[4 + e] = __uint_as_float(y[q][k][e]);
           }
-          join(__uint_as_float(v[q][0]), __uint_as_float(v[q][1]), f);
+          join(k, __uint_as_float(v[q][k][0]), __uint_as_float(v[q][k][1]), f);
         }
-    }
-    float* const mine = so + (way * RPP + r) * (D + 4);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) mine[d0 + e] = o[e];
-    if (d0 == 0) {
-      mine[D] = M;
-      mine[D + 1] = L;
-    }
-    __syncthreads();
-    if (way == 0 && m0 + r < R) {
-#pragma unroll
-      for (int w = 1; w < WAYS; ++w) {
-        const float* other = so + (w * RPP + r) * (D + 4);
-        float f[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = other[d0 + e];
-        join(other[D], other[D + 1], f);
       }
-      store_row(p, b, hk * G + m % G, m / G, d0, o, L, p.P > 0 || own_seen(p, len, m / G) > 0);
+  }
+  if constexpr (WAYS > 1) {
+    float* const mine = so + (way * RS + r) * (D + 4);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mine[d0 + e] = o[0][e];
+    if (d0 == 0) {
+      mine[D] = M[0];
+      mine[D + 1] = L[0];
     }
     __syncthreads();
+    if (way != 0) return;
+#pragma unroll
+    for (int w = 1; w < WAYS; ++w) {
+      const float* other = so + (w * RS + r) * (D + 4);
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = other[d0 + e];
+      join(0, other[D], other[D + 1], f);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < RT; ++k) {
+    const int m = r + k * RS;
+    if (m < R) store_row(p, b, hk * G + m % G, m / G, d0, o[k], L[k], p.P > 0 || own_seen(p, len, m / G) > 0);
   }
 }
 
@@ -493,7 +510,10 @@ __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb
       *last = atomicInc(c, (unsigned)(slots - 1)) == (unsigned)(slots - 1);   // the last one wraps it to 0
     }
     __syncthreads();
-    if (*last) join_rows<D>(p, smem, b, hk, slots);
+    if (*last) {   // R <= 32
+      if (R <= 8) join_rows<D, 8>(p, smem, b, hk, slots);
+      else join_rows<D, 32>(p, smem, b, hk, slots);
+    }
   }
 }
 
