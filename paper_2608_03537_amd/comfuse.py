@@ -779,7 +779,7 @@ def attention_prefix(Q, Kp, Vp, Ks=None, Vs=None, lens=None, *, causal=False, sc
     are multiples of 8 elements with unit innermost stride (caches stored
     token-major are passed as transposed views).  causal: query i sees the own
     keys j < lens[b] - (Lq - 1 - i).  A query that sees no key gets 0.  ws: a
-    workspace of the caller's own (cf_attention_prefix_workspace bytes, its first
+    workspace of the caller's own (uint8, cf_attention_prefix_workspace bytes, its first
     CF_PREFIX_WS_HEADER_BYTES zero before its first use).
     """
     here = _here(Q, stream)
