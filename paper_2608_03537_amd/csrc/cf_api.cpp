@@ -14,6 +14,7 @@
 
 #include "comfuse.h"
 #include "cf_internal.h"
+#include "cf_serving.h"
 
 using namespace cf;
 

@@ -25,6 +25,7 @@
 
 #include "cf_attn.h"
 #include "cf_gemm_big.h"
+#include "cf_serving.h"
 
 namespace cf {
 

@@ -15,6 +15,7 @@
 
 #include "cf_attn.h"
 #include "cf_gemm_tile.h"
+#include "cf_serving.h"
 #include "comfuse.h"
 
 namespace cf {

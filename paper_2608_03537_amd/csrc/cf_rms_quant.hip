@@ -11,6 +11,7 @@
 #include <algorithm>
 
 #include "cf_device.h"
+#include "cf_serving.h"
 
 namespace cf {
 
