@@ -760,12 +760,17 @@ _prefix_lock = threading.Lock()   # threads that share a stream share its worksp
 
 
 def _prefix_workspace(torch, need, device, key):
-    """workspace(need, device, kind="prefix") at less cost: cached per device and stream while nothing is captured."""
+    """workspace(need, device, kind="prefix") at less cost: cached per device and stream while nothing is captured.
+    A new one is half as large again as the last, so that a batch that grows step by step seldom needs it, and only
+    its counters are cleared."""
     if torch._C._cuda_isCurrentStreamCapturing():
         return workspace(need, device, None, kind="prefix")
     ws = _ws_cache.get(key)
     if ws is None or ws.numel() < need:
-        ws = _ws_cache[key] = torch.zeros(need, dtype=torch.uint8, device=device)
+        size = max(need, 1 << 20 if ws is None else ws.numel() * 3 // 2)
+        ws = torch.empty(size, dtype=torch.uint8, device=device)
+        ws[:CF_PREFIX_WS_HEADER_BYTES].view(torch.int32).zero_()
+        _ws_cache[key] = ws
     return ws
 
 
