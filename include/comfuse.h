@@ -387,6 +387,11 @@ typedef struct {
 
 cf_status cf_gemm_i8(const cf_gemm_i8_args* a, void* hip_stream);
 
+/* Which kernel form a call of these sizes and leading dimensions takes, in words, for tests and
+   profiles ("" where it takes none: M = 0, or sizes that the call refuses).  The text is
+   the calling thread's, valid until its next query of a form. */
+const char* cf_gemm_i8_form(const cf_gemm_i8_args* a);
+
 /* ------------------------------------------------------------------------
  * cf_attention_prefix — attention of a batch whose sequences share a prefix:
  * sequence b attends to the P prefix keys, stored once, and to the first
@@ -431,6 +436,9 @@ typedef struct {
 size_t    cf_attention_prefix_workspace(const cf_attention_prefix_args* a);
 cf_status cf_attention_prefix(const cf_attention_prefix_args* a, void* workspace,
                               size_t ws_bytes, void* hip_stream);
+
+/* How a call of these sizes is cut, in words; as cf_gemm_i8_form. */
+const char* cf_attention_prefix_form(const cf_attention_prefix_args* a);
 
 /* ------------------------------------------------------------------------
  * cf_workspace_check — reads and clears the error word of a workspace used by

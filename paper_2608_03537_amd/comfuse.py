@@ -136,6 +136,9 @@ def lib():
                     f = getattr(L, name)
                     f.restype = C.c_int
                     f.argtypes = [vp, vp, C.c_size_t, vp] if ws else [vp, vp]   # arguments: byref or packed bytes
+                for name in ("cf_gemm_i8_form", "cf_attention_prefix_form"):
+                    getattr(L, name).restype = C.c_char_p
+                    getattr(L, name).argtypes = [vp]
                 L.cf_attention_prefix_workspace.restype = C.c_size_t
                 L.cf_attention_prefix_workspace.argtypes = [vp]
                 L.cf_workspace_check.restype = C.c_int
@@ -198,12 +201,20 @@ def cf_gemm_i8(args, stream):
     return lib().cf_gemm_i8(C.byref(args), stream)
 
 
+def cf_gemm_i8_form(args):
+    return lib().cf_gemm_i8_form(C.byref(args)).decode()
+
+
 def cf_attention_prefix(args, workspace, ws_bytes, stream):
     return lib().cf_attention_prefix(C.byref(args), workspace, ws_bytes, stream)
 
 
 def cf_attention_prefix_workspace(args):
     return lib().cf_attention_prefix_workspace(C.byref(args))
+
+
+def cf_attention_prefix_form(args):
+    return lib().cf_attention_prefix_form(C.byref(args)).decode()
 
 
 def cf_workspace_check(workspace, ws_bytes, stream):

@@ -1125,20 +1125,42 @@ cf_status cf_rmsnorm_quant(const cf_rmsnorm_quant_args* a, void* hip_stream) {
 // The sum of K products of two int8 values fits 32 bits: |product| <= 2^14.
 static constexpr int64_t kGemmI8MaxK = 131056;
 
+// Sizes only: what the form depends on.
+static cf_status gemm_i8_sizes(const cf_gemm_i8_args* a, GemmI8Params& p) {
+  if (!a) return fail(CF_ERR_NULL, "args is NULL");
+  if (a->struct_size != sizeof(cf_gemm_i8_args))
+    return fail(CF_ERR_STRUCT, "struct_size %zu != %zu", a->struct_size, sizeof(cf_gemm_i8_args));
+  if (a->M < 0 || a->M > (int64_t)1 << 30 || a->N <= 0 || a->N > (int64_t)1 << 20)
+    return fail(CF_ERR_SHAPE, "need 0 <= M <= 2^30, 0 < N <= 2^20");
+  if (a->M * a->N > (int64_t)1 << 37) return fail(CF_ERR_SHAPE, "M * N exceeds 2^37");
+  if (a->K <= 0 || a->K > kGemmI8MaxK || a->K % 16 != 0)
+    return fail(CF_ERR_SHAPE, "K = %lld must be a multiple of 16 up to %lld", (long long)a->K, (long long)kGemmI8MaxK);
+  p = GemmI8Params{};
+  p.M = (int)a->M;
+  p.N = (int)a->N;
+  p.K = (int)a->K;
+  p.lda = a->lda;
+  p.ldb = a->ldb;
+  return CF_OK;
+}
+
+static thread_local char g_form[96];
+
+const char* cf_gemm_i8_form(const cf_gemm_i8_args* a) {
+  GemmI8Params p;
+  if (gemm_i8_sizes(a, p) != CF_OK || p.M == 0) return "";
+  gemm_i8_form(p, g_form, sizeof(g_form));
+  return g_form;
+}
+
 cf_status cf_gemm_i8(const cf_gemm_i8_args* a, void* hip_stream) {
   try {
-    if (!a) return fail(CF_ERR_NULL, "args is NULL");
-    if (a->struct_size != sizeof(cf_gemm_i8_args))
-      return fail(CF_ERR_STRUCT, "struct_size %zu != %zu", a->struct_size, sizeof(cf_gemm_i8_args));
-    if (a->M < 0 || a->M > (int64_t)1 << 30 || a->N <= 0 || a->N > (int64_t)1 << 20)
-      return fail(CF_ERR_SHAPE, "need 0 <= M <= 2^30, 0 < N <= 2^20");
-    if (a->M * a->N > (int64_t)1 << 37) return fail(CF_ERR_SHAPE, "M * N exceeds 2^37");
-    if (a->K <= 0 || a->K > kGemmI8MaxK || a->K % 16 != 0)
-      return fail(CF_ERR_SHAPE, "K = %lld must be a multiple of 16 up to %lld", (long long)a->K, (long long)kGemmI8MaxK);
+    GemmI8Params p;
+    cf_status s = gemm_i8_sizes(a, p);
+    if (s != CF_OK) return s;
     if (a->out_dtype != CF_F32 && a->out_dtype != CF_BF16) return fail(CF_ERR_DTYPE, "out_dtype must be F32 or BF16");
     if (a->act != CF_ACT_NONE && a->act != CF_ACT_GELU && a->act != CF_ACT_GELU_TANH && a->act != CF_ACT_RELU)
       return fail(CF_ERR_UNSUPPORTED, "unknown act");
-    cf_status s;
     if ((s = check_matrix("A", a->A, a->M, a->K, a->lda, CF_I8, true)) != CF_OK ||
         (s = check_matrix("B", a->B, a->M > 0 ? a->N : 0, a->K, a->ldb, CF_I8, true)) != CF_OK ||
         (s = check_matrix("C", a->C, a->M, a->N, a->ldc, a->out_dtype, true)) != CF_OK ||
@@ -1149,14 +1171,8 @@ cf_status cf_gemm_i8(const cf_gemm_i8_args* a, void* hip_stream) {
     if (a->M == 0) return CF_OK;
     static_assert((int)CF_ACT_GELU == (int)ACT_GELU && (int)CF_ACT_GELU_TANH == (int)ACT_GELU_TANH &&
                       (int)CF_ACT_RELU == (int)ACT_RELU, "act values");
-    GemmI8Params p{};
-    p.M = (int)a->M;
-    p.N = (int)a->N;
-    p.K = (int)a->K;
     p.A = reinterpret_cast<const int8_t*>(a->A);
-    p.lda = a->lda;
     p.B = reinterpret_cast<const int8_t*>(a->B);
-    p.ldb = a->ldb;
     p.sa = a->sa;
     p.sb = a->sb;
     p.bias = a->bias;
@@ -1233,6 +1249,13 @@ size_t cf_attention_prefix_workspace(const cf_attention_prefix_args* a) {
   } catch (...) {
     return 0;
   }
+}
+
+const char* cf_attention_prefix_form(const cf_attention_prefix_args* a) {
+  PrefixParams p;
+  if (prefix_sizes(a, p) != CF_OK || p.B == 0 || p.Lq == 0) return "";
+  prefix_form(p, g_form, sizeof(g_form));
+  return g_form;
 }
 
 cf_status cf_attention_prefix(const cf_attention_prefix_args* a, void* workspace, size_t ws_bytes, void* hip_stream) {

@@ -22,6 +22,7 @@
 // was slower from 16 tokens on (48 x 12288 x 4096 29 us against 12.8: rows of a power
 // of two apart meet in the same sets of the first-level cache).
 #include <algorithm>
+#include <cstdio>
 
 #include "cf_attn.h"
 #include "cf_gemm_big.h"
@@ -476,5 +477,10 @@ const Form& choose_form(const GemmI8Params& p) {
 }  // namespace
 
 hipError_t launch_gemm_i8(const GemmI8Params& p, hipStream_t st) { return choose_form(p).launch(p, st); }
+
+void gemm_i8_form(const GemmI8Params& p, char* text, size_t bytes) {
+  const Form& f = choose_form(p);
+  snprintf(text, bytes, "%d x %d tiles of %d threads, %s K", f.tm, f.tn, f.threads, p.K % 128 == 0 ? "whole" : "cut");
+}
 
 }  // namespace cf

@@ -12,6 +12,7 @@
 // lazily).
 #include <algorithm>
 #include <cmath>
+#include <cstdio>
 
 #include "cf_attn.h"
 #include "cf_gemm_tile.h"
@@ -92,6 +93,7 @@ struct PartRows {
 // each other.  Of 8 rows, others take the parts in turn (WAYS); of 32, each thread takes all parts, at d = 128 of
 // two rows (2 x 32 heads of 8, 2 queries, 1500 + 100 keys, d 64: 8 rows at a time 9.4 us a call, so 8.5).
 // The grouping depends on the sizes only.
+constexpr int kJoinFew = 8;
 template <int D, int RPP>
 __device__ __forceinline__ void join_rows(const PrefixParams& p, char* smem, int b, int hk, int slots) {
   constexpr int TPR = D / 8, SETS = 256 / TPR, RS = RPP < SETS ? RPP : SETS;   // rows beside each other
@@ -512,7 +514,7 @@ __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb
     }
     __syncthreads();
     if (*last) {   // R <= 32
-      if (R <= 8) join_rows<D, 8>(p, smem, b, hk, slots);
+      if (R <= kJoinFew) join_rows<D, kJoinFew>(p, smem, b, hk, slots);
       else join_rows<D, 32>(p, smem, b, hk, slots);
     }
   }
@@ -632,6 +634,7 @@ struct PrefixPlan {
   bool few;     // at most 32 rows of a (sequence, key head)
   int slots() const { return ns > 0 ? np + ns : np > 1 ? np : 0; }
   bool joined() const { return ns == 0 && np > 1 && few; }   // by the last workgroup, without a second launch
+  int ways() const { return slots() <= 4 ? 1 : slots() <= 16 ? 4 : 8; }   // of the second launch
 };
 constexpr size_t kCounterBytes = CF_PREFIX_WS_HEADER_BYTES;   // the counters of (sequence, key head); the partial results follow
 constexpr int kCUs = 256, kMaxParts = 32, kMaxOwnParts = 8;
@@ -760,8 +763,8 @@ hipError_t launch_all(PrefixParams p, const PrefixPlan& pl, hipStream_t st) {
   else if (pl.pq == 1) e = launch_split<D, 1, 1>(p, pl, st);
   else e = pl.oq == 1 ? launch_split<D, 4, 1>(p, pl, st) : launch_split<D, 4, 4>(p, pl, st);
   if (e != hipSuccess || pl.slots() == 0) return e;
-  return pl.slots() <= 4 ? launch_merge<D, 1>(p, pl.slots(), st)
-                         : pl.slots() <= 16 ? launch_merge<D, 4>(p, pl.slots(), st) : launch_merge<D, 8>(p, pl.slots(), st);
+  return pl.ways() == 1 ? launch_merge<D, 1>(p, pl.slots(), st)
+                        : pl.ways() == 4 ? launch_merge<D, 4>(p, pl.slots(), st) : launch_merge<D, 8>(p, pl.slots(), st);
 }
 
 }  // namespace
@@ -775,6 +778,16 @@ size_t prefix_workspace(const PrefixParams& p) {
 hipError_t launch_prefix(const PrefixParams& p, hipStream_t st) {
   const PrefixPlan pl = make_plan(p);
   return p.d == 128 ? launch_all<128>(p, pl, st) : launch_all<64>(p, pl, st);
+}
+
+void prefix_form(const PrefixParams& p, char* text, size_t bytes) {
+  const PrefixPlan pl = make_plan(p);
+  int n = pl.ns > 0 ? snprintf(text, bytes, "split, %d + %d rows, %d + %d parts", 32 * pl.pq, 32 * pl.oq, pl.np, pl.ns)
+                    : snprintf(text, bytes, "whole, %d rows, %d parts", 32 * pl.oq, pl.np);
+  if (pl.joined())
+    snprintf(text + n, bytes - n, ", joined by %d", (int64_t)(p.H / p.Hk) * p.Lq <= kJoinFew ? kJoinFew : 32);
+  else if (pl.slots() > 0)
+    snprintf(text + n, bytes - n, ", merged %d ways", pl.ways());
 }
 
 }  // namespace cf

@@ -31,6 +31,7 @@ struct GemmI8Params {
   void* C; int64_t ldc; int c_f32;
 };
 hipError_t launch_gemm_i8(const GemmI8Params& p, hipStream_t st);
+void gemm_i8_form(const GemmI8Params& p, char* text, size_t bytes);   // from M, N, K, lda, ldb
 
 // Attention over a shared prefix and each sequence's own keys (cf_prefix.hip).
 struct PrefixParams {
@@ -47,5 +48,6 @@ struct PrefixParams {
 };
 size_t prefix_workspace(const PrefixParams& p);
 hipError_t launch_prefix(const PrefixParams& p, hipStream_t st);
+void prefix_form(const PrefixParams& p, char* text, size_t bytes);   // from the sizes
 
 }  // namespace cf
