@@ -337,9 +337,9 @@ cf_status cf_rowop(int64_t batch, int64_t M, int64_t N, cf_dtype in,
  * and a leading dimension are neither used nor written.  H may be R itself
  * (same pointer and ld): the residual stream is then updated in place.
  * A row whose t is all zero gets s = 0 and zero codes; a row in which some t
- * is NaN or infinite gets s = NaN and zero codes.  The mean of squares is held
- * in fp32: s is 0 where it overflows (|h| about 1.8e19 and more), and with eps = 0
- * inexact, in the end infinite, where it underflows (|h| below 1e-19 throughout).
+ * is NaN or infinite gets s = NaN and zero codes.  The squares are summed in fp32, rescaled
+ * where the sum would overflow; with eps = 0, s is inexact, in the end infinite, where they
+ * underflow (|h| below 1e-19 throughout).
  * ------------------------------------------------------------------------ */
 typedef struct {
   size_t struct_size;            /* = sizeof(cf_rmsnorm_quant_args) */

@@ -7,7 +7,8 @@
 // The normed row is t / rms, and rms cancels in (t / rms) / (d / rms): the codes
 // come from t and its maximum alone.  A maximum does not depend on the order of
 // its terms, so the codes are the same bits however a row is spread over lanes,
-// and the sum of squares (fp32, order fixed by the width) enters s only.
+// and the sum of squares (fp32, order fixed by the width) enters s only.  It is kept scaled by
+// 2^-144 as well, for rows whose sum passes fp32's range.
 #include <algorithm>
 
 #include "cf_device.h"
@@ -19,6 +20,9 @@ namespace {
 
 constexpr float kUp = 1.8446744073709552e19f, kDown = 5.4210108624275222e-20f;   // 2^64, 2^-64
 constexpr float kSmall = 8.6736173798840355e-19f;                                // 2^-60
+// Of N <= 2^15 finite h, (2^-72 h)^2 adds up to less than 2^128; a row whose plain sum passes 2^128 has
+// |h| of 2^56 and more, whose scaled squares are normal.
+constexpr float kLow = 2.1175823681357508e-22f, kLow2 = 4.4841550858394146e-44f, kHalfLow = 1.4551915228366852e-11f;   // 2^-72, 2^-144, 2^-36
 
 // E = 16 / sizeof(T) consecutive elements of a row as fp32; elements at and
 // behind `left` are 0 and not read.
@@ -105,7 +109,7 @@ __global__ __launch_bounds__(NT) void rms_quant_kernel(RmsQuantParams p) {
       for (int e = 0; e < E; ++e) v[c][e] += r[e];
     }
   }
-  float ss = 0.0f;
+  float ss = 0.0f, far = 0.0f;
   uint32_t mb = 0;   // maximum of |t| by its bits: a NaN is above infinity, so it is kept
 #pragma unroll
   for (int c = 0; c < C; ++c) {
@@ -113,7 +117,11 @@ __global__ __launch_bounds__(NT) void rms_quant_kernel(RmsQuantParams p) {
     if (n >= p.N) break;
     if (p.H) store_chunk<T, E>(H + n, p.N - n, v[c]);
 #pragma unroll
-    for (int e = 0; e < E; ++e) ss = fmaf(v[c][e], v[c][e], ss);
+    for (int e = 0; e < E; ++e) {
+      const float low = v[c][e] * kLow;
+      ss = fmaf(v[c][e], v[c][e], ss);
+      far = fmaf(low, low, far);
+    }
     if (p.gamma) {
       float g[E];
       if (p.N - n >= E) {
@@ -158,12 +166,28 @@ __global__ __launch_bounds__(NT) void rms_quant_kernel(RmsQuantParams p) {
   const float qmax = p.e4m3 ? 448.0f : 127.0f;
   const float m = __uint_as_float(mb);
   const bool ok = mb != 0 && mb < 0x7F800000u;   // some value, and all finite
+  const bool over = ok && p.norm && !(ss < INFINITY);   // the same in every thread of the row
+  if (over) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) far += __shfl_xor(far, o);
+    if constexpr (W > 1) {
+      __shared__ float far_w[W];
+      if (lane == 0) far_w[tid >> 6] = far;
+      __syncthreads();
+      far = 0.0f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) far += far_w[w];
+    }
+  }
   // Small rows are raised by 2^64 (exact), so that d and 1 / d stay normal.
   const float up = m < kSmall ? kUp : 1.0f;
   const float d = ok ? m * up / qmax : 1.0f, rd = 1.0f / d;
   if (t == 0) {
     float s = m < kSmall ? d * kDown : d;
-    if (p.norm) s = m < kSmall ? d * (1.0f / sqrtf(ss / (float)p.N + p.eps)) * kDown : d / sqrtf(ss / (float)p.N + p.eps);
+    if (over)
+      s = d * kHalfLow * (1.0f / sqrtf(far / (float)p.N + p.eps * kLow2)) * kHalfLow * (m < kSmall ? kDown : 1.0f);
+    else if (p.norm)
+      s = m < kSmall ? d * (1.0f / sqrtf(ss / (float)p.N + p.eps)) * kDown : d / sqrtf(ss / (float)p.N + p.eps);
     p.s[row] = mb == 0 ? 0.0f : ok ? s : __uint_as_float(0x7FC00000u);
   }
   uint8_t* Q = reinterpret_cast<uint8_t*>(p.Q) + row * p.ldq;

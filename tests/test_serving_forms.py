@@ -1,14 +1,64 @@
 """The serving operators' helpers and kernel forms beyond test_serving_ops.py: every form of the int8 product
 and of the attention over a shared prefix, each named by the library's own query, so that a change of the
 estimates that choose them cannot move a test away from its form."""
+import math
 import types
 
 import pytest
 import torch
 
 from paper_2608_03537_amd import comfuse as cf
-from test_serving_ops import (BF16, F32, F64, check_attention, check_gemm, gemm_args, gen, gpu, i8, prefix_args,
-                              prefix_inputs)
+from test_serving_ops import (BF16, F32, F64, HALF, QMAX, U, check_attention, check_gemm, gemm_args, gen, gpu, i8,
+                              norm_ref, padded, prefix_args, prefix_inputs)
+
+
+# ---------------------------------------------------------------- rmsnorm_quant: special rows with the norm
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("N", [24, 400, 1500, 4000, 7000, 20000, 32768])
+def test_normed_special_rows(N, code, dtype):
+    """All-zero, NaN, infinite and tiny rows, rows that gamma clears, and large ones on either side of where the
+    sum of squares and their mean pass fp32's largest value."""
+    g = gen(N)
+    X, R = padded(12, N, dtype, g), padded(12, N, dtype, g, 0.25)
+    gamma = torch.rand((N,), generator=g, device="cuda") + 0.5
+    gamma[:4] = 0.0
+    X[1], R[1] = 0.0, 0.0
+    X[2, N // 2] = float("nan")
+    R[3, N - 1] = -math.inf
+    X[4] *= 1e-25
+    R[4] *= 1e-25
+    X[5, 4:], R[5, 4:] = 0.0, 0.0
+    for row, size in ((6, (0.1 * 3.4e38 / N) ** 0.5), (7, (4 * 3.4e38 / N) ** 0.5), (8, 1e19), (9, 4e19), (10, 1e30),
+                      (11, 1e37)):
+        X[row] = (X[row].float().clamp(-4, 4) * size).to(dtype)
+        R[row] = (R[row].float() * size).to(dtype)
+    Q, s, H = cf.rmsnorm_quant(X, R, gamma, eps=1e-5, code=code)
+    z, sr, h = norm_ref(X, R, gamma, 1e-5, True, code)
+    q = Q.to(F64) if code == "int8" else Q.contiguous().view(torch.float8_e4m3fn).to(F64)
+    assert not q[[1, 2, 3, 5]].any() and not s[[1, 5]].any() and s[2].isnan() and s[3].isnan()
+    rows = [0, 4, 6, 7, 8, 9, 10, 11]
+    half = 0.5 if code == "int8" else torch.clamp(z[rows].abs() * 2.0 ** -4, min=2.0 ** -10)
+    assert bool(((q[rows] - z[rows]).abs() <= half + 4.1 * U * QMAX[code]).all())
+    # s: h, t, d; half of h, of its square and of a sum of at most 64 terms a lane and 10 levels, of the mean and of
+    # eps' addition; the root, its reciprocal, two products.  Below 2^-126 a product is off by half of 2^-149
+    bad = ~((s.to(F64)[rows] - sr[rows]).abs() <= (7 + (1 + 74 + 3) / 2) * U * sr[rows] + 2.0 ** -149)
+    assert not bool(bad.any()), (bad.nonzero().tolist(), s[rows].tolist(), sr[rows].tolist())
+    assert bool(((H[rows].to(F64) - h[rows]).abs() <= (HALF[dtype] + U) * h[rows].abs()).all())
+
+
+@gpu
+@pytest.mark.parametrize("N", [64, 3000])
+def test_normed_large_rows_in_place(N):
+    """The same where the residual stream is updated in place, bit for bit."""
+    g = gen(N)
+    X, R = padded(9, N, BF16, g), padded(9, N, BF16, g)
+    X[3:6] = (X[3:6].float() * 1e30).to(BF16)
+    R[4:7] = (R[4:7].float() * 1e25).to(BF16)
+    want = cf.rmsnorm_quant(X, R)
+    got = cf.rmsnorm_quant(X, R, residual=R)
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and bool((want[1] > 0).all())
 
 
 # ---------------------------------------------------------------- gemm_i8: every tile, K whole and cut
