@@ -1147,10 +1147,14 @@ static cf_status gemm_i8_sizes(const cf_gemm_i8_args* a, GemmI8Params& p) {
 static thread_local char g_form[96];
 
 const char* cf_gemm_i8_form(const cf_gemm_i8_args* a) {
-  GemmI8Params p;
-  if (gemm_i8_sizes(a, p) != CF_OK || p.M == 0) return "";
-  gemm_i8_form(p, g_form, sizeof(g_form));
-  return g_form;
+  try {
+    GemmI8Params p;
+    if (gemm_i8_sizes(a, p) != CF_OK || p.M == 0) return "";
+    gemm_i8_form(p, g_form, sizeof(g_form));
+    return g_form;
+  } catch (...) {
+    return "";
+  }
 }
 
 cf_status cf_gemm_i8(const cf_gemm_i8_args* a, void* hip_stream) {
@@ -1252,10 +1256,14 @@ size_t cf_attention_prefix_workspace(const cf_attention_prefix_args* a) {
 }
 
 const char* cf_attention_prefix_form(const cf_attention_prefix_args* a) {
-  PrefixParams p;
-  if (prefix_sizes(a, p) != CF_OK || p.B == 0 || p.Lq == 0) return "";
-  prefix_form(p, g_form, sizeof(g_form));
-  return g_form;
+  try {
+    PrefixParams p;
+    if (prefix_sizes(a, p) != CF_OK || p.B == 0 || p.Lq == 0) return "";
+    prefix_form(p, g_form, sizeof(g_form));
+    return g_form;
+  } catch (...) {
+    return "";
+  }
 }
 
 cf_status cf_attention_prefix(const cf_attention_prefix_args* a, void* workspace, size_t ws_bytes, void* hip_stream) {
