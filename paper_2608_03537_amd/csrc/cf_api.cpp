@@ -1224,7 +1224,7 @@ static cf_status prefix_sizes(const cf_attention_prefix_args* a, PrefixParams& p
     return fail(CF_ERR_STRUCT, "struct_size %zu != %zu", a->struct_size, sizeof(cf_attention_prefix_args));
   if (a->dtype != CF_BF16) return fail(CF_ERR_DTYPE, "cf_attention_prefix computes in bf16 only");
   if (a->batch < 0 || a->batch > 65535 || a->H <= 0 || a->Hk <= 0 || a->H > 65535 || a->Lq < 0 ||
-      a->Lq > (int64_t)1 << 24 || a->P < 0 || a->S < 0 || a->P > (int64_t)1 << 30 || a->S > (int64_t)1 << 30)
+      a->Lq > (int64_t)1 << 24 || a->P < 0 || a->S < 0 || a->P > kPrefixMaxKeys || a->S > kPrefixMaxKeys)
     return fail(CF_ERR_SHAPE, "need 0 <= batch <= 65535, 0 < H <= 65535, 0 <= Lq <= 2^24, 0 <= P, S <= 2^30");
   if (a->H % a->Hk != 0) return fail(CF_ERR_SHAPE, "H = %lld is not a multiple of Hk = %lld", (long long)a->H, (long long)a->Hk);
   if (a->batch * a->Hk > 65535) return fail(CF_ERR_SHAPE, "batch * Hk exceeds 65535");

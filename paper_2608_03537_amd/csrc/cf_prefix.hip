@@ -208,7 +208,7 @@ __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb
   const int first = KIND == PREFIX ? 0 : own_seen(p, len, m0 / G);                        // ... that every row sees
   const int seen = KIND == PREFIX ? 0 : own_seen(p, len, qi);                             // ... that this lane's row sees
   const int nball = nbp + (last + BK - 1) / BK;
-  // (blocks <= 2^26 + 2^26 and parts <= kMaxParts: the products fit 32 bits)
+  // (at most 2^25 + 2^25 blocks and 32 parts: the products are at most 2^31; asserted at kMaxParts)
   const int jb = (int)((uint32_t)nball * z / (uint32_t)parts), NB = (int)((uint32_t)nball * (z + 1) / (uint32_t)parts);
   const bf16_t* const Kp = p.Kp + hk * p.kp_h;
   const bf16_t* const Vp = p.Vp + hk * p.vp_h;
@@ -638,6 +638,8 @@ struct PrefixPlan {
 };
 constexpr size_t kCounterBytes = CF_PREFIX_WS_HEADER_BYTES;   // the counters of (sequence, key head); the partial results follow
 constexpr int kCUs = 256, kMaxParts = 32, kMaxOwnParts = 8;
+static_assert(2 * kPrefixMaxKeys / std::min(PrefixShape<128, 1>::BK, PrefixShape<128, 4>::BK) * kMaxParts <= UINT32_MAX,
+              "a part's first block is computed in 32 bits (attend)");
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t row_blocks(int64_t rows, int qg) { return ceil_div(rows, 32 * qg); }

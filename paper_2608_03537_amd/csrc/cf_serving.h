@@ -46,6 +46,7 @@ struct PrefixParams {
   uint16_t* O; int64_t o_b, o_h, o_l;
   float* ws;
 };
+constexpr int64_t kPrefixMaxKeys = (int64_t)1 << 30;   // of the prefix, and of the own keys
 size_t prefix_workspace(const PrefixParams& p);
 hipError_t launch_prefix(const PrefixParams& p, hipStream_t st);
 void prefix_form(const PrefixParams& p, char* text, size_t bytes);   // from the sizes
