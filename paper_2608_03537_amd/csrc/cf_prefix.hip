@@ -353,6 +353,9 @@ __device__ __forceinline__ void attend(const PrefixParams& p, char* smem, int rb
     const float corr = need ? __builtin_amdgcn_exp2f(m_used - m_eff) : 1.0f;
     m_used = m_eff;
     const float nm = m_used == -INFINITY ? 0.0f : -m_used;   // nothing seen yet: P are 0
+    // P goes to the second product as bf16, the type of V and so of the MFMA's other operand.  Of the output's error
+    // against 64 bits, 0.0022 to 0.0023 (relative norm), 0.0017 is its own rounding and 0.0014 to 0.0016 this one;
+    // P as a sum of two bf16 would double the product.
     u32x4_t P[A::NH][2];
 #pragma unroll
     for (int e = 0; e < 16 * A::NH; ++e)
