@@ -653,12 +653,13 @@ int64_t row_blocks(int64_t rows, int qg) { return ceil_div(rows, 32 * qg); }
 // 64 to 16000 prefix keys, each measured in up to 80 cuts, at the time that a caller in Python sees (a second
 // launch costs the host 4 us): the cut that the estimate takes is 2 % slower than the best one on
 // average, 25 % at worst; with powers of two only 3 %, with 128 rows a workgroup for all calls
-// of more than 32 rows 4 %.  Some of them (us: whole rows; the best split):
-//     4 x 8 heads, 1 query, 128 + 64 keys, d 64                5.6     8.5
-//     64 x 8 heads, 1 query, 512 + 128, d 64                  10.7    12.5
-//     16 x 16 heads, 5 queries, 4095 + 333, d 64              22.6    15.5 (4 + 1 parts)
-//     1 x 32 heads of 8, 1 query, 8192 + 512, d 128             67    13.4 (16 + 2)
-//     64 x 32 heads of 8, 1 query, 8192 + 512, d 128           118    39.8 (8 + 2)
+// of more than 32 rows 4 %.  Some of them (us, launched from C: whole rows in one part; the best split;
+// what the estimate takes, where that is another):
+//     4 x 8 heads, 1 query, 128 + 64 keys, d 64                5.6     8.0
+//     64 x 8 heads, 1 query, 512 + 128, d 64                   9.8    11.9
+//     16 x 16 heads, 5 queries, 4095 + 333, d 64              24.1    14.4 (4 + 1 parts)
+//     1 x 32 heads of 8, 1 query, 8192 + 512, d 128           61.7    12.9 (16 + 2)   16.5 (whole rows in 32 parts)
+//     64 x 32 heads of 8, 1 query, 8192 + 512, d 128           117    40.2 (16 + 1)
 constexpr double kStepFew = 0.95, kStepFew2 = 1.88, kStepMany = 1.35, kStepMany2 = 2.13;   // QG 1, QG 4; 2: two a CU
 constexpr double kStepMany64 = 0.59;              // QG 4 steps at d = 64 by those at d = 128
 constexpr double kStart = 6.5, kPartial = 1.8e-6, kStream = 5.8e6;   // kStream: bytes a us
