@@ -333,7 +333,7 @@ cf_status cf_rowop(int64_t batch, int64_t M, int64_t N, cf_dtype in,
  *
  * X, R (NULL: 0) and H (NULL: not wanted) are M x N in dtype F32 or BF16,
  * gamma fp32 [N] or NULL (1), Q M x N of code_dtype I8 or FP8_E4M3 (a byte an
- * element, ldq a multiple of 16), s fp32 [M].  1 <= N <= 32768; bytes between N
+ * element, ldq a multiple of 16; cf_gemm_i8 reads I8, E4M3 codes are for the caller's products), s fp32 [M].  1 <= N <= 32768; bytes between N
  * and a leading dimension are neither used nor written.  H may be R itself
  * (same pointer and ld): the residual stream is then updated in place.
  * A row whose t is all zero gets s = 0 and zero codes; a row in which some t
@@ -368,7 +368,9 @@ cf_status cf_rmsnorm_quant(const cf_rmsnorm_quant_args* a, void* hip_stream);
  * bias fp32 [N] or NULL, C M x N in out_dtype F32 or BF16.  The sum is exact (32-bit integers;
  * hence K <= 131056) and its conversion, the scales and act are fp32.
  * Shape rules: K % 16 == 0; 1 <= N <= 2^20, M * N <= 2^37; columns between N and ldc are left as
- * they are.  act: none, GELU (erf), GELU_TANH or RELU.
+ * they are.  act: none, GELU (erf), GELU_TANH or RELU; the GELUs' erf and tanh are off by up to 5e-7, the
+ * output by |x| / 2 times that beside its rounding (about 1e-3 of GELU itself at x = -4, 5e-2 at -5, where it
+ * is -1.4e-6).
  * ------------------------------------------------------------------------ */
 typedef enum { CF_ACT_NONE = 0, CF_ACT_GELU = 1, CF_ACT_GELU_TANH = 2, CF_ACT_RELU = 3 } cf_act;
 

@@ -685,7 +685,14 @@ def rmsnorm_quant(X, R=None, gamma=None, *, eps=1e-5, norm=True, code="int8", re
     E4M3 codes (code="e4m3"); s fp32 [M]; Q * s stands for the normed row.
     norm=False quantises the rows as they are.  H is None without R; `residual`
     names the tensor it goes to, which may be R (in place).  `out` and `scale`
-    take Q and s.  Q is what gemm_i8 takes as its tokens, s as sa.
+    take Q and s.  Q of int8 is what gemm_i8 takes as its tokens, s as sa; E4M3
+    codes are for a product of the caller's own.
+
+    Rows start every multiple of 16 bytes, here and in gemm_i8: a width of whole
+    16 bytes, or rows that are padded to it (views of wider tensors).  Other
+    tensors are refused (CF_ERR_ALIGN), also as outputs.  New outputs of other
+    widths are views of padded rows, which these helpers take as they are and
+    which are not contiguous: .contiguous() packs them.
     """
     here = _here(X, stream)
     if here is None:
@@ -733,7 +740,8 @@ def gemm_i8(A, B, sa=None, sb=None, *, bias=None, act="none", out_dtype=None, ou
     """C = act((A . B^T) * sa[:, None] * sb + bias) of int8 A [M, K] and B [N, K].
 
     sa fp32 [M] or [M, 1] (a scale per token), sb fp32 [N] (per channel), bias fp32 [N];
-    act "none", "gelu", "gelu_tanh" or "relu"; C bf16 (or fp32) [M, N].
+    act "none", "gelu", "gelu_tanh" or "relu"; C bf16 (or fp32) [M, N], its rows padded to whole
+    16 bytes where N is not (as rmsnorm_quant's outputs).  K is a multiple of 16.
     """
     here = _here(A, stream)
     if here is None:

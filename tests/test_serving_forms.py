@@ -61,6 +61,28 @@ def test_normed_large_rows_in_place(N):
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and bool((want[1] > 0).all())
 
 
+# ---------------------------------------------------------------- widths that are no whole 16 bytes
+@gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("N", [1, 30, 333])
+def test_outputs_of_odd_widths(N, dt):
+    """New outputs have padded rows, which the helpers take as they are; contiguous ones are refused."""
+    g = gen(N)
+    A, B = i8(g, 5, 64), i8(g, N, 64)
+    C = cf.gemm_i8(A, B, out_dtype=dt)
+    want = (A.to(F64) @ B.to(F64).t()).to(dt)
+    assert torch.equal(C, want) and C.stride(0) * C.element_size() % 16 == 0 and not C.is_contiguous()
+    assert torch.equal(C.contiguous().view(-1), want.view(-1))
+    Q, s, H = cf.rmsnorm_quant(C, C)
+    z, sr, h = norm_ref(C, C, None, 1e-5, True, "int8")
+    assert bool(((Q.to(F64) - z).abs() <= 0.5 + 4.1 * U * 127).all())
+    assert bool(((s.to(F64) - sr).abs() <= (5 + (3 + 74) / 2) * U * sr).all()) and torch.equal(H, (2 * want.to(F32)).to(dt))
+    for call in (lambda: cf.rmsnorm_quant(want), lambda: cf.gemm_i8(A, B, out=want),
+                 lambda: cf.rmsnorm_quant(C, out=torch.empty((5, N), dtype=torch.int8, device="cuda"))):
+        with pytest.raises(cf.CfError, match="CF_ERR_ALIGN"):
+            call()
+
+
 # ---------------------------------------------------------------- gemm_i8: every tile, K whole and cut
 GEMM_FORMS = [
     (100, 300, 640, "32 x 32 tiles of 256 threads, whole K"), (100, 131, 1008, "32 x 32 tiles of 256 threads, cut K"),
