@@ -242,8 +242,8 @@ hipError_t launch(RmsQuantParams p, hipStream_t st) {
 // chunk): 16384 x 4096 bf16 with residual 80 on 256 threads x 2 chunks, 86 on 512 x 2, 93 on 256 x 4, 115 on
 // 64 x 8; 4096 x 16384 bf16 without 39 on 1024 x 2, 46 on 512 x 4, 69 on 256 x 8; 65536 x 1024 77 on 64 x
 // 2, 117 on 256 x 2; 16384 x 2048 45 on 64 x 4; fp32 8192 x 4096 74 on 512 x 2, 777 x 5120 6.7 on 512 x 4 and 8.2
-// on 1024 x 2.  16384 x 4096 is 470 MB at 5.8 TB/s: with three sets of operands in turn part of it comes
-// from the last-level cache (a large copy reaches 4.8).  One row takes about 4 us, the launch.
+// on 1024 x 2.  16384 x 4096 is 470 MB at 5.9 TB/s, the rate of a large sum of two arrays (5.85;
+// a large read reaches 6.4, a large copy 4.9).  One row takes about 4 us, the launch.
 hipError_t launch_rms_quant(const RmsQuantParams& p, hipStream_t st) {
   if (p.f32) {
     if (p.N <= 256) return launch<float, 64, 1, 256>(p, st);
