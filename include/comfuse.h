@@ -57,13 +57,16 @@ extern "C" {
    the call runs as row clusters, without it (NULL) on whole rows. */
 #define CF_WS_OPTIONAL_BYTES 8917008  /* CF_WS_HEADER_BYTES + 16 */
 #define CF_PREFIX_WS_HEADER_BYTES 262144  /* cf_attention_prefix arrival counters: 65536 words of 4 bytes */
+#define CF_PAGED_WS_HEADER_BYTES 262144   /* cf_attention_paged arrival counters: 65536 words of 4 bytes */
 #define CF_B2B_WS_HEADER_BYTES 1048576  /* split-MLP arrival counters: 262144 words of 4 bytes */
 
 typedef enum {
   CF_F32 = 0,       /* IEEE binary32 */
   CF_BF16 = 1,      /* bfloat16 */
   CF_FP8_E4M3 = 2,  /* OCP E4M3FN: bias 7, max 448, no infinities */
-  CF_I8 = 3         /* two's complement integers of 8 bits */
+  CF_I8 = 3,        /* two's complement integers of 8 bits */
+  CF_I4 = 4,        /* two's complement integers of 4 bits: -8 .. 7 */
+  CF_FP4_E2M1 = 5   /* OCP E2M1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives */
 } cf_dtype;
 
 typedef enum {
@@ -441,6 +444,197 @@ cf_status cf_attention_prefix(const cf_attention_prefix_args* a, void* workspace
 
 /* How a call of these sizes is cut, in words; as cf_gemm_i8_form. */
 const char* cf_attention_prefix_form(const cf_attention_prefix_args* a);
+
+/* ------------------------------------------------------------------------
+ * 4-bit weights.  A weight of N channels by K is kept in tiles of 32 channels
+ * by 64 k, 1024 bytes each, tile (n / 32, k / 64) at byte 1024 ((n / 32)
+ * ceil(K / 64) + k / 64): the order in which the matrix instructions take it, so a
+ * wave reads a tile with one contiguous load.  Within a tile, byte
+ *     16 (32 h + r) + 4 j + b      (h < 2, r < 32, j < 4, b < 4)
+ * holds channel r, k = 16 j + 8 h + 2 b in its low four bits and k + 1 in its
+ * high four.  Codes of channels behind N and of k behind K are zero.
+ * CF_W4_BYTES(N, K) is the size of the whole.  w_dtype: CF_I4 or CF_FP4_E2M1.
+ *
+ * cf_w4_quant  codes of W (N x K, dtype F32 or BF16, K a multiple of `group`,
+ *     `group` a multiple of 32), with a scale per channel and group of k:
+ *         s[k / group, n] = max over the group of |W[n, k]| / qmax   (7 for I4, 6 for E2M1)
+ *     rounded to s_dtype (F32 or BF16), code = nearest value to W / s (ties to even),
+ *     at most qmax in magnitude.  s is K / group rows of N, lds apart (elements).  A
+ *     group of zeros gets s = 0; one with a NaN or an infinity gets s = NaN; both get zero codes.
+ *     Where the scale is subnormal in s_dtype its own rounding adds to the codes'.
+ * cf_w4_pack   codes that exist already into tiles: `codes` has N rows of
+ *     K / 2 bytes, ldc bytes apart, k in the low and k + 1 in the high four
+ *     bits; K a multiple of 32.
+ * Both run once for a weight.  1 <= N <= 2^20, K <= 2^20.
+ * ------------------------------------------------------------------------ */
+#define CF_W4_BYTES(N, K) ((((N) + 31) / 32) * (((K) + 63) / 64) * 1024)
+
+typedef struct {
+  size_t struct_size;            /* = sizeof(cf_w4_quant_args) */
+  int64_t N, K, group;
+  cf_dtype dtype;
+  const void* W; int64_t ldw;
+  cf_dtype w_dtype;
+  void* tiles;
+  cf_dtype s_dtype;
+  void* s; int64_t lds;
+} cf_w4_quant_args;
+
+cf_status cf_w4_quant(const cf_w4_quant_args* a, void* hip_stream);
+
+cf_status cf_w4_pack(int64_t N, int64_t K, const void* codes, int64_t ldc, void* tiles, void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * cf_gemm_w4 — matrix product with 4-bit weights and a scale per group of k:
+ *
+ *     C[m,n] = act(sum_g s[g,n] sum_{k in group g} A[m,k] w[n,k] + bias[n])
+ *
+ * A M x K bf16, W in tiles as above, s K / group rows of N (s_dtype F32 or
+ * BF16, lds elements apart), bias fp32 [N] or NULL, C M x N in out_dtype F32
+ * or BF16.  The codes enter the products as exact bf16 values, the sums of a
+ * group and over the groups and the scales are fp32: no weight is rounded.
+ * Shape rules: group % 32 == 0, K % group == 0, K <= 2^20, 1 <= N <= 2^20,
+ * M * N <= 2^37; columns between N and ldc are left as they are.  act as in cf_gemm_i8.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  size_t struct_size;            /* = sizeof(cf_gemm_w4_args) */
+  int64_t M, N, K, group;
+  const void* A; int64_t lda;
+  cf_dtype w_dtype;
+  const void* W;
+  cf_dtype s_dtype;
+  const void* s; int64_t lds;
+  const float* bias;
+  cf_act act;
+  cf_dtype out_dtype;
+  void* C; int64_t ldc;
+} cf_gemm_w4_args;
+
+cf_status cf_gemm_w4(const cf_gemm_w4_args* a, void* hip_stream);
+
+/* Which kernel form a call of these sizes takes, in words; as cf_gemm_i8_form. */
+const char* cf_gemm_w4_form(const cf_gemm_w4_args* a);
+
+/* ------------------------------------------------------------------------
+ * Cache of pages.  Keys and values of a batch lie in pages of `page` tokens
+ * (a power of two, 16 .. 1024): row l of page p of head h at p, h, l times
+ * the strides (elements; rows have unit stride), d elements of code_dtype
+ *     BF16, or I8 / FP8_E4M3 codes that stand for code * scale, with
+ *     fp32 scales at p, h times their own strides, the page's tokens beside each other.
+ * Strides of rows are multiples of 16 bytes, those of scales multiples of 4
+ * elements; d in {64, 128}.  Slot t of the cache is row t % page of page t / page;
+ * n_pages * page < 2^31.
+ *
+ * cf_cache_write — rotary positions, and the rows of T new tokens into the cache:
+ *
+ *     angle(t, i) = pos[axis(i), t] * freq[i]                   (i < rot / 2)
+ *     (x_i, y_i) -> (x_i cos - y_i sin, y_i cos + x_i sin)      for Q and K
+ *
+ * where pair i is elements i and i + rot / 2 (pairs = CF_PAIRS_HALVES) or 2 i
+ * and 2 i + 1 (CF_PAIRS_NEIGHBOURS); elements from rot on stay as they are.  The first sections[0]
+ * pairs take axis 0, the next sections[1] axis 1, and so on (time, height, width;
+ * text has one axis); the sections of the n_axes <= 4 axes add up to rot / 2.  pos: int32, n_axes
+ * rows of T, ldpos apart; freq: fp32 [rot / 2].  The angle is a product in 64
+ * bits, and so are its cosine and sine, which are then rounded to fp32; the
+ * rotation is in fp32.  rot = 0: no rotation (pos, freq unused); rot is a multiple of 16, <= d.
+ * Q (T x H rows of d, bf16; H = 0: none) comes back rotated in Qo, which may be Q
+ * itself with the same strides.  K and V (T x Hk rows of d, bf16) go to slot
+ * slots[t] (int32): a slot outside [0, n_pages * page) is padding, and not written.
+ * Two tokens of a call must not have the same slot.  Codes: with d_max = max |x| / qmax (127
+ * I8, 448 E4M3) of the fp32 row, scale = d_max and code = the value nearest to
+ * x / d_max (IEEE quotient, ties to even); a row of zeros gets scale 0, one with a NaN
+ * or an infinity scale NaN, and both zero codes.
+ * ------------------------------------------------------------------------ */
+typedef enum { CF_PAIRS_HALVES = 0, CF_PAIRS_NEIGHBOURS = 1 } cf_pairs;
+
+typedef struct {
+  cf_dtype code_dtype;
+  int64_t n_pages, page;
+  void* K; int64_t k_p, k_h, k_l;             /* strides over page, head, row */
+  void* V; int64_t v_p, v_h, v_l;
+  float* Ks; int64_t ks_p, ks_h;              /* scales of 8-bit codes, else NULL */
+  float* Vs; int64_t vs_p, vs_h;
+} cf_cache;
+
+typedef struct {
+  size_t struct_size;            /* = sizeof(cf_cache_write_args) */
+  int64_t T, H, Hk, d;
+  const void* Q; int64_t q_t, q_h;            /* strides over token, head */
+  void* Qo; int64_t qo_t, qo_h;
+  const void* K; int64_t k_t, k_h;
+  const void* V; int64_t v_t, v_h;
+  const int32_t* slots;
+  int64_t rot; cf_pairs pairs;
+  const int32_t* pos; int64_t ldpos;
+  const float* freq;
+  int64_t n_axes, sections[4];
+  cf_cache cache;
+} cf_cache_write_args;
+
+cf_status cf_cache_write(const cf_cache_write_args* a, void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * cf_cache_read — the first lens[b] rows of each sequence as bf16 matrices,
+ * the form in which cf_attention_prefix takes own keys: row j of sequence b
+ * is row j % page of page table[b, j / page].  table: int32, batch rows of
+ * `pages` entries, ldt apart; lens: int32 [batch], clamped to [0, min(S,
+ * pages * page)].  K, V: batch x Hk x S rows of d bf16 with strides over
+ * batch, head and row.  Rows at and behind lens[b], and rows of a page whose
+ * table entry lies outside [0, n_pages), are left as they are.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  size_t struct_size;            /* = sizeof(cf_cache_read_args) */
+  int64_t batch, Hk, S, d;
+  cf_cache cache;
+  const int32_t* table; int64_t ldt, pages;
+  const int32_t* lens;
+  void* K; int64_t k_b, k_h, k_l;
+  void* V; int64_t v_b, v_h, v_l;
+} cf_cache_read_args;
+
+cf_status cf_cache_read(const cf_cache_read_args* a, void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * cf_attention_paged — attention of each sequence's last Lq tokens over its
+ * pages:
+ *
+ *     O_b = softmax(cap(scale Q_b K_b^T)) V_b,   cap(x) = softcap tanh(x / softcap), or x (softcap = 0)
+ *
+ * over the keys j < lens[b] (clamped to [0, pages * page]) of the cache, row
+ * j % page of page table[b, j / page]; keys of a page whose table entry lies
+ * outside [0, n_pages) are not seen.  Q, O: batch x H x Lq rows of d bf16 with
+ * their own strides (multiples of 8 elements); H is a multiple of Hk, query
+ * head h reads key head h / (H / Hk).  causal = 1: query i sees the keys
+ * j < lens[b] - (Lq - 1 - i).  A query that sees no key gets O = 0.  Table entries behind
+ * lens[b] are not read, and rows at and behind it not used, whatever they hold; an infinity or NaN
+ * in a value row that causal hides from some queries of a call only may reach those of them that see
+ * other keys (as 0 * NaN).  1 <= Lq <= 64 (longer parts of a prompt: cf_cache_read and
+ * cf_attention_prefix).  scale finite and > 0, softcap finite and >= 0.  The softmax is exact
+ * (running maximum and sum in fp32); its weights, times the value's scale, are
+ * rounded to bf16 for the second product.
+ * Workspace: cf_attention_paged_workspace() bytes (may be 0), 16-byte aligned:
+ * CF_PAGED_WS_HEADER_BYTES of arrival counters, then partial results.  Zero-fill
+ * the header once before the first call; every call leaves it all zero again,
+ * so later calls of any shape find it valid.  Do not share the workspace with
+ * calls of another kind, and do not let calls that share it overlap in time.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  size_t struct_size;            /* = sizeof(cf_attention_paged_args) */
+  int64_t batch, H, Hk, Lq, d;
+  const void* Q; int64_t q_b, q_h, q_l;
+  cf_cache cache;
+  const int32_t* table; int64_t ldt, pages;
+  const int32_t* lens;
+  int causal;
+  float scale, softcap;
+  void* O; int64_t o_b, o_h, o_l;
+} cf_attention_paged_args;
+
+size_t    cf_attention_paged_workspace(const cf_attention_paged_args* a);
+cf_status cf_attention_paged(const cf_attention_paged_args* a, void* workspace, size_t ws_bytes, void* hip_stream);
+
+/* How a call of these sizes is cut, in words; as cf_gemm_i8_form. */
+const char* cf_attention_paged_form(const cf_attention_paged_args* a);
 
 /* ------------------------------------------------------------------------
  * cf_workspace_check — reads and clears the error word of a workspace used by

@@ -20,17 +20,19 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcomfuse.so")
 
 # ---------------------------------------------------------------- enums
-CF_F32, CF_BF16, CF_FP8_E4M3, CF_I8 = 0, 1, 2, 3
+CF_F32, CF_BF16, CF_FP8_E4M3, CF_I8, CF_I4, CF_FP4_E2M1 = 0, 1, 2, 3, 4, 5
 CF_LAYOUT_KN, CF_LAYOUT_NK = 0, 1
 (CF_N_SCALE, CF_N_BIAS, CF_N_RESIDUAL, CF_N_LAYERNORM, CF_N_RMSNORM, CF_N_GELU,
  CF_N_GELU_TANH, CF_N_RELU, CF_N_STORE, CF_N_ROWAMAX_QUANT, CF_N_SOFTMAX, CF_N_SOFTCAP) = range(12)
 CF_MID_GELU_BIAS, CF_MID_SOFTMAX, CF_MID_RELU_BIAS = 0, 1, 2
 CF_OUT_STORE, CF_OUT_BIAS_RESIDUAL_LN, CF_OUT_BIAS_RELU = 0, 1, 2
 CF_ACT_NONE, CF_ACT_GELU, CF_ACT_GELU_TANH, CF_ACT_RELU = 0, 1, 2, 3
+CF_PAIRS_HALVES, CF_PAIRS_NEIGHBOURS = 0, 1
 PATH_AUTO, PATH_WHOLE_ROW, PATH_CLUSTER, PATH_SPLIT = 0, 1, 2, 3
 CF_WS_HEADER_BYTES = 8916992       # zero-filled start of a row workspace
 CF_WS_OPTIONAL_BYTES = 8917008     # a workspace query's answer where the workspace may be left out
 CF_PREFIX_WS_HEADER_BYTES = 1 << 18   # arrival counters at the start of attention_prefix's workspace
+CF_PAGED_WS_HEADER_BYTES = 1 << 18    # ... of attention_paged's
 CF_B2B_WS_HEADER_BYTES = 1 << 20   # split-MLP arrival counters at the start of its workspace
 STATUS = {0: "CF_OK", 1: "CF_ERR_NULL", 2: "CF_ERR_SHAPE", 3: "CF_ERR_LD", 4: "CF_ERR_ALIGN",
           5: "CF_ERR_DTYPE", 6: "CF_ERR_WORKSPACE", 7: "CF_ERR_UNSUPPORTED", 8: "CF_ERR_ALIAS",
@@ -93,6 +95,44 @@ class AttentionPrefixArgs(C.Structure):
                 ("O", vp), ("o_b", i64), ("o_h", i64), ("o_l", i64)]
 
 
+class W4QuantArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_size_t), ("N", i64), ("K", i64), ("group", i64), ("dtype", C.c_int), ("W", vp),
+                ("ldw", i64), ("w_dtype", C.c_int), ("tiles", vp), ("s_dtype", C.c_int), ("s", vp), ("lds", i64)]
+
+
+class GemmW4Args(C.Structure):
+    _fields_ = [("struct_size", C.c_size_t), ("M", i64), ("N", i64), ("K", i64), ("group", i64), ("A", vp), ("lda", i64),
+                ("w_dtype", C.c_int), ("W", vp), ("s_dtype", C.c_int), ("s", vp), ("lds", i64), ("bias", vp),
+                ("act", C.c_int), ("out_dtype", C.c_int), ("C", vp), ("ldc", i64)]
+
+
+# cf_cache, a member of the structures below
+_CACHE_FIELDS = [("code_dtype", C.c_int), ("n_pages", i64), ("page", i64),
+                 ("cK", vp), ("ck_p", i64), ("ck_h", i64), ("ck_l", i64), ("cV", vp), ("cv_p", i64), ("cv_h", i64),
+                 ("cv_l", i64), ("cKs", vp), ("cks_p", i64), ("cks_h", i64), ("cVs", vp), ("cvs_p", i64), ("cvs_h", i64)]
+
+
+class CacheWriteArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_size_t), ("T", i64), ("H", i64), ("Hk", i64), ("d", i64),
+                ("Q", vp), ("q_t", i64), ("q_h", i64), ("Qo", vp), ("qo_t", i64), ("qo_h", i64),
+                ("K", vp), ("k_t", i64), ("k_h", i64), ("V", vp), ("v_t", i64), ("v_h", i64), ("slots", vp),
+                ("rot", i64), ("pairs", C.c_int), ("pos", vp), ("ldpos", i64), ("freq", vp), ("n_axes", i64),
+                ("section0", i64), ("section1", i64), ("section2", i64), ("section3", i64)] + _CACHE_FIELDS
+
+
+class CacheReadArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_size_t), ("batch", i64), ("Hk", i64), ("S", i64), ("d", i64)] + _CACHE_FIELDS + [
+                ("table", vp), ("ldt", i64), ("pages", i64), ("lens", vp),
+                ("K", vp), ("k_b", i64), ("k_h", i64), ("k_l", i64), ("V", vp), ("v_b", i64), ("v_h", i64), ("v_l", i64)]
+
+
+class AttentionPagedArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_size_t), ("batch", i64), ("H", i64), ("Hk", i64), ("Lq", i64), ("d", i64),
+                ("Q", vp), ("q_b", i64), ("q_h", i64), ("q_l", i64)] + _CACHE_FIELDS + [
+                ("table", vp), ("ldt", i64), ("pages", i64), ("lens", vp), ("causal", C.c_int), ("scale", C.c_float),
+                ("softcap", C.c_float), ("O", vp), ("o_b", i64), ("o_h", i64), ("o_l", i64)]
+
+
 class CfError(RuntimeError):
     def __init__(self, status, detail):
         self.status = status
@@ -132,15 +172,20 @@ def lib():
                 L.cf_rowop.argtypes = [i64, i64, i64, C.c_int, vp, i64, i64, C.POINTER(Node), C.c_int, vp]
                 L.cf_gemm_subgraph_noalloc.restype = C.c_int
                 L.cf_gemm_subgraph_noalloc.argtypes = [C.POINTER(SubgraphArgs), vp]
-                for name, ws in [("cf_rmsnorm_quant", False), ("cf_gemm_i8", False), ("cf_attention_prefix", True)]:
+                for name, ws in [("cf_rmsnorm_quant", False), ("cf_gemm_i8", False), ("cf_attention_prefix", True),
+                                 ("cf_w4_quant", False), ("cf_gemm_w4", False), ("cf_cache_write", False),
+                                 ("cf_cache_read", False), ("cf_attention_paged", True)]:
                     f = getattr(L, name)
                     f.restype = C.c_int
                     f.argtypes = [vp, vp, C.c_size_t, vp] if ws else [vp, vp]   # arguments: byref or packed bytes
-                for name in ("cf_gemm_i8_form", "cf_attention_prefix_form"):
+                L.cf_w4_pack.restype = C.c_int
+                L.cf_w4_pack.argtypes = [i64, i64, vp, i64, vp, vp]
+                for name in ("cf_gemm_i8_form", "cf_attention_prefix_form", "cf_gemm_w4_form", "cf_attention_paged_form"):
                     getattr(L, name).restype = C.c_char_p
                     getattr(L, name).argtypes = [vp]
-                L.cf_attention_prefix_workspace.restype = C.c_size_t
-                L.cf_attention_prefix_workspace.argtypes = [vp]
+                for name in ("cf_attention_prefix_workspace", "cf_attention_paged_workspace"):
+                    getattr(L, name).restype = C.c_size_t
+                    getattr(L, name).argtypes = [vp]
                 L.cf_workspace_check.restype = C.c_int
                 L.cf_workspace_check.argtypes = [vp, C.c_size_t, vp]
                 _lib = L
@@ -217,6 +262,42 @@ def cf_attention_prefix_form(args):
     return lib().cf_attention_prefix_form(C.byref(args)).decode()
 
 
+def cf_w4_quant(args, stream):
+    return lib().cf_w4_quant(C.byref(args), stream)
+
+
+def cf_w4_pack(*args):
+    return lib().cf_w4_pack(*args)
+
+
+def cf_gemm_w4(args, stream):
+    return lib().cf_gemm_w4(C.byref(args), stream)
+
+
+def cf_gemm_w4_form(args):
+    return lib().cf_gemm_w4_form(C.byref(args)).decode()
+
+
+def cf_cache_write(args, stream):
+    return lib().cf_cache_write(C.byref(args), stream)
+
+
+def cf_cache_read(args, stream):
+    return lib().cf_cache_read(C.byref(args), stream)
+
+
+def cf_attention_paged(args, workspace, ws_bytes, stream):
+    return lib().cf_attention_paged(C.byref(args), workspace, ws_bytes, stream)
+
+
+def cf_attention_paged_workspace(args):
+    return lib().cf_attention_paged_workspace(C.byref(args))
+
+
+def cf_attention_paged_form(args):
+    return lib().cf_attention_paged_form(C.byref(args)).decode()
+
+
 def cf_workspace_check(workspace, ws_bytes, stream):
     return lib().cf_workspace_check(workspace, ws_bytes, stream)
 
@@ -283,7 +364,8 @@ def _graph_workspace(nbytes, key, device, stream):
     capture = _capture_id(stream)
     have = _ws_graph.get(key)
     if have is None or capture is None or have[0] != capture or have[1].numel() < nbytes:
-        header = {"rows": CF_WS_HEADER_BYTES, "b2b": CF_B2B_WS_HEADER_BYTES, "prefix": CF_PREFIX_WS_HEADER_BYTES}[key[2]]
+        header = {"rows": CF_WS_HEADER_BYTES, "b2b": CF_B2B_WS_HEADER_BYTES, "prefix": CF_PREFIX_WS_HEADER_BYTES,
+                  "paged": CF_PAGED_WS_HEADER_BYTES}[key[2]]
         with torch.cuda.stream(stream):
             ws = torch.empty(max(nbytes, header), dtype=torch.uint8, device=device)
             ws[:header].view(torch.int32).zero_()
@@ -297,8 +379,8 @@ def workspace(nbytes, device, stream=None, kind="rows"):
     share it; calls on different streams get different workspaces (the
     row-cluster round counters live in it).  kind "b2b" is that of the split
     MLP and of attention with split keys (their arrival counters must not meet
-    another entry point's data), "prefix" that of attention_prefix, for the same
-    reason.  Calls captured into a graph share one of the
+    another entry point's data), "prefix" that of attention_prefix and "paged" that of
+    attention_paged, for the same reason.  Calls captured into a graph share one of the
     capture's own, never an eager one: a graph outlives what the cache holds,
     and its replays may overlap eager calls or another graph."""
     torch = _torch()
@@ -779,16 +861,16 @@ _prefix_lock = threading.Lock()   # threads that share a stream share its worksp
 
 
 def _prefix_workspace(torch, need, device, key):
-    """workspace(need, device, kind="prefix") at less cost: cached per device and stream while nothing is captured.
+    """workspace(need, device, kind=key[2]) at less cost: cached per device and stream while nothing is captured.
     A new one is half as large again as the last, so that a batch that grows step by step seldom needs it, and only
     its counters are cleared."""
     if torch._C._cuda_isCurrentStreamCapturing():
-        return workspace(need, device, None, kind="prefix")
+        return workspace(need, device, None, kind=key[2])
     ws = _ws_cache.get(key)
     if ws is None or ws.numel() < need:
         size = max(need, 1 << 20 if ws is None else ws.numel() * 3 // 2)
         ws = torch.empty(size, dtype=torch.uint8, device=device)
-        ws[:CF_PREFIX_WS_HEADER_BYTES].view(torch.int32).zero_()
+        ws[:CF_PREFIX_WS_HEADER_BYTES].view(torch.int32).zero_()   # attention_paged's counters are as many
         _ws_cache[key] = ws
     return ws
 
@@ -855,6 +937,305 @@ def attention_prefix(Q, Kp, Vp, Ks=None, Vs=None, lens=None, *, causal=False, sc
         if ws.dtype is not torch.uint8 or not ws.is_contiguous() or ws.get_device() != device:
             raise ValueError("ws: expected a contiguous uint8 tensor beside the other operands")
         status = L.cf_attention_prefix(a, ws.data_ptr(), ws.numel(), raw)
+    if status:
+        _check(status)
+    return O
+
+
+# ---------------------------------------------------------------- 4-bit weights
+_CODES4 = {"int4": CF_I4, "e2m1": CF_FP4_E2M1}
+_W4_QUANT, _GEMM_W4, _CACHE_WRITE, _CACHE_READ, _PAGED = (
+    struct.Struct("@" + "".join(_FORMATS[f] for _, f in t._fields_))
+    for t in (W4QuantArgs, GemmW4Args, CacheWriteArgs, CacheReadArgs, AttentionPagedArgs))
+
+
+def _tiles(N, K):
+    return -(-N // 32), -(-K // 64), 1024
+
+
+def w4_quant(W, group=128, *, code="int4", scales=None, stream=None):
+    """(tiles, s): W [N, K] (bf16 or fp32) as 4-bit codes with a scale per channel and `group` k.
+
+    code "int4" (s = max / 7) or "e2m1" (OCP 4-bit floating point, s = max / 6); `group` is a multiple
+    of 32 that divides K.  s [K / group, N] is fp32, or of the type `scales`
+    (torch.bfloat16: the codes are taken by the rounded scale).  tiles: uint8
+    [ceil(N / 32), ceil(K / 64), 1024], as gemm_w4 takes them.  Done once for a weight.
+    """
+    here = _here(W, stream)
+    if here is None:
+        return _elsewhere(w4_quant, W, stream, group, code=code, scales=scales)
+    L, torch, device, raw = here
+    N, K = W.shape
+    size = W.element_size()
+    sdt = torch.float32 if scales is None else scales
+    if sdt not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"unsupported dtype {sdt}")
+    if group <= 0 or K % group:
+        raise ValueError(f"group: expected a divisor of {K}, got {group}")
+    w = torch.empty(_tiles(N, K), dtype=torch.uint8, device=W.device)
+    s = torch.empty(K // group, N, dtype=sdt, device=W.device)
+    a = _W4_QUANT.pack(_W4_QUANT.size, N, K, group, _dt(W), W.data_ptr(), _row_ld(W, N, K, size),
+                       _choice(_CODES4, code, "code"), w.data_ptr(), _dt(s), s.data_ptr(), N)
+    _check(L.cf_w4_quant(a, raw))
+    return w, s
+
+
+def w4_pack(codes, stream=None):
+    """Tiles, as gemm_w4 takes them, of 4-bit codes [N, K / 2] (uint8: k in the low four bits, k + 1 in the
+    high ones); K is a multiple of 32.  Done once for a weight."""
+    here = _here(codes, stream)
+    if here is None:
+        return _elsewhere(w4_pack, codes, stream)
+    L, torch, device, raw = here
+    if codes.dtype is not torch.uint8:
+        raise TypeError(f"expected uint8 codes, got {codes.dtype}")
+    N, K = codes.size(0), 2 * codes.size(1)
+    if codes.stride(1) != 1:
+        raise ValueError("expected a 2-D tensor with unit column stride")
+    w = torch.empty(_tiles(N, K), dtype=torch.uint8, device=codes.device)
+    _check(L.cf_w4_pack(N, K, codes.data_ptr(), codes.stride(0), w.data_ptr(), raw))
+    return w
+
+
+def gemm_w4(A, W, s, *, code="int4", bias=None, act="none", out_dtype=None, out=None, stream=None):
+    """C = act(A . w^T + bias) with 4-bit weights w[n, k] = s[k / group, n] * value(code[n, k]).
+
+    A [M, K] bf16; W the tiles of w4_quant or w4_pack; s [K / group, N] bf16 or fp32,
+    its rows any distance apart; code "int4" or "e2m1"; bias fp32 [N]; act "none", "gelu",
+    "gelu_tanh" or "relu"; C bf16 (or fp32) [M, N], its rows padded to whole 16 bytes where N is not
+    (as rmsnorm_quant's outputs).
+    """
+    here = _here(A, stream)
+    if here is None:
+        return _elsewhere(gemm_w4, A, stream, W, s, code=code, bias=bias, act=act, out_dtype=out_dtype, out=out)
+    L, torch, device, raw = here
+    bf16, f32 = torch.bfloat16, torch.float32
+    M, K = A.shape
+    ng, N = s.shape
+    if A.dtype is not bf16:
+        raise TypeError(f"expected bf16 tokens, got {A.dtype}")
+    if ng == 0 or K % ng:
+        raise ValueError(f"s: expected [K / group, N], got {tuple(s.shape)} for K = {K}")
+    if W.shape != _tiles(N, K) or W.dtype is not torch.uint8 or W.get_device() != device or not W.is_contiguous():
+        _like(W, _tiles(N, K), torch.uint8, device, "W")
+        raise ValueError("W: expected contiguous tiles")
+    if s.get_device() != device or (s.stride(1) != 1 and N > 1):
+        raise ValueError("s: expected rows of unit stride beside the other operands")
+    if out is None:
+        dt = CF_F32 if out_dtype is f32 else CF_BF16
+        if dt == CF_BF16 and out_dtype not in (None, bf16):
+            raise TypeError(f"unsupported dtype {out_dtype}")
+        Cm, ldc = _rows(torch, M, N, f32 if dt == CF_F32 else bf16, A.device, 4 if dt == CF_F32 else 2)
+    else:
+        dt, Cm = _dt(out), _like(out, (M, N), out_dtype or out.dtype, device, "out")
+        ldc = _row_ld(Cm, M, N, 4 if dt == CF_F32 else 2)
+    a = _GEMM_W4.pack(_GEMM_W4.size, M, N, K, K // ng, A.data_ptr(),
+                      K if K % 8 == 0 and A.is_contiguous() else _row_ld(A, M, K, 2),
+                      _choice(_CODES4, code, "code"), W.data_ptr(), CF_BF16 if s.dtype is bf16 else _dt(s), s.data_ptr(),
+                      s.stride(0), 0 if bias is None else _vector(bias, N, f32, device, "bias"),
+                      CF_ACT_NONE if act == "none" else _choice(_ACTS, act, "act"), dt, Cm.data_ptr(), ldc)
+    status = L.cf_gemm_w4(a, raw)
+    if status:
+        _check(status)
+    return Cm
+
+
+# ---------------------------------------------------------------- cache of pages
+# Kc, Vc [n_pages, Hk, page, d]: bf16, or int8 or E4M3 codes (uint8 or torch.float8_e4m3fn) with fp32 scales Ks,
+# Vs [n_pages, Hk, page]; pages of a power of two of 16 to 1024 tokens, d 64 or 128.  Any strides that are multiples of 16
+# bytes with unit innermost stride (pages stored token-major are passed as transposed views); the scales of a page's
+# tokens lie beside each other.  Slot t is row t % page of page t // page.
+def cache_pages(n_pages, Hk, page, d, code="bf16", device="cuda"):
+    """(Kc, Vc, Ks, Vs) for a new cache, zero; code "bf16" (Ks, Vs None), "int8" or "e4m3"."""
+    torch = _torch()
+    dtypes = {"bf16": torch.bfloat16, "int8": torch.int8, "e4m3": torch.uint8}
+    dtype = _choice(dtypes, code, "code")
+    rows = [torch.zeros(n_pages, Hk, page, d, dtype=dtype, device=device) for _ in range(2)]
+    if code == "bf16":
+        return (*rows, None, None)
+    return (*rows, *(torch.zeros(n_pages, Hk, page, dtype=torch.float32, device=device) for _ in range(2)))
+
+
+def _cache(torch, Kc, Vc, Ks, Vs, Hk, d, device):
+    """The fields of cf_cache."""
+    dtype, shape = Kc.dtype, Kc.shape
+    dt = (CF_BF16 if dtype is torch.bfloat16 else CF_I8 if dtype is torch.int8 else
+          CF_FP8_E4M3 if dtype in (torch.uint8, torch.float8_e4m3fn) else None)
+    if dt is None:
+        raise TypeError(f"Kc: expected bf16, int8 or E4M3 pages, got {dtype}")
+    if len(shape) != 4 or shape[1] != Hk or shape[3] != d:
+        raise ValueError(f"Kc: expected [n_pages, {Hk}, page, {d}], got {tuple(shape)}")
+    if Vc.dtype is not dtype or Vc.shape != shape or Kc.get_device() != device or Vc.get_device() != device:
+        _like(Kc, shape, dtype, device, "Kc")
+        _like(Vc, shape, dtype, device, "Vc")
+    k, v = Kc.stride(), Vc.stride()
+    if not k[3] == v[3] == 1:
+        raise ValueError("expected unit innermost strides")
+    if dt == CF_BF16:
+        if Ks is not None or Vs is not None:
+            raise ValueError("bf16 pages have no scales")
+        return dt, shape[0], shape[2], Kc.data_ptr(), k[0], k[1], k[2], Vc.data_ptr(), v[0], v[1], v[2], 0, 0, 0, 0, 0, 0
+    if Ks is None or Vs is None:
+        raise ValueError("8-bit pages come with the scales Ks and Vs")
+    f32 = torch.float32
+    if not (Ks.dtype is Vs.dtype is f32 and Ks.shape == Vs.shape == shape[:3] and Ks.get_device() == Vs.get_device() == device):
+        _like(Ks, shape[:3], f32, device, "Ks")
+        _like(Vs, shape[:3], f32, device, "Vs")
+    ks, vs = Ks.stride(), Vs.stride()
+    if not ks[2] == vs[2] == 1:
+        raise ValueError("expected unit innermost strides")
+    return (dt, shape[0], shape[2], Kc.data_ptr(), k[0], k[1], k[2], Vc.data_ptr(), v[0], v[1], v[2],
+            Ks.data_ptr(), ks[0], ks[1], Vs.data_ptr(), vs[0], vs[1])
+
+
+def _ints(t, shape, device, name):
+    """t, checked to hold int32 values of a shape with unit innermost stride on `device`."""
+    if t.dim() != len(shape) or t.get_device() != device or t.stride(-1) != 1 and t.shape[-1] > 1 or str(t.dtype) != "torch.int32" \
+            or t.shape != shape:
+        raise ValueError(f"{name}: expected int32 {tuple(shape)} with unit innermost stride beside the other operands, got "
+                         f"{tuple(t.shape)} of {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+_PAIRS = {"halves": CF_PAIRS_HALVES, "neighbours": CF_PAIRS_NEIGHBOURS}
+
+
+def cache_write(K, V, slots, Kc, Vc, Ks=None, Vs=None, *, q=None, pos=None, freq=None, sections=None, pairs="halves",
+                out=None, stream=None):
+    """Write the rows K, V [T, Hk, d] of T new tokens (bf16) to slots [T] (int32) of the cache, after rotary
+    positions; returns the queries q [T, H, d], rotated as the keys are (None without q).
+
+    A slot outside the cache is padding, and not written; the slots of a call differ.  pos int32
+    [T], or [axes, T] where a pair takes its angle from one of up to four axes (time, height, width): the
+    first sections[0] pairs from axis 0, the next sections[1] from axis 1.  Pair i turns by pos * freq[i];
+    freq fp32 [rot / 2], rot <= d a multiple of 16, elements from rot on stay as they are.  pairs "halves":
+    elements i and i + rot / 2; "neighbours": 2 i and 2 i + 1.  Without pos nothing is rotated.
+    `out` takes the queries, and may be q (in place).  8-bit codes: see rmsnorm_quant; each row has its scale.
+    """
+    here = _here(K, stream)
+    if here is None:
+        return _elsewhere(cache_write, K, stream, V, slots, Kc, Vc, Ks, Vs, q=q, pos=pos, freq=freq, sections=sections,
+                          pairs=pairs, out=out)
+    L, torch, device, raw = here
+    bf16, shape = torch.bfloat16, K.shape
+    T, Hk, d = shape
+    if not (K.dtype is V.dtype is bf16 and V.shape == shape and V.get_device() == device):
+        _like(K, shape, bf16, device, "K")
+        _like(V, shape, bf16, device, "V")
+    k, v = K.stride(), V.stride()
+    if not k[2] == v[2] == 1:
+        raise ValueError("expected unit innermost strides")
+    H, Q, qs, os_ = 0, None, (0, 0), (0, 0)
+    if q is not None:
+        H = q.size(1)
+        _like(q, (T, H, d), bf16, device, "q")
+        Q = torch.empty((T, H, d), dtype=bf16, device=K.device) if out is None else _like(out, (T, H, d), bf16, device, "out")
+        qs, os_ = q.stride(), Q.stride()
+        if not qs[2] == os_[2] == 1:
+            raise ValueError("expected unit innermost strides")
+    elif out is not None:
+        raise ValueError("out comes with q")
+    rot = n_axes = ldpos = pp = fp = 0
+    sec = (0, 0, 0, 0)
+    if (pos is None) != (freq is None):
+        raise ValueError("pos and freq come together")
+    if pos is not None:
+        rot = 2 * freq.numel()
+        fp = _vector(freq, rot // 2, torch.float32, device, "freq")
+        n_axes = 1 if pos.dim() == 1 else pos.size(0)
+        pp = _ints(pos, (T,) if pos.dim() == 1 else (n_axes, T), device, "pos")
+        ldpos = pos.stride(0) if n_axes > 1 else T
+        if sections is None and n_axes == 1:
+            sections = (rot // 2,)
+        if sections is None or len(sections) != n_axes or n_axes > 4:
+            raise ValueError(f"sections: expected one for each of up to 4 axes, got {sections}")
+        sec = (*sections, 0, 0, 0)[:4]
+    a = _CACHE_WRITE.pack(_CACHE_WRITE.size, T, H, Hk, d, 0 if q is None else q.data_ptr(), qs[0], qs[1],
+                          0 if Q is None else Q.data_ptr(), os_[0], os_[1], K.data_ptr(), k[0], k[1], V.data_ptr(), v[0], v[1],
+                          _ints(slots, (T,), device, "slots"), rot, _choice(_PAIRS, pairs, "pairs"), pp, ldpos, fp, n_axes, *sec,
+                          *_cache(torch, Kc, Vc, Ks, Vs, Hk, d, device))
+    status = L.cf_cache_write(a, raw)
+    if status:
+        _check(status)
+    return Q
+
+
+def cache_read(Kc, Vc, table, lens, Ks=None, Vs=None, *, S=None, out=None, stream=None):
+    """(K, V) [B, Hk, S, d] bf16: the first lens[b] rows of each sequence, row j from page table[b, j // page].
+
+    table int32 [B, pages], lens int32 [B].  S: by default what the table's pages hold.  Rows behind lens[b] (and
+    of pages that the cache has not) are left as they are in `out`, a pair of tensors, and hold anything in new ones;
+    attention_prefix takes K, V and lens as a batch's own keys.
+    """
+    here = _here(Kc, stream)
+    if here is None:
+        return _elsewhere(cache_read, Kc, stream, Vc, table, lens, Ks, Vs, S=S, out=out)
+    L, torch, device, raw = here
+    bf16 = torch.bfloat16
+    _, Hk, page, d = Kc.shape
+    B, pages = table.shape
+    if out is None:
+        S = pages * page if S is None else S
+        K, V = (torch.empty((B, Hk, S, d), dtype=bf16, device=Kc.device) for _ in range(2))
+    else:
+        K, V = out
+        S = K.size(2) if S is None else S
+        _like(K, (B, Hk, S, d), bf16, device, "out")
+        _like(V, (B, Hk, S, d), bf16, device, "out")
+    k, v = K.stride(), V.stride()
+    if not k[3] == v[3] == 1:
+        raise ValueError("expected unit innermost strides")
+    a = _CACHE_READ.pack(_CACHE_READ.size, B, Hk, S, d, *_cache(torch, Kc, Vc, Ks, Vs, Hk, d, device),
+                         _ints(table, (B, pages), device, "table"), table.stride(0), pages, _ints(lens, (B,), device, "lens"),
+                         K.data_ptr(), k[0], k[1], k[2], V.data_ptr(), v[0], v[1], v[2])
+    status = L.cf_cache_read(a, raw)
+    if status:
+        _check(status)
+    return K, V
+
+
+def attention_paged(Q, Kc, Vc, table, lens, Ks=None, Vs=None, *, causal=False, scale=None, softcap=0.0, out=None, ws=None,
+                    stream=None):
+    """O = softmax(cap(scale * Q K^T)) V over the first lens[b] keys of each sequence's pages; cap(x) = softcap *
+    tanh(x / softcap), or x where softcap is 0.
+
+    Q [B, H, Lq, d] bf16, Lq up to 64, H a multiple of Hk; table int32 [B, pages], lens int32 [B] (the new tokens
+    among them: cache_write comes first).  causal: query i sees the keys j < lens[b] - (Lq - 1 - i).  A
+    query that sees no key gets 0; keys of a page that the cache has not are not seen.  ws: a
+    workspace of the caller's own (uint8, cf_attention_paged_workspace bytes, its first CF_PAGED_WS_HEADER_BYTES
+    zero before its first use).
+    """
+    here = _here(Q, stream)
+    if here is None:
+        return _elsewhere(attention_paged, Q, stream, Kc, Vc, table, lens, Ks, Vs, causal=causal, scale=scale,
+                          softcap=softcap, out=out, ws=ws)
+    L, torch, device, raw = here
+    bf16 = torch.bfloat16
+    shape = Q.shape
+    B, H, Lq, d = shape
+    if Q.dtype is not bf16:
+        _like(Q, shape, bf16, device, "Q")
+    O = torch.empty_like(Q) if out is None else _like(out, shape, bf16, device, "out")
+    q, o = Q.stride(), O.stride()
+    if not q[3] == o[3] == 1:
+        raise ValueError("expected unit innermost strides")
+    pages = table.size(1)
+    Hk = Kc.size(1)
+    a = _PAGED.pack(_PAGED.size, B, H, Hk, Lq, d, Q.data_ptr(), q[0], q[1], q[2],
+                    *_cache(torch, Kc, Vc, Ks, Vs, Hk, d, device), _ints(table, (B, pages), device, "table"), table.stride(0), pages,
+                    _ints(lens, (B,), device, "lens"), 1 if causal else 0, d ** -0.5 if scale is None else scale, softcap,
+                    O.data_ptr(), o[0], o[1], o[2])
+    need = 0 if ws is not None else L.cf_attention_paged_workspace(a)
+    if need:
+        with _prefix_lock:
+            ws = _prefix_workspace(torch, need, Q.device, (device, raw, "paged"))
+            status = L.cf_attention_paged(a, ws.data_ptr(), ws.numel(), raw)
+    elif ws is None:
+        status = L.cf_attention_paged(a, None, 0, raw)
+    else:
+        if ws.dtype is not torch.uint8 or not ws.is_contiguous() or ws.get_device() != device:
+            raise ValueError("ws: expected a contiguous uint8 tensor beside the other operands")
+        status = L.cf_attention_paged(a, ws.data_ptr(), ws.numel(), raw)
     if status:
         _check(status)
     return O

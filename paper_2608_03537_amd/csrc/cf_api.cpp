@@ -1320,4 +1320,434 @@ cf_status cf_attention_prefix(const cf_attention_prefix_args* a, void* workspace
   }
 }
 
+// Scales of 4-bit weights: K / group rows of N values.
+static cf_status check_w4(int64_t N, int64_t K, int64_t group, cf_dtype w, cf_dtype st, int64_t lds) {
+  if (N <= 0 || N > (int64_t)1 << 20 || K <= 0 || K > (int64_t)1 << 20) return fail(CF_ERR_SHAPE, "need 0 < N, K <= 2^20");
+  if (group <= 0 || group % 32 != 0 || K % group != 0)
+    return fail(CF_ERR_SHAPE, "group = %lld must be a multiple of 32 that divides K = %lld", (long long)group, (long long)K);
+  if (w != CF_I4 && w != CF_FP4_E2M1) return fail(CF_ERR_DTYPE, "w_dtype must be I4 or FP4_E2M1");
+  if (st != CF_F32 && st != CF_BF16) return fail(CF_ERR_DTYPE, "s_dtype must be F32 or BF16");
+  if (K / group > 1 && (lds < N || lds > (int64_t)1 << 40)) return fail(CF_ERR_LD, "s: leading dimension %lld < %lld, or too large", (long long)lds, (long long)N);
+  return CF_OK;
+}
+static cf_status check_scales(const void* s, cf_dtype st) {
+  if (!s) return fail(CF_ERR_NULL, "s is NULL");
+  if (reinterpret_cast<uintptr_t>(s) % dsize(st) != 0) return fail(CF_ERR_ALIGN, "s is not aligned to its elements");
+  return CF_OK;
+}
+static cf_status check_tiles(const char* name, const void* p) {
+  if (!p) return fail(CF_ERR_NULL, "%s is NULL", name);
+  if (!aligned16(p)) return fail(CF_ERR_ALIGN, "%s is not 16-byte aligned", name);
+  return CF_OK;
+}
+
+cf_status cf_w4_quant(const cf_w4_quant_args* a, void* hip_stream) {
+  try {
+    if (!a) return fail(CF_ERR_NULL, "args is NULL");
+    if (a->struct_size != sizeof(cf_w4_quant_args))
+      return fail(CF_ERR_STRUCT, "struct_size %zu != %zu", a->struct_size, sizeof(cf_w4_quant_args));
+    cf_status s = check_w4(a->N, a->K, a->group, a->w_dtype, a->s_dtype, a->lds);
+    if (s != CF_OK) return s;
+    if (a->dtype != CF_F32 && a->dtype != CF_BF16) return fail(CF_ERR_DTYPE, "dtype must be F32 or BF16");
+    if ((s = check_matrix("W", a->W, a->N, a->K, a->ldw, a->dtype, true)) != CF_OK ||
+        (s = check_tiles("tiles", a->tiles)) != CF_OK || (s = check_scales(a->s, a->s_dtype)) != CF_OK)
+      return s;
+    if (outputs_alias(a->tiles, {a->W, a->s}) || outputs_alias(a->s, {a->W})) return fail(CF_ERR_ALIAS, "an output aliases another operand");
+    W4QuantParams p{};
+    p.N = (int)a->N;
+    p.K = (int)a->K;
+    p.group = (int)a->group;
+    p.f32 = a->dtype == CF_F32;
+    p.e2m1 = a->w_dtype == CF_FP4_E2M1;
+    p.W = a->W;
+    p.ldw = a->ldw;
+    p.tiles = reinterpret_cast<uint8_t*>(a->tiles);
+    p.s = a->s;
+    p.lds = a->lds;
+    p.s_f32 = a->s_dtype == CF_F32;
+    return hip_status(launch_w4_quant(p, reinterpret_cast<hipStream_t>(hip_stream)), "4-bit quantisation launch");
+  } catch (...) {
+    return fail(CF_ERR_HIP, "internal error");
+  }
+}
+
+cf_status cf_w4_pack(int64_t N, int64_t K, const void* codes, int64_t ldc, void* tiles, void* hip_stream) {
+  try {
+    if (N <= 0 || N > (int64_t)1 << 20 || K <= 0 || K > (int64_t)1 << 20 || K % 32 != 0)
+      return fail(CF_ERR_SHAPE, "need 0 < N, K <= 2^20, K a multiple of 32");
+    if (!codes) return fail(CF_ERR_NULL, "codes is NULL");
+    if (N > 1 && (ldc < K / 2 || ldc > (int64_t)1 << 40)) return fail(CF_ERR_LD, "codes: %lld bytes a row, need %lld", (long long)ldc, (long long)(K / 2));
+    const cf_status s = check_tiles("tiles", tiles);
+    if (s != CF_OK) return s;
+    if (outputs_alias(tiles, {codes})) return fail(CF_ERR_ALIAS, "tiles aliases codes");
+    return hip_status(launch_w4_pack((int)N, (int)K, reinterpret_cast<const uint8_t*>(codes), ldc,
+                                     reinterpret_cast<uint8_t*>(tiles), reinterpret_cast<hipStream_t>(hip_stream)),
+                      "4-bit packing launch");
+  } catch (...) {
+    return fail(CF_ERR_HIP, "internal error");
+  }
+}
+
+// Sizes only: what the form depends on.
+static cf_status gemm_w4_sizes(const cf_gemm_w4_args* a, GemmW4Params& p) {
+  if (!a) return fail(CF_ERR_NULL, "args is NULL");
+  if (a->struct_size != sizeof(cf_gemm_w4_args))
+    return fail(CF_ERR_STRUCT, "struct_size %zu != %zu", a->struct_size, sizeof(cf_gemm_w4_args));
+  const cf_status s = check_w4(a->N, a->K, a->group, a->w_dtype, a->s_dtype, a->lds);
+  if (s != CF_OK) return s;
+  if (a->M < 0 || a->M > (int64_t)1 << 30) return fail(CF_ERR_SHAPE, "need 0 <= M <= 2^30");
+  if (a->M * a->N > (int64_t)1 << 37) return fail(CF_ERR_SHAPE, "M * N exceeds 2^37");
+  p = GemmW4Params{};
+  p.M = (int)a->M;
+  p.N = (int)a->N;
+  p.K = (int)a->K;
+  p.group = (int)a->group;
+  p.e2m1 = a->w_dtype == CF_FP4_E2M1;
+  p.s_f32 = a->s_dtype == CF_F32;
+  return CF_OK;
+}
+
+const char* cf_gemm_w4_form(const cf_gemm_w4_args* a) {
+  try {
+    GemmW4Params p;
+    if (gemm_w4_sizes(a, p) != CF_OK || p.M == 0) return "";
+    gemm_w4_form(p, g_form, sizeof(g_form));
+    return g_form;
+  } catch (...) {
+    return "";
+  }
+}
+
+cf_status cf_gemm_w4(const cf_gemm_w4_args* a, void* hip_stream) {
+  try {
+    GemmW4Params p;
+    cf_status s = gemm_w4_sizes(a, p);
+    if (s != CF_OK) return s;
+    if (a->out_dtype != CF_F32 && a->out_dtype != CF_BF16) return fail(CF_ERR_DTYPE, "out_dtype must be F32 or BF16");
+    if (a->act != CF_ACT_NONE && a->act != CF_ACT_GELU && a->act != CF_ACT_GELU_TANH && a->act != CF_ACT_RELU)
+      return fail(CF_ERR_UNSUPPORTED, "unknown act");
+    if ((s = check_matrix("A", a->A, a->M, a->K, a->lda, CF_BF16, true)) != CF_OK ||
+        (s = check_matrix("C", a->C, a->M, a->N, a->ldc, a->out_dtype, true)) != CF_OK || (s = check_vec("bias", a->bias)) != CF_OK)
+      return s;
+    if (a->M == 0) return CF_OK;
+    if ((s = check_tiles("W", a->W)) != CF_OK || (s = check_scales(a->s, a->s_dtype)) != CF_OK) return s;
+    if (outputs_alias(a->C, {a->A, a->W, a->s, a->bias})) return fail(CF_ERR_ALIAS, "C aliases an input");
+    p.A = reinterpret_cast<const uint16_t*>(a->A);
+    p.lda = a->lda;
+    p.W = reinterpret_cast<const uint8_t*>(a->W);
+    p.s = a->s;
+    p.lds = a->lds;
+    p.bias = a->bias;
+    p.act = a->act;
+    p.C = a->C;
+    p.ldc = a->ldc;
+    p.c_f32 = a->out_dtype == CF_F32;
+    return hip_status(launch_gemm_w4(p, reinterpret_cast<hipStream_t>(hip_stream)), "4-bit GEMM launch");
+  } catch (...) {
+    return fail(CF_ERR_HIP, "internal error");
+  }
+}
+
+// Pages: sizes (`sizes`: no pointers, for the queries), then pointers and strides.
+static cf_status check_cache(const cf_cache& c, int64_t Hk, int64_t d, bool sizes, CachePages& p) {
+  if (c.code_dtype != CF_BF16 && c.code_dtype != CF_I8 && c.code_dtype != CF_FP8_E4M3)
+    return fail(CF_ERR_DTYPE, "code_dtype must be BF16, I8 or FP8_E4M3");
+  if (c.page < 16 || c.page > 1024 || (c.page & (c.page - 1)) != 0) return fail(CF_ERR_UNSUPPORTED, "page = %lld must be a power of two in [16, 1024]", (long long)c.page);
+  if (c.n_pages <= 0 || c.n_pages > (((int64_t)1 << 31) - 1) / c.page) return fail(CF_ERR_SHAPE, "need 0 < n_pages, n_pages * page < 2^31");
+  p = CachePages{};
+  p.code = c.code_dtype == CF_BF16 ? CACHE_BF16 : c.code_dtype == CF_I8 ? CACHE_I8 : CACHE_E4M3;
+  p.n_pages = (int)c.n_pages;
+  while ((int64_t)1 << p.shift < c.page) ++p.shift;
+  if (sizes) return CF_OK;
+  const int64_t e = (int64_t)dsize(c.code_dtype), step = 16 / e;
+  auto rows = [&](const char* name, const void* at, int64_t sp, int64_t sh, int64_t sl) {
+    if (!at) return fail(CF_ERR_NULL, "cache %s is NULL", name);
+    if (!aligned16(at)) return fail(CF_ERR_ALIGN, "cache %s is not 16-byte aligned", name);
+    if (sl < d) return fail(CF_ERR_LD, "cache %s: row stride %lld < %lld", name, (long long)sl, (long long)d);
+    if (sl >= kMaxRowPitch / e) return fail(CF_ERR_LD, "cache %s: row stride of %lld bytes or more", name, (long long)kMaxRowPitch);
+    if (sp < 0 || sp % step != 0 || sh < 0 || sh % step != 0 || sl % step != 0)
+      return fail(CF_ERR_ALIGN, "cache %s: strides must be non-negative multiples of 16 bytes", name);
+    if (sp > (int64_t)1 << 40 || sh > (int64_t)1 << 40) return fail(CF_ERR_LD, "cache %s: stride too large", name);
+    return CF_OK;
+  };
+  auto scales = [&](const char* name, const float* at, int64_t sp, int64_t sh) {
+    if (p.code == CACHE_BF16) return CF_OK;
+    if (!at) return fail(CF_ERR_NULL, "cache %s is NULL", name);
+    if (!aligned16(at)) return fail(CF_ERR_ALIGN, "cache %s is not 16-byte aligned", name);
+    if (sp < 0 || sp % 4 != 0 || sh < 0 || sh % 4 != 0) return fail(CF_ERR_ALIGN, "cache %s: strides must be non-negative multiples of 4", name);
+    if (sp > (int64_t)1 << 40 || sh > (int64_t)1 << 40) return fail(CF_ERR_LD, "cache %s: stride too large", name);
+    return CF_OK;
+  };
+  cf_status s;
+  if ((s = rows("K", c.K, c.k_p, c.k_h, c.k_l)) != CF_OK || (s = rows("V", c.V, c.v_p, c.v_h, c.v_l)) != CF_OK ||
+      (s = scales("Ks", c.Ks, c.ks_p, c.ks_h)) != CF_OK || (s = scales("Vs", c.Vs, c.vs_p, c.vs_h)) != CF_OK)
+    return s;
+  p.K = reinterpret_cast<char*>(c.K);
+  p.k_p = c.k_p * e;
+  p.k_h = c.k_h * e;
+  p.k_l = c.k_l * e;
+  p.V = reinterpret_cast<char*>(c.V);
+  p.v_p = c.v_p * e;
+  p.v_h = c.v_h * e;
+  p.v_l = c.v_l * e;
+  p.Ks = c.Ks;
+  p.ks_p = c.ks_p;
+  p.ks_h = c.ks_h;
+  p.Vs = c.Vs;
+  p.vs_p = c.vs_p;
+  p.vs_h = c.vs_h;
+  return CF_OK;
+}
+// A cache that is written: rows of different pages, heads and tokens do not overlap (strides nest).
+static cf_status check_nesting(const char* name, int64_t n, int64_t sp, int64_t Hk, int64_t sh, int64_t rows, int64_t sl, int64_t d) {
+  std::pair<int64_t, int64_t> dims[3] = {{sp, n}, {sh, Hk}, {sl, rows}};
+  std::sort(dims, dims + 3);
+  int64_t extent = d;
+  for (const auto& [stride, count] : dims) {
+    if (count <= 1) continue;
+    if (stride < extent) return fail(CF_ERR_LD, "cache %s: rows overlap (strides below the extent of what they step over)", name);
+    if (stride > ((int64_t)1 << 61) / count) return fail(CF_ERR_LD, "cache %s: stride too large", name);
+    extent += stride * (count - 1);
+  }
+  return CF_OK;
+}
+
+cf_status cf_cache_write(const cf_cache_write_args* a, void* hip_stream) {
+  try {
+    if (!a) return fail(CF_ERR_NULL, "args is NULL");
+    if (a->struct_size != sizeof(cf_cache_write_args))
+      return fail(CF_ERR_STRUCT, "struct_size %zu != %zu", a->struct_size, sizeof(cf_cache_write_args));
+    if (a->T < 0 || a->T > (int64_t)1 << 24 || a->H < 0 || a->H > 65535 || a->Hk <= 0 || a->Hk > 65535)
+      return fail(CF_ERR_SHAPE, "need 0 <= T <= 2^24, 0 <= H <= 65535, 0 < Hk <= 65535");
+    if (a->d != 64 && a->d != 128) return fail(CF_ERR_UNSUPPORTED, "head dim %lld not compiled (64, 128)", (long long)a->d);
+    if (a->rot < 0 || a->rot > a->d || a->rot % 16 != 0) return fail(CF_ERR_SHAPE, "rot = %lld must be a multiple of 16 up to d", (long long)a->rot);
+    if (a->pairs != CF_PAIRS_HALVES && a->pairs != CF_PAIRS_NEIGHBOURS) return fail(CF_ERR_UNSUPPORTED, "unknown pairs");
+    CacheWriteParams p{};
+    if (a->rot > 0) {
+      if (a->n_axes < 1 || a->n_axes > 4) return fail(CF_ERR_SHAPE, "need 1 to 4 axes");
+      int64_t sum = 0;
+      for (int i = 0; i < 4; ++i) {
+        if (i < a->n_axes) {
+          if (a->sections[i] < 0 || a->sections[i] > a->rot / 2) return fail(CF_ERR_SHAPE, "a section is negative or too long");
+          sum += a->sections[i];
+        }
+        p.first[i] = (int)(i < a->n_axes - 1 ? sum : a->rot / 2);
+      }
+      if (sum != a->rot / 2) return fail(CF_ERR_SHAPE, "the sections add up to %lld, not rot / 2 = %lld", (long long)sum, (long long)(a->rot / 2));
+      if (a->n_axes > 1 && a->T > 0 && (a->ldpos < a->T || a->ldpos > (int64_t)1 << 40)) return fail(CF_ERR_LD, "pos: leading dimension %lld < %lld, or too large", (long long)a->ldpos, (long long)a->T);
+    }
+    const bool any = a->T > 0;
+    cf_status s = check_cache(a->cache, a->Hk, a->d, !any, p.c);
+    if (s != CF_OK) return s;
+    if (!any) return CF_OK;
+    const bool q = a->H > 0;
+    if ((s = check_rows("Q", a->Q, q, 1, 0, a->H, a->q_h, a->T, a->q_t, a->d)) != CF_OK ||
+        (s = check_rows("Qo", a->Qo, q, 1, 0, a->H, a->qo_h, a->T, a->qo_t, a->d, true)) != CF_OK ||
+        (s = check_rows("K", a->K, true, 1, 0, a->Hk, a->k_h, a->T, a->k_t, a->d)) != CF_OK ||
+        (s = check_rows("V", a->V, true, 1, 0, a->Hk, a->v_h, a->T, a->v_t, a->d)) != CF_OK)
+      return s;
+    const cf_cache& c = a->cache;
+    if ((s = check_nesting("K", c.n_pages, c.k_p, a->Hk, c.k_h, c.page, c.k_l, a->d)) != CF_OK ||
+        (s = check_nesting("V", c.n_pages, c.v_p, a->Hk, c.v_h, c.page, c.v_l, a->d)) != CF_OK)
+      return s;
+    if (p.c.code != CACHE_BF16 &&
+        ((s = check_nesting("Ks", c.n_pages, c.ks_p, a->Hk, c.ks_h, 1, 0, c.page)) != CF_OK ||
+         (s = check_nesting("Vs", c.n_pages, c.vs_p, a->Hk, c.vs_h, 1, 0, c.page)) != CF_OK))
+      return s;
+    if (!a->slots) return fail(CF_ERR_NULL, "slots is NULL");
+    if (a->rot > 0 && (!a->pos || !a->freq)) return fail(CF_ERR_NULL, "pos or freq is NULL");
+    for (const void* v : {(const void*)a->slots, (const void*)(a->rot > 0 ? a->pos : nullptr), (const void*)(a->rot > 0 ? a->freq : nullptr)})
+      if (reinterpret_cast<uintptr_t>(v) & 3u) return fail(CF_ERR_ALIGN, "slots, pos or freq is not 4-byte aligned");
+    const float* const ks = p.c.code == CACHE_BF16 ? nullptr : c.Ks;
+    const float* const vs = p.c.code == CACHE_BF16 ? nullptr : c.Vs;
+    const void* const qo = q ? a->Qo : nullptr;
+    for (const void* out : {(const void*)c.K, (const void*)c.V, (const void*)ks, (const void*)vs, qo})
+      if (outputs_alias(out, {a->K, a->V, a->slots, a->rot > 0 ? a->pos : nullptr, a->rot > 0 ? a->freq : nullptr}))
+        return fail(CF_ERR_ALIAS, "an output aliases an input");
+    for (const void* out : {(const void*)c.K, (const void*)c.V, (const void*)ks, (const void*)vs})
+      if (outputs_alias(out, {q ? a->Q : nullptr, qo})) return fail(CF_ERR_ALIAS, "the cache aliases the queries");
+    if (outputs_alias(c.K, {c.V, ks, vs}) || outputs_alias(c.V, {ks, vs}) || outputs_alias(ks, {vs}))
+      return fail(CF_ERR_ALIAS, "the cache's parts alias each other");
+    // Qo may be Q: every element is read by the thread that writes it.
+    if (q && a->Qo == a->Q && ((a->T > 1 && a->q_t != a->qo_t) || (a->H > 1 && a->q_h != a->qo_h)))
+      return fail(CF_ERR_ALIAS, "Qo is Q with other strides");
+    p.T = (int)a->T;
+    p.H = (int)a->H;
+    p.Hk = (int)a->Hk;
+    p.d = (int)a->d;
+    p.Q = reinterpret_cast<const uint16_t*>(a->Q);
+    p.q_t = a->q_t;
+    p.q_h = a->q_h;
+    p.Qo = reinterpret_cast<uint16_t*>(a->Qo);
+    p.qo_t = a->qo_t;
+    p.qo_h = a->qo_h;
+    p.K = reinterpret_cast<const uint16_t*>(a->K);
+    p.k_t = a->k_t;
+    p.k_h = a->k_h;
+    p.V = reinterpret_cast<const uint16_t*>(a->V);
+    p.v_t = a->v_t;
+    p.v_h = a->v_h;
+    p.slots = a->slots;
+    p.rot = (int)a->rot;
+    p.neighbours = a->pairs == CF_PAIRS_NEIGHBOURS;
+    p.pos = a->pos;
+    p.ldpos = a->n_axes > 1 ? a->ldpos : 0;
+    p.freq = a->freq;
+    return hip_status(launch_cache_write(p, reinterpret_cast<hipStream_t>(hip_stream)), "cache write launch");
+  } catch (...) {
+    return fail(CF_ERR_HIP, "internal error");
+  }
+}
+
+// The table of a batch's pages.
+static cf_status check_table(int64_t batch, const int32_t* table, int64_t ldt, int64_t pages, const int32_t* lens) {
+  if (pages > 0 && !table) return fail(CF_ERR_NULL, "table is NULL");
+  if (!lens) return fail(CF_ERR_NULL, "lens is NULL");
+  if ((reinterpret_cast<uintptr_t>(table) & 3u) || (reinterpret_cast<uintptr_t>(lens) & 3u))
+    return fail(CF_ERR_ALIGN, "table or lens is not 4-byte aligned");
+  if (batch > 1 && (ldt < 0 || ldt > (int64_t)1 << 40)) return fail(CF_ERR_LD, "table: leading dimension %lld", (long long)ldt);
+  return CF_OK;
+}
+constexpr int64_t kPagedMaxKeys = (int64_t)1 << 30;   // pages * page of a sequence
+
+cf_status cf_cache_read(const cf_cache_read_args* a, void* hip_stream) {
+  try {
+    if (!a) return fail(CF_ERR_NULL, "args is NULL");
+    if (a->struct_size != sizeof(cf_cache_read_args))
+      return fail(CF_ERR_STRUCT, "struct_size %zu != %zu", a->struct_size, sizeof(cf_cache_read_args));
+    if (a->batch < 0 || a->batch > 65535 || a->Hk <= 0 || a->Hk > 65535 || a->S < 0 || a->S > kPagedMaxKeys || a->pages < 0 ||
+        a->pages > kPagedMaxKeys)
+      return fail(CF_ERR_SHAPE, "need 0 <= batch <= 65535, 0 < Hk <= 65535, 0 <= S, pages <= 2^30");
+    if (a->d != 64 && a->d != 128) return fail(CF_ERR_UNSUPPORTED, "head dim %lld not compiled (64, 128)", (long long)a->d);
+    CacheReadParams p{};
+    const bool any = a->batch > 0 && a->S > 0 && a->pages > 0;
+    cf_status s = check_cache(a->cache, a->Hk, a->d, !any, p.c);
+    if (s != CF_OK) return s;
+    if (a->pages > kPagedMaxKeys / a->cache.page) return fail(CF_ERR_SHAPE, "pages * page exceeds 2^30");
+    if (!any) return CF_OK;
+    if ((s = check_table(a->batch, a->table, a->ldt, a->pages, a->lens)) != CF_OK ||
+        (s = check_rows("K", a->K, true, a->batch, a->k_b, a->Hk, a->k_h, a->S, a->k_l, a->d, true)) != CF_OK ||
+        (s = check_rows("V", a->V, true, a->batch, a->v_b, a->Hk, a->v_h, a->S, a->v_l, a->d, true)) != CF_OK)
+      return s;
+    const cf_cache& c = a->cache;
+    for (const void* out : {(const void*)a->K, (const void*)a->V})
+      if (outputs_alias(out, {c.K, c.V, p.c.code == CACHE_BF16 ? nullptr : c.Ks, p.c.code == CACHE_BF16 ? nullptr : c.Vs, a->table, a->lens}))
+        return fail(CF_ERR_ALIAS, "an output aliases an input");
+    if (a->K == a->V) return fail(CF_ERR_ALIAS, "K aliases V");
+    p.B = (int)a->batch;
+    p.Hk = (int)a->Hk;
+    p.S = (int)a->S;
+    p.d = (int)a->d;
+    p.table = a->table;
+    p.ldt = a->batch > 1 ? a->ldt : 0;
+    p.pages = (int)a->pages;
+    p.lens = a->lens;
+    p.K = reinterpret_cast<uint16_t*>(a->K);
+    p.k_b = a->k_b;
+    p.k_h = a->k_h;
+    p.k_l = a->k_l;
+    p.V = reinterpret_cast<uint16_t*>(a->V);
+    p.v_b = a->v_b;
+    p.v_h = a->v_h;
+    p.v_l = a->v_l;
+    return hip_status(launch_cache_read(p, reinterpret_cast<hipStream_t>(hip_stream)), "cache read launch");
+  } catch (...) {
+    return fail(CF_ERR_HIP, "internal error");
+  }
+}
+
+// Sizes only: what the workspace query needs.
+static cf_status paged_sizes(const cf_attention_paged_args* a, PagedParams& p) {
+  if (!a) return fail(CF_ERR_NULL, "args is NULL");
+  if (a->struct_size != sizeof(cf_attention_paged_args))
+    return fail(CF_ERR_STRUCT, "struct_size %zu != %zu", a->struct_size, sizeof(cf_attention_paged_args));
+  if (a->batch < 0 || a->batch > 65535 || a->H <= 0 || a->Hk <= 0 || a->H > 65535 || a->Lq < 0 || a->pages < 0 || a->pages > kPagedMaxKeys)
+    return fail(CF_ERR_SHAPE, "need 0 <= batch <= 65535, 0 < H <= 65535, Lq >= 0, 0 <= pages <= 2^30");
+  if (a->H % a->Hk != 0) return fail(CF_ERR_SHAPE, "H = %lld is not a multiple of Hk = %lld", (long long)a->H, (long long)a->Hk);
+  if (a->Lq > 64) return fail(CF_ERR_UNSUPPORTED, "Lq = %lld exceeds 64", (long long)a->Lq);
+  if (a->batch * a->H * a->Lq > (int64_t)1 << 24) return fail(CF_ERR_SHAPE, "batch * H * Lq exceeds 2^24");
+  if (a->d != 64 && a->d != 128) return fail(CF_ERR_UNSUPPORTED, "head dim %lld not compiled (64, 128)", (long long)a->d);
+  if (a->causal != 0 && a->causal != 1) return fail(CF_ERR_UNSUPPORTED, "causal must be 0 or 1");
+  if (!std::isfinite(a->scale) || !(a->scale > 0.0f)) return fail(CF_ERR_SHAPE, "scale must be finite and > 0");
+  if (!std::isfinite(a->softcap) || !(a->softcap >= 0.0f)) return fail(CF_ERR_SHAPE, "softcap must be finite and >= 0");
+  const cf_status s = check_cache(a->cache, a->Hk, a->d, true, p.c);
+  if (s != CF_OK) return s;
+  if (a->pages > kPagedMaxKeys / a->cache.page) return fail(CF_ERR_SHAPE, "pages * page exceeds 2^30");
+  const CachePages c = p.c;
+  p = PagedParams{};
+  p.c = c;
+  p.B = (int)a->batch;
+  p.H = (int)a->H;
+  p.Hk = (int)a->Hk;
+  p.Lq = (int)a->Lq;
+  p.d = (int)a->d;
+  p.pages = (int)a->pages;
+  p.causal = a->causal;
+  p.scale = a->scale;
+  p.softcap = a->softcap;
+  return CF_OK;
+}
+
+size_t cf_attention_paged_workspace(const cf_attention_paged_args* a) {
+  try {
+    PagedParams p;
+    if (paged_sizes(a, p) != CF_OK || p.B == 0 || p.Lq == 0) return 0;
+    return paged_workspace(p);
+  } catch (...) {
+    return 0;
+  }
+}
+
+const char* cf_attention_paged_form(const cf_attention_paged_args* a) {
+  try {
+    PagedParams p;
+    if (paged_sizes(a, p) != CF_OK || p.B == 0 || p.Lq == 0) return "";
+    paged_form(p, g_form, sizeof(g_form));
+    return g_form;
+  } catch (...) {
+    return "";
+  }
+}
+
+cf_status cf_attention_paged(const cf_attention_paged_args* a, void* workspace, size_t ws_bytes, void* hip_stream) {
+  try {
+    PagedParams p;
+    cf_status s = paged_sizes(a, p);
+    if (s != CF_OK) return s;
+    if (p.B == 0 || p.Lq == 0) return CF_OK;
+    const cf_cache& c = a->cache;
+    if ((s = check_cache(c, a->Hk, a->d, false, p.c)) != CF_OK ||
+        (s = check_table(a->batch, a->table, a->ldt, a->pages, a->lens)) != CF_OK ||
+        (s = check_rows("Q", a->Q, true, p.B, a->q_b, p.H, a->q_h, p.Lq, a->q_l, p.d)) != CF_OK ||
+        (s = check_rows("O", a->O, true, p.B, a->o_b, p.H, a->o_h, p.Lq, a->o_l, p.d, true)) != CF_OK)
+      return s;
+    const float* const ks = p.c.code == CACHE_BF16 ? nullptr : c.Ks;
+    const float* const vs = p.c.code == CACHE_BF16 ? nullptr : c.Vs;
+    if (outputs_alias(a->O, {a->Q, c.K, c.V, ks, vs, a->table, a->lens})) return fail(CF_ERR_ALIAS, "O aliases an input");
+    const size_t need = paged_workspace(p);
+    if (need > 0) {
+      if (!workspace) return fail(CF_ERR_WORKSPACE, "workspace of %zu bytes required", need);
+      if (ws_bytes < need) return fail(CF_ERR_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+      if (!aligned16(workspace)) return fail(CF_ERR_ALIGN, "workspace is not 16-byte aligned");
+      if (outputs_alias(workspace, {a->O, a->Q, c.K, c.V, ks, vs, a->table, a->lens}))
+        return fail(CF_ERR_ALIAS, "the workspace aliases an operand");
+    }
+    p.Q = reinterpret_cast<const uint16_t*>(a->Q);
+    p.q_b = a->q_b;
+    p.q_h = a->q_h;
+    p.q_l = a->q_l;
+    p.table = a->table;
+    p.ldt = p.B > 1 ? a->ldt : 0;
+    p.lens = a->lens;
+    p.O = reinterpret_cast<uint16_t*>(a->O);
+    p.o_b = a->o_b;
+    p.o_h = a->o_h;
+    p.o_l = a->o_l;
+    p.ws = reinterpret_cast<float*>(workspace);
+    return hip_status(launch_paged(p, reinterpret_cast<hipStream_t>(hip_stream)), "paged attention launch");
+  } catch (...) {
+    return fail(CF_ERR_HIP, "internal error");
+  }
+}
+
 }  // extern "C"

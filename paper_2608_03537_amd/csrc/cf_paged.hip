@@ -1,0 +1,456 @@
+// Attention of each sequence's last tokens over its pages:
+//     O_b = softmax(cap(scale Q_b K_b^T)) V_b.
+//
+// Rows.  The queries of one (sequence, key head) are G Lq rows, row i G + g being query i of
+// head g, in blocks of 16 RT rows.  The keys of a block are cut into parts, a workgroup each; its four
+// waves take 32 keys in turn and keep running maxima and sums of their own, which meet in LDS; the
+// parts' results meet in the workspace, where the workgroup that finishes a block last joins them.
+//
+// Products, on 16 x 16 x 32 MFMAs with no LDS: S^T = K Q^T takes a lane's 16-byte pieces of 16 key
+// rows as they lie in a page, so a lane holds one query row c = lane % 16 and keys 4 q + i, q = lane / 16, of
+// each 16.  That is the layout in which O^T = V^T P^T takes P^T, with k = 8 q + j standing for key
+// 4 q + j (j < 4) and 16 + 4 q + j - 4.  V^T of 16 dimensions needs one dimension of those 8 keys: a lane loads
+// D / 16 neighbouring ones of each (16 lanes a whole row), and picking the t-th of each, in the step that makes
+// bf16 of the codes, gives the operand for dimensions t, t + D / 16, ...: the transposition costs nothing.
+#include <algorithm>
+#include <cstdio>
+
+#include "cf_attn.h"
+#include "cf_gemm_tile.h"
+#include "cf_serving.h"
+#include "comfuse.h"
+
+namespace cf {
+
+namespace {
+
+constexpr int kWaves = 4, kStepKeys = 32;
+
+// Keys that query i of sequence b sees.
+__device__ __forceinline__ int paged_len(const PagedParams& p, int b) {
+  return (int)min((int64_t)max(p.lens[b], 0), (int64_t)p.pages << p.c.shift);
+}
+__device__ __forceinline__ int paged_seen(const PagedParams& p, int len, int i) {
+  return p.causal ? max(0, len - (p.Lq - 1 - i)) : len;
+}
+
+__device__ __forceinline__ float quad_max(float v) {   // over the lanes c, c + 16, c + 32, c + 48
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+#endif
+  return v;
+}
+__device__ __forceinline__ float quad_sum(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
+__device__ __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+// Two neighbouring codes (bytes 2 h, 2 h + 1 of w) as bf16: exact for int8 and for E4M3.
+template <int CODE, int H>
+__device__ __forceinline__ uint32_t codes_bf16(uint32_t w) {
+  if constexpr (CODE == CACHE_I8) {
+    return pack_bf16x2((float)(int8_t)(w >> (16 * H)), (float)(int8_t)(w >> (16 * H + 8)));
+  } else {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, H != 0));
+#else
+    return 0;
+#endif
+  }
+}
+
+template <int D, int CODE, int RT>
+struct PagedShape {
+  static constexpr int DT = D / 16, KS = D / 32;            // 16-wide blocks of d, MFMA steps over d
+  static constexpr int E = CODE == CACHE_BF16 ? 2 : 1;      // bytes of an element
+  static constexpr int KL = D * E / 64, VW = D * E / 64;    // 16-byte loads of a key tile; words of a value row, of a lane
+  static constexpr int ROWS = 16 * RT, PITCH = D + 4;       // merge: floats of a row
+  static constexpr int LDS = kWaves * ROWS * PITCH * 4;
+};
+
+// 8 d of an output row.
+__device__ __forceinline__ void paged_store(const PagedParams& p, int b, int h, int i, int d0, const float (&o)[8], float l) {
+  const float inv = 1.0f / l;
+  u32x4_t w = {pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv), pack_bf16x2(o[4] * inv, o[5] * inv),
+               pack_bf16x2(o[6] * inv, o[7] * inv)};
+  if (l == 0.0f) w = u32x4_t{};   // no key: o may be NaN, 0 times what a hidden value row holds
+  *reinterpret_cast<u32x4_t*>(p.O + b * p.o_b + h * p.o_h + i * p.o_l + d0) = w;
+}
+
+struct Joined {   // running join of parts: maximum, sum, 8 d
+  float M = kLowestF32, L = 0.0f, o[8] = {};
+  __device__ __forceinline__ void add(float m, float l, const float* x) {
+    const float mn = fmaxf(M, m), fo = __builtin_amdgcn_exp2f(M - mn), fz = __builtin_amdgcn_exp2f(m - mn);
+    M = mn;
+    L = fmaf(fz, l, fo * L);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = fmaf(fz, x[e], fo * o[e]);
+  }
+};
+
+template <int D, int CODE, int RT>
+__global__ __launch_bounds__(64 * kWaves) void paged_kernel(PagedParams p, int nrb, int parts, unsigned* count) {
+  using A = PagedShape<D, CODE, RT>;
+  __shared__ __attribute__((aligned(16))) char smem[A::LDS];
+  __shared__ int last_one;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c = lane & 15, q = lane >> 4;
+  int task = blockIdx.x;
+  const int rb = task % nrb;
+  task /= nrb;
+  const int z = task % parts;
+  task /= parts;
+  const int hk = task % p.Hk, b = task / p.Hk;
+  const int G = p.H / p.Hk, R = G * p.Lq, m0 = rb * A::ROWS;
+
+  const int len = paged_len(p, b);
+  const int last = paged_seen(p, len, (min(m0 + A::ROWS, R) - 1) / G);   // keys that some row sees
+  const int first = paged_seen(p, len, m0 / G);                          // ... that every row sees
+  const int steps = (last + kStepKeys - 1) / kStepKeys;
+  const int np = max(1, min(parts, (steps + kWaves - 1) / kWaves));      // parts of this block in use
+  if (z >= np) return;
+  const int j0 = (int)((int64_t)steps * z / np), j1 = (int)((int64_t)steps * (z + 1) / np);
+
+  // Q fragments.  16-byte pieces of a row of codes hold two steps' d of a lane.
+  u32x4_t qf[RT][A::KS];
+  int seen[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int m = min(m0 + 16 * rt + c, R - 1), i = m / G;
+    const bf16_t* src = p.Q + b * p.q_b + (hk * G + m % G) * p.q_h + i * p.q_l;
+#pragma unroll
+    for (int ks = 0; ks < A::KS; ++ks)
+      qf[rt][ks] = gload16(src + (CODE == CACHE_BF16 ? ks * 32 + q * 8 : (ks >> 1) * 64 + q * 16 + (ks & 1) * 8));
+    seen[rt] = paged_seen(p, len, i);
+  }
+
+  f32x4_t O[RT][A::DT] = {};
+  float M[RT], L[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    M[rt] = kLowestF32;
+    L[rt] = 0.0f;
+  }
+  const float cap = p.softcap, sl = cap > 0.0f ? p.scale / cap : p.scale * 1.4426950408889634f;
+  const float cap2 = cap * 1.4426950408889634f;
+
+  // Pages of the wave's next 64 steps, one a lane; entries that hold no page become -1.
+  int page0 = 0, page1 = 0;
+  auto look_up = [&](int j) {   // from step j on, kWaves apart
+    const int64_t key = (int64_t)(j + lane * kWaves) * kStepKeys;
+    auto entry = [&](int64_t k) {
+      int e = -1;
+      if (k < last) e = p.table[b * p.ldt + (k >> p.c.shift)];
+      return (uint32_t)e < (uint32_t)p.c.n_pages ? e : -1;
+    };
+    page0 = entry(key);
+    page1 = entry(key + 16);
+  };
+  u32x4_t kf[2][A::KL];
+  uint32_t vf[8][A::VW];
+  f32x4_t ksc[2], vsc[2];
+  const int klane = c * (int)p.c.k_l + q * 16, vlane = 4 * q * (int)p.c.v_l + c * A::VW * 4;
+  auto load_k = [&](int j, int n) {   // the wave's n-th step
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int64_t pg = max(0, __builtin_amdgcn_readlane(t ? page1 : page0, n & 63)), row = (j * kStepKeys + 16 * t) & ((1 << p.c.shift) - 1);
+      const char* src = p.c.K + pg * p.c.k_p + hk * p.c.k_h + row * p.c.k_l;
+#pragma unroll
+      for (int x = 0; x < A::KL; ++x) kf[t][x] = gload16(src + klane + x * 64);
+      if constexpr (CODE != CACHE_BF16) ksc[t] = *reinterpret_cast<const f32x4_t*>(p.c.Ks + pg * p.c.ks_p + hk * p.c.ks_h + row + 4 * q);
+    }
+  };
+  auto load_v = [&](int j, int n) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int64_t pg = max(0, __builtin_amdgcn_readlane(t ? page1 : page0, n & 63)), row = (j * kStepKeys + 16 * t) & ((1 << p.c.shift) - 1);
+      const char* src = p.c.V + pg * p.c.v_p + hk * p.c.v_h + row * p.c.v_l;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const char* at = src + vlane + i * (int)p.c.v_l;
+        if constexpr (A::VW == 4) {
+          const u32x4_t w = gload16(at);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) vf[4 * t + i][x] = w[x];
+        } else if constexpr (A::VW == 2) {
+          const u32x2_t w = *reinterpret_cast<const u32x2_t*>(at);
+          vf[4 * t + i][0] = w[0];
+          vf[4 * t + i][1] = w[1];
+        } else {
+          vf[4 * t + i][0] = *reinterpret_cast<const uint32_t*>(at);
+        }
+      }
+      if constexpr (CODE != CACHE_BF16) vsc[t] = *reinterpret_cast<const f32x4_t*>(p.c.Vs + pg * p.c.vs_p + hk * p.c.vs_h + row + 4 * q);
+    }
+  };
+
+  int n = 0;
+  if (j0 + wave < j1) {
+    look_up(j0 + wave);
+    load_k(j0 + wave, 0);
+    load_v(j0 + wave, 0);
+  }
+  for (int j = j0 + wave; j < j1; j += kWaves, ++n) {
+    const int next = j + kWaves;
+    const int k0 = j * kStepKeys;
+    const bool bad0 = __builtin_amdgcn_readlane(page0, n & 63) < 0, bad1 = __builtin_amdgcn_readlane(page1, n & 63) < 0;
+    const bool masked = k0 + kStepKeys > first || bad0 || bad1;
+    // S^T, in log2 units; with a cap its argument first
+    float s[RT][8];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      u32x4_t a[A::KS];
+#pragma unroll
+      for (int ks = 0; ks < A::KS; ++ks) {
+        if constexpr (CODE == CACHE_BF16) a[ks] = kf[t][ks];
+        else {
+          const uint32_t w0 = kf[t][ks >> 1][2 * (ks & 1)], w1 = kf[t][ks >> 1][2 * (ks & 1) + 1];
+          a[ks] = u32x4_t{codes_bf16<CODE, 0>(w0), codes_bf16<CODE, 1>(w0), codes_bf16<CODE, 0>(w1), codes_bf16<CODE, 1>(w1)};
+        }
+      }
+      f32x4_t sc = {sl, sl, sl, sl};
+      if constexpr (CODE != CACHE_BF16)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[i] *= ksc[t][i];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        f32x4_t acc = {};
+#pragma unroll
+        for (int ks = 0; ks < A::KS; ++ks) acc = mfma16(a[ks], qf[rt][ks], acc);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[rt][4 * t + i] = acc[i] * sc[i];
+      }
+    }
+    const f32x4_t v0 = vsc[0], v1 = vsc[1];
+    if ((n & 63) == 63 && next < j1) look_up(next);   // (bad0, bad1 are taken; V of this step is in flight)
+    if (next < j1) load_k(next, n + 1);
+    if (cap > 0.0f) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[rt][e] = cap2 * tanh_exp(s[rt][e]);
+    }
+    if (masked) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int key = k0 + 16 * (e >> 2) + 4 * q + (e & 3);
+        const bool bad = e < 4 ? bad0 : bad1;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+          if (bad || key >= seen[rt]) s[rt][e] = -INFINITY;
+        if (bad || key >= last)
+#pragma unroll
+          for (int x = 0; x < A::VW; ++x) vf[e][x] = 0;
+      }
+    }
+    u32x4_t pf[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float mx = s[rt][0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[rt][e]);
+      // The maximum is raised, and what was summed rescaled, only where a score passes it by 2^8.
+      if (__any(mx > M[rt] + 8.0f)) {
+        const float mn = fmaxf(M[rt], quad_max(mx)), f = __builtin_amdgcn_exp2f(M[rt] - mn);
+        M[rt] = mn;
+        L[rt] *= f;
+#pragma unroll
+        for (int d = 0; d < A::DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) O[rt][d][i] *= f;
+      }
+      float w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        w[e] = __builtin_amdgcn_exp2f(s[rt][e] - M[rt]);
+        L[rt] += w[e];
+        if constexpr (CODE != CACHE_BF16) {
+          const float y = w[e] * (e < 4 ? v0[e & 3] : v1[e & 3]);
+          w[e] = masked && s[rt][e] == -INFINITY ? 0.0f : y;   // whatever the scale of a hidden row holds
+        }
+      }
+      pf[rt] = u32x4_t{pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7])};
+    }
+    // O^T += V^T P^T
+#pragma unroll
+    for (int d = 0; d < A::DT; ++d) {
+      u32x4_t a;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if constexpr (CODE == CACHE_I8) {
+          a[x] = pack_bf16x2((float)(int8_t)(vf[2 * x][d / 4] >> (8 * (d % 4))), (float)(int8_t)(vf[2 * x + 1][d / 4] >> (8 * (d % 4))));
+        } else if constexpr (CODE == CACHE_E4M3) {
+          const uint32_t e0 = d % 4 / 2 ? codes_bf16<CODE, 1>(vf[2 * x][d / 4]) : codes_bf16<CODE, 0>(vf[2 * x][d / 4]);
+          const uint32_t e1 = d % 4 / 2 ? codes_bf16<CODE, 1>(vf[2 * x + 1][d / 4]) : codes_bf16<CODE, 0>(vf[2 * x + 1][d / 4]);
+          a[x] = __builtin_amdgcn_perm(e1, e0, d % 2 ? 0x07060302u : 0x05040100u);
+        } else {
+          a[x] = __builtin_amdgcn_perm(vf[2 * x + 1][d / 2], vf[2 * x][d / 2], d % 2 ? 0x07060302u : 0x05040100u);
+        }
+      }
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) O[rt][d] = mfma16(a, pf[rt], O[rt][d]);
+    }
+    if (next < j1) load_v(next, n + 1);
+  }
+
+  // The waves' results meet in LDS.  A lane holds d (4 q + i) D / 16 + t of row c: D / 4 neighbouring ones.
+  float* const so = reinterpret_cast<float*>(smem);
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    float* mine = so + (wave * A::ROWS + 16 * rt + c) * A::PITCH;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int d = 0; d < A::DT; d += 4)
+        *reinterpret_cast<f32x4_t*>(mine + (4 * q + i) * A::DT + d) = f32x4_t{O[rt][d][i], O[rt][d + 1][i], O[rt][d + 2][i], O[rt][d + 3][i]};
+    const float l = quad_sum(L[rt]);
+    if (q == 0) {
+      mine[D] = M[rt];
+      mine[D + 1] = l;
+    }
+  }
+  __syncthreads();
+  constexpr int TPR = D / 8, RPP = 64 * kWaves / TPR;
+  const int64_t rows = (int64_t)p.B * p.Hk * R;
+  const int d0 = tid % TPR * 8;
+  for (int r = tid / TPR; r < min(A::ROWS, R - m0); r += RPP) {
+    Joined a;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float* other = so + (w * A::ROWS + r) * A::PITCH;
+      a.add(other[D], other[D + 1], other + d0);
+    }
+    const int m = m0 + r;
+    if (np == 1) {
+      paged_store(p, b, hk * G + m % G, m / G, d0, a.o, a.L);
+    } else {   // the partial results take less than 2^31 bytes
+      const uint32_t at = (uint32_t)(z * rows + (int64_t)(b * p.Hk + hk) * R + m);
+      const f32x4_t x = {a.o[0], a.o[1], a.o[2], a.o[3]}, y = {a.o[4], a.o[5], a.o[6], a.o[7]};
+      coherent_store16(p.ws, at * (D * 4) + d0 * 4, __builtin_bit_cast(u32x4_t, x));
+      coherent_store16(p.ws, at * (D * 4) + d0 * 4 + 16, __builtin_bit_cast(u32x4_t, y));
+      if (d0 == 0)
+        coherent_store8(p.ws, (uint32_t)(parts * rows) * (D * 4) + at * 8, u32x2_t{__float_as_uint(a.M), __float_as_uint(a.L)});
+    }
+  }
+  if (np == 1) return;
+  wait_vmcnt<0>();   // this wave's partial results are written
+  __syncthreads();   // ... and every wave's
+  if (tid == 0) {
+    unsigned* const cnt = count + (b * p.Hk + hk) * nrb + rb;
+    last_one = atomicInc(cnt, (unsigned)(np - 1)) == (unsigned)(np - 1);   // the last one wraps it to 0
+  }
+  __syncthreads();
+  if (!last_one) return;
+  // Join the block's rows: D / 8 threads a row; where there are few rows, others take the parts in turn.
+  const int nr = min(A::ROWS, R - m0);
+  int rs = 1;   // rows beside each other
+  while (rs < nr && rs < RPP) rs *= 2;
+  const int ways = RPP / rs, way = tid / TPR / rs;
+  for (int r0 = 0; r0 < nr; r0 += rs) {
+    const int r = r0 + tid / TPR % rs, m = m0 + min(r, nr - 1);
+    Joined a;
+    constexpr int AHEAD = 4;
+    for (int s0 = way; s0 < np; s0 += AHEAD * ways) {
+      u32x4_t x[AHEAD], y[AHEAD];
+      u32x2_t v[AHEAD];
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e) {
+        const uint32_t at = (uint32_t)(min(s0 + e * ways, np - 1) * rows + (int64_t)(b * p.Hk + hk) * R + m);
+        x[e] = coherent_load16(p.ws, at * (D * 4) + d0 * 4);
+        y[e] = coherent_load16(p.ws, at * (D * 4) + d0 * 4 + 16);
+        v[e] = coherent_load8(p.ws, (uint32_t)(parts * rows) * (D * 4) + at * 8);
+      }
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e)
+        if (s0 + e * ways < np) {
+          float f[8];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            f[k] = __uint_as_float(x[e][k]);
+            f[4 + k] = __uint_as_float(y[e][k]);
+          }
+          a.add(__uint_as_float(v[e][0]), __uint_as_float(v[e][1]), f);
+        }
+    }
+    if (ways > 1) {   // (then one pass: rs >= nr)
+      float* mine = so + tid / TPR * A::PITCH;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mine[d0 + e] = a.o[e];
+      if (d0 == 0) {
+        mine[D] = a.M;
+        mine[D + 1] = a.L;
+      }
+      __syncthreads();
+      if (way == 0)
+        for (int w = 1; w < ways; ++w) {
+          const float* other = so + (w * rs + tid / TPR) * A::PITCH;
+          a.add(other[D], other[D + 1], other + d0);
+        }
+    }
+    if (way == 0 && r < nr) paged_store(p, b, hk * G + m % G, m / G, d0, a.o, a.L);
+  }
+}
+
+struct PagedPlan {
+  int rt, nrb, parts;
+};
+constexpr size_t kCounterBytes = CF_PAGED_WS_HEADER_BYTES;
+constexpr int kMaxParts = 64;
+
+PagedPlan make_plan(const PagedParams& p) {
+  const int64_t R = (int64_t)(p.H / p.Hk) * p.Lq;
+  PagedPlan pl;
+  pl.rt = R <= 16 ? 1 : 2;
+  pl.nrb = (int)((R + 16 * pl.rt - 1) / (16 * pl.rt));
+  const int64_t blocks = (int64_t)p.B * p.Hk * pl.nrb, keys = (int64_t)p.pages << p.c.shift, rows = (int64_t)p.B * p.Hk * R;
+  int64_t parts = std::min<int64_t>({kMaxParts, (768 + blocks - 1) / blocks, keys / (kStepKeys * kWaves)});
+  parts = std::min<int64_t>(parts, ((int64_t)1 << 30) / (rows * (p.d + 2) * 4));
+  if (blocks > (int64_t)kCounterBytes / 4) parts = 1;
+  pl.parts = (int)std::max<int64_t>(1, parts);
+  return pl;
+}
+
+template <int D, int CODE, int RT>
+hipError_t launch_rt(PagedParams p, const PagedPlan& pl, hipStream_t st) {
+  unsigned* const count = reinterpret_cast<unsigned*>(p.ws);
+  if (pl.parts > 1) p.ws += kCounterBytes / 4;
+  const int64_t wgs = (int64_t)p.B * p.Hk * pl.nrb * pl.parts;
+  hipLaunchKernelGGL((paged_kernel<D, CODE, RT>), dim3((unsigned)wgs), dim3(64 * kWaves), 0, st, p, pl.nrb, pl.parts, count);
+  return hipGetLastError();
+}
+template <int D, int CODE>
+hipError_t launch_code(const PagedParams& p, const PagedPlan& pl, hipStream_t st) {
+  return pl.rt == 1 ? launch_rt<D, CODE, 1>(p, pl, st) : launch_rt<D, CODE, 2>(p, pl, st);
+}
+template <int D>
+hipError_t launch_d(const PagedParams& p, const PagedPlan& pl, hipStream_t st) {
+  return p.c.code == CACHE_BF16 ? launch_code<D, CACHE_BF16>(p, pl, st)
+         : p.c.code == CACHE_I8 ? launch_code<D, CACHE_I8>(p, pl, st) : launch_code<D, CACHE_E4M3>(p, pl, st);
+}
+
+}  // namespace
+
+size_t paged_workspace(const PagedParams& p) {
+  const int parts = make_plan(p).parts;
+  if (parts == 1) return 0;
+  return kCounterBytes + (size_t)parts * (size_t)p.B * (size_t)p.H * (size_t)p.Lq * (size_t)(p.d + 2) * 4;
+}
+
+hipError_t launch_paged(const PagedParams& p, hipStream_t st) {
+  const PagedPlan pl = make_plan(p);
+  return p.d == 128 ? launch_d<128>(p, pl, st) : launch_d<64>(p, pl, st);
+}
+
+void paged_form(const PagedParams& p, char* text, size_t bytes) {
+  const PagedPlan pl = make_plan(p);
+  snprintf(text, bytes, "%d rows, %d blocks, %d parts", 16 * pl.rt, pl.nrb, pl.parts);
+}
+
+}  // namespace cf
