@@ -522,7 +522,7 @@ const char* cf_gemm_w4_form(const cf_gemm_w4_args* a);
  *     BF16, or I8 / FP8_E4M3 codes that stand for code * scale, with
  *     fp32 scales at p, h times their own strides, the page's tokens beside each other.
  * Strides of rows are multiples of 16 bytes, those of scales multiples of 4
- * elements; d in {64, 128}.  Slot t of the cache is row t % page of page t / page;
+ * elements; pages lie less than 2^32 bytes apart, a page's rows of a head within 2^31; d in {64, 128}.  Slot t of the cache is row t % page of page t / page;
  * n_pages * page < 2^31.
  *
  * cf_cache_write — rotary positions, and the rows of T new tokens into the cache:

@@ -857,6 +857,7 @@ def gemm_i8(A, B, sa=None, sb=None, *, bias=None, act="none", out_dtype=None, ou
     return Cm
 
 
+_CF_ERR_WORKSPACE = 6
 _prefix_lock = threading.Lock()   # threads that share a stream share its workspace: a call's launches stay together
 
 
@@ -1088,10 +1089,9 @@ def _cache(torch, Kc, Vc, Ks, Vs, Hk, d, device):
             Ks.data_ptr(), ks[0], ks[1], Vs.data_ptr(), vs[0], vs[1])
 
 
-def _ints(t, shape, device, name):
-    """t, checked to hold int32 values of a shape with unit innermost stride on `device`."""
-    if t.dim() != len(shape) or t.get_device() != device or t.stride(-1) != 1 and t.shape[-1] > 1 or str(t.dtype) != "torch.int32" \
-            or t.shape != shape:
+def _ints(t, shape, i32, device, name):
+    """The address of int32 values of a shape with unit innermost stride on `device`."""
+    if t.dtype is not i32 or t.shape != shape or t.get_device() != device or t.stride(-1) != 1 and shape[-1] > 1:
         raise ValueError(f"{name}: expected int32 {tuple(shape)} with unit innermost stride beside the other operands, got "
                          f"{tuple(t.shape)} of {t.dtype} on {t.device}")
     return t.data_ptr()
@@ -1143,7 +1143,7 @@ def cache_write(K, V, slots, Kc, Vc, Ks=None, Vs=None, *, q=None, pos=None, freq
         rot = 2 * freq.numel()
         fp = _vector(freq, rot // 2, torch.float32, device, "freq")
         n_axes = 1 if pos.dim() == 1 else pos.size(0)
-        pp = _ints(pos, (T,) if pos.dim() == 1 else (n_axes, T), device, "pos")
+        pp = _ints(pos, (T,) if pos.dim() == 1 else (n_axes, T), torch.int32, device, "pos")
         ldpos = pos.stride(0) if n_axes > 1 else T
         if sections is None and n_axes == 1:
             sections = (rot // 2,)
@@ -1152,7 +1152,7 @@ def cache_write(K, V, slots, Kc, Vc, Ks=None, Vs=None, *, q=None, pos=None, freq
         sec = (*sections, 0, 0, 0)[:4]
     a = _CACHE_WRITE.pack(_CACHE_WRITE.size, T, H, Hk, d, 0 if q is None else q.data_ptr(), qs[0], qs[1],
                           0 if Q is None else Q.data_ptr(), os_[0], os_[1], K.data_ptr(), k[0], k[1], V.data_ptr(), v[0], v[1],
-                          _ints(slots, (T,), device, "slots"), rot, _choice(_PAIRS, pairs, "pairs"), pp, ldpos, fp, n_axes, *sec,
+                          _ints(slots, (T,), torch.int32, device, "slots"), rot, _choice(_PAIRS, pairs, "pairs"), pp, ldpos, fp, n_axes, *sec,
                           *_cache(torch, Kc, Vc, Ks, Vs, Hk, d, device))
     status = L.cf_cache_write(a, raw)
     if status:
@@ -1171,7 +1171,7 @@ def cache_read(Kc, Vc, table, lens, Ks=None, Vs=None, *, S=None, out=None, strea
     if here is None:
         return _elsewhere(cache_read, Kc, stream, Vc, table, lens, Ks, Vs, S=S, out=out)
     L, torch, device, raw = here
-    bf16 = torch.bfloat16
+    bf16, i32 = torch.bfloat16, torch.int32
     _, Hk, page, d = Kc.shape
     B, pages = table.shape
     if out is None:
@@ -1186,7 +1186,7 @@ def cache_read(Kc, Vc, table, lens, Ks=None, Vs=None, *, S=None, out=None, strea
     if not k[3] == v[3] == 1:
         raise ValueError("expected unit innermost strides")
     a = _CACHE_READ.pack(_CACHE_READ.size, B, Hk, S, d, *_cache(torch, Kc, Vc, Ks, Vs, Hk, d, device),
-                         _ints(table, (B, pages), device, "table"), table.stride(0), pages, _ints(lens, (B,), device, "lens"),
+                         _ints(table, (B, pages), i32, device, "table"), table.stride(0), pages, _ints(lens, (B,), i32, device, "lens"),
                          K.data_ptr(), k[0], k[1], k[2], V.data_ptr(), v[0], v[1], v[2])
     status = L.cf_cache_read(a, raw)
     if status:
@@ -1210,7 +1210,7 @@ def attention_paged(Q, Kc, Vc, table, lens, Ks=None, Vs=None, *, causal=False, s
         return _elsewhere(attention_paged, Q, stream, Kc, Vc, table, lens, Ks, Vs, causal=causal, scale=scale,
                           softcap=softcap, out=out, ws=ws)
     L, torch, device, raw = here
-    bf16 = torch.bfloat16
+    bf16, i32 = torch.bfloat16, torch.int32
     shape = Q.shape
     B, H, Lq, d = shape
     if Q.dtype is not bf16:
@@ -1222,20 +1222,22 @@ def attention_paged(Q, Kc, Vc, table, lens, Ks=None, Vs=None, *, causal=False, s
     pages = table.size(1)
     Hk = Kc.size(1)
     a = _PAGED.pack(_PAGED.size, B, H, Hk, Lq, d, Q.data_ptr(), q[0], q[1], q[2],
-                    *_cache(torch, Kc, Vc, Ks, Vs, Hk, d, device), _ints(table, (B, pages), device, "table"), table.stride(0), pages,
-                    _ints(lens, (B,), device, "lens"), 1 if causal else 0, d ** -0.5 if scale is None else scale, softcap,
+                    *_cache(torch, Kc, Vc, Ks, Vs, Hk, d, device), _ints(table, (B, pages), i32, device, "table"), table.stride(0), pages,
+                    _ints(lens, (B,), i32, device, "lens"), 1 if causal else 0, d ** -0.5 if scale is None else scale, softcap,
                     O.data_ptr(), o[0], o[1], o[2])
-    need = 0 if ws is not None else L.cf_attention_paged_workspace(a)
-    if need:
-        with _prefix_lock:
-            ws = _prefix_workspace(torch, need, Q.device, (device, raw, "paged"))
-            status = L.cf_attention_paged(a, ws.data_ptr(), ws.numel(), raw)
-    elif ws is None:
-        status = L.cf_attention_paged(a, None, 0, raw)
-    else:
+    if ws is not None:
         if ws.dtype is not torch.uint8 or not ws.is_contiguous() or ws.get_device() != device:
             raise ValueError("ws: expected a contiguous uint8 tensor beside the other operands")
         status = L.cf_attention_paged(a, ws.data_ptr(), ws.numel(), raw)
+    else:
+        key = (device, raw, "paged")
+        with _prefix_lock:
+            # the cached workspace as it is: a call that wants a larger one says so, and has done nothing
+            ws = None if torch._C._cuda_isCurrentStreamCapturing() else _ws_cache.get(key)
+            status = L.cf_attention_paged(a, None, 0, raw) if ws is None else L.cf_attention_paged(a, ws.data_ptr(), ws.numel(), raw)
+            if status == _CF_ERR_WORKSPACE:
+                ws = _prefix_workspace(torch, L.cf_attention_paged_workspace(a), Q.device, key)
+                status = L.cf_attention_paged(a, ws.data_ptr(), ws.numel(), raw)
     if status:
         _check(status)
     return O

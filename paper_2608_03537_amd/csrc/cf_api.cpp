@@ -1467,7 +1467,8 @@ static cf_status check_cache(const cf_cache& c, int64_t Hk, int64_t d, bool size
     if (sl >= kMaxRowPitch / e) return fail(CF_ERR_LD, "cache %s: row stride of %lld bytes or more", name, (long long)kMaxRowPitch);
     if (sp < 0 || sp % step != 0 || sh < 0 || sh % step != 0 || sl % step != 0)
       return fail(CF_ERR_ALIGN, "cache %s: strides must be non-negative multiples of 16 bytes", name);
-    if (sp > (int64_t)1 << 40 || sh > (int64_t)1 << 40) return fail(CF_ERR_LD, "cache %s: stride too large", name);
+    if (sp * e >= (int64_t)1 << 32 || sh > (int64_t)1 << 40 || sl * e > (((int64_t)1 << 31) - 1) / c.page)
+      return fail(CF_ERR_LD, "cache %s: stride too large (a page's rows within 2^31 bytes, pages less than 2^32 apart)", name);
     return CF_OK;
   };
   auto scales = [&](const char* name, const float* at, int64_t sp, int64_t sh) {
@@ -1475,7 +1476,7 @@ static cf_status check_cache(const cf_cache& c, int64_t Hk, int64_t d, bool size
     if (!at) return fail(CF_ERR_NULL, "cache %s is NULL", name);
     if (!aligned16(at)) return fail(CF_ERR_ALIGN, "cache %s is not 16-byte aligned", name);
     if (sp < 0 || sp % 4 != 0 || sh < 0 || sh % 4 != 0) return fail(CF_ERR_ALIGN, "cache %s: strides must be non-negative multiples of 4", name);
-    if (sp > (int64_t)1 << 40 || sh > (int64_t)1 << 40) return fail(CF_ERR_LD, "cache %s: stride too large", name);
+    if (sp * 4 >= (int64_t)1 << 32 || sh > (int64_t)1 << 40) return fail(CF_ERR_LD, "cache %s: stride too large", name);
     return CF_OK;
   };
   cf_status s;

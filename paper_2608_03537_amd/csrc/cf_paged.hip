@@ -95,8 +95,8 @@ struct Joined {   // running join of parts: maximum, sum, 8 d
   }
 };
 
-template <int D, int CODE, int RT>
-__global__ __launch_bounds__(64 * kWaves) void paged_kernel(PagedParams p, int nrb, int parts, unsigned* count) {
+template <int D, int CODE, int RT, bool ONCE>
+__global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, int nrb, int parts, unsigned* count) {
   using A = PagedShape<D, CODE, RT>;
   __shared__ __attribute__((aligned(16))) char smem[A::LDS];
   __shared__ int last_one;
@@ -110,17 +110,8 @@ __global__ __launch_bounds__(64 * kWaves) void paged_kernel(PagedParams p, int n
   const int hk = task % p.Hk, b = task / p.Hk;
   const int G = p.H / p.Hk, R = G * p.Lq, m0 = rb * A::ROWS;
 
-  const int len = paged_len(p, b);
-  const int last = paged_seen(p, len, (min(m0 + A::ROWS, R) - 1) / G);   // keys that some row sees
-  const int first = paged_seen(p, len, m0 / G);                          // ... that every row sees
-  const int steps = (last + kStepKeys - 1) / kStepKeys;
-  const int np = max(1, min(parts, (steps + kWaves - 1) / kWaves));      // parts of this block in use
-  if (z >= np) return;
-  const int j0 = (int)((int64_t)steps * z / np), j1 = (int)((int64_t)steps * (z + 1) / np);
-
-  // Q fragments.  16-byte pieces of a row of codes hold two steps' d of a lane.
+  // Q fragments (on their way while the length is looked up).  16-byte pieces of a row of codes hold two steps' d of a lane.
   u32x4_t qf[RT][A::KS];
-  int seen[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int m = min(m0 + 16 * rt + c, R - 1), i = m / G;
@@ -128,8 +119,18 @@ __global__ __launch_bounds__(64 * kWaves) void paged_kernel(PagedParams p, int n
 #pragma unroll
     for (int ks = 0; ks < A::KS; ++ks)
       qf[rt][ks] = gload16(src + (CODE == CACHE_BF16 ? ks * 32 + q * 8 : (ks >> 1) * 64 + q * 16 + (ks & 1) * 8));
-    seen[rt] = paged_seen(p, len, i);
   }
+
+  const int len = paged_len(p, b);
+  const int last = paged_seen(p, len, (min(m0 + A::ROWS, R) - 1) / G);   // keys that some row sees
+  const int first = paged_seen(p, len, m0 / G);                          // ... that every row sees
+  const int steps = (last + kStepKeys - 1) / kStepKeys;
+  const int np = max(1, min(parts, (steps + kWaves - 1) / kWaves));      // parts of this block in use
+  if (z >= np) return;
+  const int j0 = (int)((int64_t)steps * z / np), j1 = (int)((int64_t)steps * (z + 1) / np);
+  int seen[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) seen[rt] = paged_seen(p, len, min(m0 + 16 * rt + c, R - 1) / G);
 
   f32x4_t O[RT][A::DT] = {};
   float M[RT], L[RT];
@@ -141,67 +142,115 @@ __global__ __launch_bounds__(64 * kWaves) void paged_kernel(PagedParams p, int n
   const float cap = p.softcap, sl = cap > 0.0f ? p.scale / cap : p.scale * 1.4426950408889634f;
   const float cap2 = cap * 1.4426950408889634f;
 
-  // Pages of the wave's next 64 steps, one a lane; entries that hold no page become -1.
-  int page0 = 0, page1 = 0;
-  auto look_up = [&](int j) {   // from step j on, kWaves apart
-    const int64_t key = (int64_t)(j + lane * kWaves) * kStepKeys;
-    auto entry = [&](int64_t k) {
-      int e = -1;
-      if (k < last) e = p.table[b * p.ldt + (k >> p.c.shift)];
-      return (uint32_t)e < (uint32_t)p.c.n_pages ? e : -1;
-    };
-    page0 = entry(key);
-    page1 = entry(key + 16);
+  // The pages of a step's two tiles (one where pages hold 32 tokens and more).  Their entries are asked for a step
+  // before they are used, by scalar loads: they are the wave's.
+  typedef const __attribute__((address_space(4))) int32_t* Table;
+  const Table table = (Table)(uintptr_t)(p.table + b * p.ldt);
+  const bool wide = p.c.shift > 4;
+  struct Pages {
+    int at[2];
   };
+  auto look_up = [&](int j) {   // (any entry in use for a step behind the last)
+    const int key = min(j, j1 - 1) * kStepKeys, e = table[key >> p.c.shift];
+    return Pages{{e, wide ? e : table[min(key + 16, last - 1) >> 4]}};
+  };
+  auto resolve = [&](int j, Pages e) {   // -1: behind the last key, or an entry that names no page
+    const int key = j * kStepKeys;
+    const bool in = j < j1;
+    return Pages{{in && (uint32_t)e.at[0] < (uint32_t)p.c.n_pages ? e.at[0] : -1,
+                  in && key + 16 < last && (uint32_t)e.at[1] < (uint32_t)p.c.n_pages ? e.at[1] : -1}};
+  };
+  // A tile is read through a buffer that ends behind the last key that some row sees (of no bytes where there is no
+  // page): what lies there comes back as 0, whatever it holds.  A step behind the last reads nothing, so that no branch hides
+  // how many loads are under way.  ONCE: the cache is larger than the last level's, so its lines are not kept.
+  [[maybe_unused]] constexpr int kHint = ONCE ? 2 : 0;
   u32x4_t kf[2][A::KL];
   uint32_t vf[8][A::VW];
   f32x4_t ksc[2], vsc[2];
-  const int klane = c * (int)p.c.k_l + q * 16, vlane = 4 * q * (int)p.c.v_l + c * A::VW * 4;
-  auto load_k = [&](int j, int n) {   // the wave's n-th step
+  [[maybe_unused]] const uint32_t klane = c * (uint32_t)p.c.k_l + q * 16;
+  uint32_t vlane[4];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int64_t pg = max(0, __builtin_amdgcn_readlane(t ? page1 : page0, n & 63)), row = (j * kStepKeys + 16 * t) & ((1 << p.c.shift) - 1);
-      const char* src = p.c.K + pg * p.c.k_p + hk * p.c.k_h + row * p.c.k_l;
-#pragma unroll
-      for (int x = 0; x < A::KL; ++x) kf[t][x] = gload16(src + klane + x * 64);
-      if constexpr (CODE != CACHE_BF16) ksc[t] = *reinterpret_cast<const f32x4_t*>(p.c.Ks + pg * p.c.ks_p + hk * p.c.ks_h + row + 4 * q);
-    }
+  for (int i = 0; i < 4; ++i) vlane[i] = (4 * q + i) * (uint32_t)p.c.v_l + c * A::VW * 4;
+#if defined(__HIP_DEVICE_COMPILE__)
+  auto buffer = [](const void* base, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00020000);
   };
-  auto load_v = [&](int j, int n) {
+  // Byte offsets of a step's tiles: the page stride is below 2^32 bytes, a page's rows lie within 2^31.
+  auto tiles = [&](int key, Pages pg, uint32_t page, uint32_t row, uint64_t (&at)[2]) {
+    at[0] = (uint64_t)(uint32_t)pg.at[0] * page + ((uint32_t)key & ((1u << p.c.shift) - 1)) * row;
+    at[1] = wide ? at[0] + 16 * row : (uint64_t)(uint32_t)pg.at[1] * page;
+  };
+  const char* const kbase = p.c.K + hk * p.c.k_h;
+  const char* const vbase = p.c.V + hk * p.c.v_h;
+  const char* const ksbase = reinterpret_cast<const char*>(p.c.Ks + hk * p.c.ks_h);
+  const char* const vsbase = reinterpret_cast<const char*>(p.c.Vs + hk * p.c.vs_h);
+#endif
+  auto load_k = [&](int j, Pages pg) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int key = j * kStepKeys;
+    uint64_t at[2];
+    tiles(key, pg, (uint32_t)p.c.k_p, (uint32_t)p.c.k_l, at);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int64_t pg = max(0, __builtin_amdgcn_readlane(t ? page1 : page0, n & 63)), row = (j * kStepKeys + 16 * t) & ((1 << p.c.shift) - 1);
-      const char* src = p.c.V + pg * p.c.v_p + hk * p.c.v_h + row * p.c.v_l;
+      const auto src = buffer(kbase + at[t], pg.at[t] < 0 ? 0 : min(16, last - key - 16 * t) * (uint32_t)p.c.k_l);
+#pragma unroll
+      for (int x = 0; x < A::KL; ++x)
+        kf[t][x] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(src, klane + x * 64, 0, kHint));
+    }
+    if constexpr (CODE != CACHE_BF16) {
+      tiles(key, pg, (uint32_t)p.c.ks_p * 4, 4, at);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        ksc[t] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(buffer(ksbase + at[t], pg.at[t] < 0 ? 0 : 64), q * 16, 0, 0));
+    }
+#endif
+  };
+  auto load_v = [&](int j, Pages pg) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int key = j * kStepKeys;
+    uint64_t at[2];
+    tiles(key, pg, (uint32_t)p.c.v_p, (uint32_t)p.c.v_l, at);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const auto src = buffer(vbase + at[t], pg.at[t] < 0 ? 0 : min(16, last - key - 16 * t) * (uint32_t)p.c.v_l);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const char* at = src + vlane + i * (int)p.c.v_l;
         if constexpr (A::VW == 4) {
-          const u32x4_t w = gload16(at);
+          const u32x4_t w = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(src, vlane[i], 0, kHint));
 #pragma unroll
           for (int x = 0; x < 4; ++x) vf[4 * t + i][x] = w[x];
         } else if constexpr (A::VW == 2) {
-          const u32x2_t w = *reinterpret_cast<const u32x2_t*>(at);
+          const u32x2_t w = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(src, vlane[i], 0, kHint));
           vf[4 * t + i][0] = w[0];
           vf[4 * t + i][1] = w[1];
         } else {
-          vf[4 * t + i][0] = *reinterpret_cast<const uint32_t*>(at);
+          vf[4 * t + i][0] = __builtin_amdgcn_raw_buffer_load_b32(src, vlane[i], 0, kHint);
         }
       }
-      if constexpr (CODE != CACHE_BF16) vsc[t] = *reinterpret_cast<const f32x4_t*>(p.c.Vs + pg * p.c.vs_p + hk * p.c.vs_h + row + 4 * q);
     }
+    if constexpr (CODE != CACHE_BF16) {
+      tiles(key, pg, (uint32_t)p.c.vs_p * 4, 4, at);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        vsc[t] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(buffer(vsbase + at[t], pg.at[t] < 0 ? 0 : 64), q * 16, 0, 0));
+    }
+#endif
   };
 
-  int n = 0;
+  Pages pages = {}, ahead = {};   // of the step whose rows are under way, and the entries of the one after it
   if (j0 + wave < j1) {
-    look_up(j0 + wave);
-    load_k(j0 + wave, 0);
-    load_v(j0 + wave, 0);
+    pages = resolve(j0 + wave, look_up(j0 + wave));
+    load_k(j0 + wave, pages);
+    load_v(j0 + wave, pages);
+    ahead = look_up(j0 + wave + kWaves);
   }
-  for (int j = j0 + wave; j < j1; j += kWaves, ++n) {
+  for (int j = j0 + wave; j < j1; j += kWaves) {
     const int next = j + kWaves;
     const int k0 = j * kStepKeys;
-    const bool bad0 = __builtin_amdgcn_readlane(page0, n & 63) < 0, bad1 = __builtin_amdgcn_readlane(page1, n & 63) < 0;
+    const bool bad0 = pages.at[0] < 0, bad1 = pages.at[1] < 0;
     const bool masked = k0 + kStepKeys > first || bad0 || bad1;
+    pages = resolve(next, ahead);
+    ahead = look_up(next + kWaves);
     // S^T, in log2 units; with a cap its argument first
     float s[RT][8];
 #pragma unroll
@@ -228,9 +277,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_kernel(PagedParams p, int n
         for (int i = 0; i < 4; ++i) s[rt][4 * t + i] = acc[i] * sc[i];
       }
     }
-    const f32x4_t v0 = vsc[0], v1 = vsc[1];
-    if ((n & 63) == 63 && next < j1) look_up(next);   // (bad0, bad1 are taken; V of this step is in flight)
-    if (next < j1) load_k(next, n + 1);
+    load_k(next, pages);
     if (cap > 0.0f) {
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
@@ -245,9 +292,6 @@ __global__ __launch_bounds__(64 * kWaves) void paged_kernel(PagedParams p, int n
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
           if (bad || key >= seen[rt]) s[rt][e] = -INFINITY;
-        if (bad || key >= last)
-#pragma unroll
-          for (int x = 0; x < A::VW; ++x) vf[e][x] = 0;
       }
     }
     u32x4_t pf[RT];
@@ -272,10 +316,12 @@ __global__ __launch_bounds__(64 * kWaves) void paged_kernel(PagedParams p, int n
         w[e] = __builtin_amdgcn_exp2f(s[rt][e] - M[rt]);
         L[rt] += w[e];
         if constexpr (CODE != CACHE_BF16) {
-          const float y = w[e] * (e < 4 ? v0[e & 3] : v1[e & 3]);
-          w[e] = masked && s[rt][e] == -INFINITY ? 0.0f : y;   // whatever the scale of a hidden row holds
+          w[e] *= vsc[e >> 2][e & 3];
         }
       }
+      if (CODE != CACHE_BF16 && masked)   // whatever the scale of a hidden row holds
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = s[rt][e] == -INFINITY ? 0.0f : w[e];
       pf[rt] = u32x4_t{pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7])};
     }
     // O^T += V^T P^T
@@ -297,7 +343,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_kernel(PagedParams p, int n
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) O[rt][d] = mfma16(a, pf[rt], O[rt][d]);
     }
-    if (next < j1) load_v(next, n + 1);
+    load_v(next, pages);
   }
 
   // The waves' results meet in LDS.  A lane holds d (4 q + i) D / 16 + t of row c: D / 4 neighbouring ones.
@@ -398,11 +444,24 @@ __global__ __launch_bounds__(64 * kWaves) void paged_kernel(PagedParams p, int n
   }
 }
 
+// How a call is cut.  A part costs its start, a partial result and its place in the join, 4 to 5 us beside a call in one part, so there
+// are only as many as the chip wants waves, each of 256 or 384 keys at least.  The share of the workgroups that fit the chip at
+// once, and the keys, are those with which 150 random calls (1 to 64 sequences, 64 to 16384 keys, 1 to 64 heads, measured with 1 to 48
+// parts each) are 3 % slower than with their best cut on average, 33 % at worst.  For instance (us; parts 1, 4, 8, 16, 32):
+//     1 x 32 heads of 8, 3072 keys, bf16, d 128      31   13 10.1  9.3 10.3
+//     1 x 32 heads of 8, 12288 keys, int8           131   37   22   15   15
+//     64 x 32 heads of 8, 6144 keys, int8           154  152  157
+//     16 x 16 heads of 4, 5 queries, 3072, E4M3, d 64  45 17  16   23   39
+// Eight waves a workgroup in place of four were 1.4 % faster at their best over all calls, 20 % for some.
 struct PagedPlan {
   int rt, nrb, parts;
+  bool once;
 };
 constexpr size_t kCounterBytes = CF_PAGED_WS_HEADER_BYTES;
-constexpr int kMaxParts = 64;
+constexpr int kMaxParts = 64, kCUs = 256;
+// Bytes of the cache from which its lines are not kept: the last-level cache has 256 MB, and a call over more finds little of
+// it there next time (215 MB: 48.3 -> 46.3 us so; 98 MB in it: 19.8 -> 20.7).
+constexpr int64_t kOnceBytes = 192 << 20;
 
 PagedPlan make_plan(const PagedParams& p) {
   const int64_t R = (int64_t)(p.H / p.Hk) * p.Lq;
@@ -410,20 +469,29 @@ PagedPlan make_plan(const PagedParams& p) {
   pl.rt = R <= 16 ? 1 : 2;
   pl.nrb = (int)((R + 16 * pl.rt - 1) / (16 * pl.rt));
   const int64_t blocks = (int64_t)p.B * p.Hk * pl.nrb, keys = (int64_t)p.pages << p.c.shift, rows = (int64_t)p.B * p.Hk * R;
-  int64_t parts = std::min<int64_t>({kMaxParts, (768 + blocks - 1) / blocks, keys / (kStepKeys * kWaves)});
-  parts = std::min<int64_t>(parts, ((int64_t)1 << 30) / (rows * (p.d + 2) * 4));
+  const bool bf16 = p.c.code == CACHE_BF16;
+  pl.once = pl.nrb == 1 && 2 * (int64_t)p.B * p.Hk * keys * (bf16 ? 2 * p.d : p.d + 4) > kOnceBytes;
+  const int resident = kCUs * (p.d == 128 ? (pl.rt == 1 ? 3 : 2) : (pl.rt == 1 ? 5 : 3));   // workgroups, by registers
+  const double share = bf16 && p.d == 128 && pl.rt == 1 ? 0.35 : 0.7;
+  const int64_t few_keys = pl.rt == 1 ? 256 : 384;
+  int64_t parts = std::min<int64_t>({kMaxParts, (int64_t)(resident * share) / blocks, keys / few_keys});
+  parts = std::min<int64_t>(parts, ((int64_t)1 << 30) / (rows * (p.d + 2) * 4));   // the partial results are addressed in 32 bits
   if (blocks > (int64_t)kCounterBytes / 4) parts = 1;
   pl.parts = (int)std::max<int64_t>(1, parts);
   return pl;
 }
 
-template <int D, int CODE, int RT>
-hipError_t launch_rt(PagedParams p, const PagedPlan& pl, hipStream_t st) {
+template <int D, int CODE, int RT, bool ONCE>
+hipError_t launch_once(PagedParams p, const PagedPlan& pl, hipStream_t st) {
   unsigned* const count = reinterpret_cast<unsigned*>(p.ws);
   if (pl.parts > 1) p.ws += kCounterBytes / 4;
   const int64_t wgs = (int64_t)p.B * p.Hk * pl.nrb * pl.parts;
-  hipLaunchKernelGGL((paged_kernel<D, CODE, RT>), dim3((unsigned)wgs), dim3(64 * kWaves), 0, st, p, pl.nrb, pl.parts, count);
+  hipLaunchKernelGGL((paged_kernel<D, CODE, RT, ONCE>), dim3((unsigned)wgs), dim3(64 * kWaves), 0, st, p, pl.nrb, pl.parts, count);
   return hipGetLastError();
+}
+template <int D, int CODE, int RT>
+hipError_t launch_rt(const PagedParams& p, const PagedPlan& pl, hipStream_t st) {
+  return pl.once ? launch_once<D, CODE, RT, true>(p, pl, st) : launch_once<D, CODE, RT, false>(p, pl, st);
 }
 template <int D, int CODE>
 hipError_t launch_code(const PagedParams& p, const PagedPlan& pl, hipStream_t st) {
@@ -450,7 +518,7 @@ hipError_t launch_paged(const PagedParams& p, hipStream_t st) {
 
 void paged_form(const PagedParams& p, char* text, size_t bytes) {
   const PagedPlan pl = make_plan(p);
-  snprintf(text, bytes, "%d rows, %d blocks, %d parts", 16 * pl.rt, pl.nrb, pl.parts);
+  snprintf(text, bytes, "%d rows, %d blocks, %d parts%s", 16 * pl.rt, pl.nrb, pl.parts, pl.once ? ", read once" : "");
 }
 
 }  // namespace cf
