@@ -948,6 +948,7 @@ _CODES4 = {"int4": CF_I4, "e2m1": CF_FP4_E2M1}
 _W4_QUANT, _GEMM_W4, _CACHE_WRITE, _CACHE_READ, _PAGED = (
     struct.Struct("@" + "".join(_FORMATS[f] for _, f in t._fields_))
     for t in (W4QuantArgs, GemmW4Args, CacheWriteArgs, CacheReadArgs, AttentionPagedArgs))
+_GEMM_W4_SIZE, _CACHE_WRITE_SIZE, _CACHE_READ_SIZE, _PAGED_SIZE = (s.size for s in (_GEMM_W4, _CACHE_WRITE, _CACHE_READ, _PAGED))
 
 
 def _tiles(N, K):
@@ -1017,7 +1018,7 @@ def gemm_w4(A, W, s, *, code="int4", bias=None, act="none", out_dtype=None, out=
         raise TypeError(f"expected bf16 tokens, got {A.dtype}")
     if ng == 0 or K % ng:
         raise ValueError(f"s: expected [K / group, N], got {tuple(s.shape)} for K = {K}")
-    if W.shape != _tiles(N, K) or W.dtype is not torch.uint8 or W.get_device() != device or not W.is_contiguous():
+    if W.shape != (-(-N // 32), -(-K // 64), 1024) or W.dtype is not torch.uint8 or W.get_device() != device or not W.is_contiguous():
         _like(W, _tiles(N, K), torch.uint8, device, "W")
         raise ValueError("W: expected contiguous tiles")
     if s.get_device() != device or (s.stride(1) != 1 and N > 1):
@@ -1030,7 +1031,7 @@ def gemm_w4(A, W, s, *, code="int4", bias=None, act="none", out_dtype=None, out=
     else:
         dt, Cm = _dt(out), _like(out, (M, N), out_dtype or out.dtype, device, "out")
         ldc = _row_ld(Cm, M, N, 4 if dt == CF_F32 else 2)
-    a = _GEMM_W4.pack(_GEMM_W4.size, M, N, K, K // ng, A.data_ptr(),
+    a = _GEMM_W4.pack(_GEMM_W4_SIZE, M, N, K, K // ng, A.data_ptr(),
                       K if K % 8 == 0 and A.is_contiguous() else _row_ld(A, M, K, 2),
                       _choice(_CODES4, code, "code"), W.data_ptr(), CF_BF16 if s.dtype is bf16 else _dt(s), s.data_ptr(),
                       s.stride(0), 0 if bias is None else _vector(bias, N, f32, device, "bias"),
@@ -1117,43 +1118,49 @@ def cache_write(K, V, slots, Kc, Vc, Ks=None, Vs=None, *, q=None, pos=None, freq
         return _elsewhere(cache_write, K, stream, V, slots, Kc, Vc, Ks, Vs, q=q, pos=pos, freq=freq, sections=sections,
                           pairs=pairs, out=out)
     L, torch, device, raw = here
-    bf16, shape = torch.bfloat16, K.shape
+    bf16, i32, shape = torch.bfloat16, torch.int32, K.shape
     T, Hk, d = shape
-    if not (K.dtype is V.dtype is bf16 and V.shape == shape and V.get_device() == device):
+    if not (K.dtype is V.dtype is bf16 and V.shape == shape and V.get_device() == slots.get_device() == device and
+            slots.dtype is i32 and slots.shape == (T,) and slots.is_contiguous()):
         _like(K, shape, bf16, device, "K")
         _like(V, shape, bf16, device, "V")
+        _ints(slots, (T,), i32, device, "slots")
+        if T > 1 and slots.stride(0) != 1:
+            raise ValueError("slots: expected a contiguous vector")
     k, v = K.stride(), V.stride()
-    if not k[2] == v[2] == 1:
-        raise ValueError("expected unit innermost strides")
-    H, Q, qs, os_ = 0, None, (0, 0), (0, 0)
+    H, Q, qp, op, qs, os_ = 0, None, 0, 0, (0, 0, 1), (0, 0, 1)
     if q is not None:
         H = q.size(1)
-        _like(q, (T, H, d), bf16, device, "q")
-        Q = torch.empty((T, H, d), dtype=bf16, device=K.device) if out is None else _like(out, (T, H, d), bf16, device, "out")
-        qs, os_ = q.stride(), Q.stride()
-        if not qs[2] == os_[2] == 1:
-            raise ValueError("expected unit innermost strides")
+        if q.dtype is not bf16 or q.get_device() != device or q.shape != (T, H, d):
+            _like(q, (T, H, d), bf16, device, "q")
+        Q = torch.empty_like(q) if out is None else _like(out, (T, H, d), bf16, device, "out")
+        qp, op, qs, os_ = q.data_ptr(), Q.data_ptr(), q.stride(), Q.stride()
     elif out is not None:
         raise ValueError("out comes with q")
-    rot = n_axes = ldpos = pp = fp = 0
-    sec = (0, 0, 0, 0)
+    if not k[2] == v[2] == qs[2] == os_[2] == 1:
+        raise ValueError("expected unit innermost strides")
+    rot = n_axes = ldpos = pp = fp = s0 = s1 = s2 = s3 = 0
     if (pos is None) != (freq is None):
         raise ValueError("pos and freq come together")
     if pos is not None:
-        rot = 2 * freq.numel()
-        fp = _vector(freq, rot // 2, torch.float32, device, "freq")
-        n_axes = 1 if pos.dim() == 1 else pos.size(0)
-        pp = _ints(pos, (T,) if pos.dim() == 1 else (n_axes, T), torch.int32, device, "pos")
-        ldpos = pos.stride(0) if n_axes > 1 else T
-        if sections is None and n_axes == 1:
-            sections = (rot // 2,)
-        if sections is None or len(sections) != n_axes or n_axes > 4:
-            raise ValueError(f"sections: expected one for each of up to 4 axes, got {sections}")
-        sec = (*sections, 0, 0, 0)[:4]
-    a = _CACHE_WRITE.pack(_CACHE_WRITE.size, T, H, Hk, d, 0 if q is None else q.data_ptr(), qs[0], qs[1],
-                          0 if Q is None else Q.data_ptr(), os_[0], os_[1], K.data_ptr(), k[0], k[1], V.data_ptr(), v[0], v[1],
-                          _ints(slots, (T,), torch.int32, device, "slots"), rot, _choice(_PAIRS, pairs, "pairs"), pp, ldpos, fp, n_axes, *sec,
-                          *_cache(torch, Kc, Vc, Ks, Vs, Hk, d, device))
+        half = freq.numel()
+        rot, fp = 2 * half, _vector(freq, half, torch.float32, device, "freq")
+        if pos.dim() == 1:
+            n_axes, ldpos, s0 = 1, T, half
+            pp = _ints(pos, (T,), i32, device, "pos")
+        else:
+            n_axes, ldpos = pos.size(0), pos.stride(0)
+            pp = _ints(pos, (n_axes, T), i32, device, "pos")
+        if sections is not None or n_axes > 1:
+            if sections is None or len(sections) != n_axes or n_axes > 4:
+                raise ValueError(f"sections: expected one for each of up to 4 axes, got {sections}")
+            s0, s1, s2, s3 = (*sections, 0, 0, 0)[:4]
+        elif n_axes == 1:
+            s0 = half
+    a = _CACHE_WRITE.pack(_CACHE_WRITE_SIZE, T, H, Hk, d, qp, qs[0], qs[1], op, os_[0], os_[1], K.data_ptr(), k[0], k[1],
+                          V.data_ptr(), v[0], v[1], slots.data_ptr(), rot,
+                          CF_PAIRS_HALVES if pairs == "halves" else _choice(_PAIRS, pairs, "pairs"), pp, ldpos, fp, n_axes,
+                          s0, s1, s2, s3, *_cache(torch, Kc, Vc, Ks, Vs, Hk, d, device))
     status = L.cf_cache_write(a, raw)
     if status:
         _check(status)
@@ -1180,12 +1187,14 @@ def cache_read(Kc, Vc, table, lens, Ks=None, Vs=None, *, S=None, out=None, strea
     else:
         K, V = out
         S = K.size(2) if S is None else S
-        _like(K, (B, Hk, S, d), bf16, device, "out")
-        _like(V, (B, Hk, S, d), bf16, device, "out")
+        shape = (B, Hk, S, d)
+        if not (K.dtype is V.dtype is bf16 and K.shape == shape and V.shape == shape and K.get_device() == V.get_device() == device):
+            _like(K, shape, bf16, device, "out")
+            _like(V, shape, bf16, device, "out")
     k, v = K.stride(), V.stride()
     if not k[3] == v[3] == 1:
         raise ValueError("expected unit innermost strides")
-    a = _CACHE_READ.pack(_CACHE_READ.size, B, Hk, S, d, *_cache(torch, Kc, Vc, Ks, Vs, Hk, d, device),
+    a = _CACHE_READ.pack(_CACHE_READ_SIZE, B, Hk, S, d, *_cache(torch, Kc, Vc, Ks, Vs, Hk, d, device),
                          _ints(table, (B, pages), i32, device, "table"), table.stride(0), pages, _ints(lens, (B,), i32, device, "lens"),
                          K.data_ptr(), k[0], k[1], k[2], V.data_ptr(), v[0], v[1], v[2])
     status = L.cf_cache_read(a, raw)
@@ -1221,7 +1230,7 @@ def attention_paged(Q, Kc, Vc, table, lens, Ks=None, Vs=None, *, causal=False, s
         raise ValueError("expected unit innermost strides")
     pages = table.size(1)
     Hk = Kc.size(1)
-    a = _PAGED.pack(_PAGED.size, B, H, Hk, Lq, d, Q.data_ptr(), q[0], q[1], q[2],
+    a = _PAGED.pack(_PAGED_SIZE, B, H, Hk, Lq, d, Q.data_ptr(), q[0], q[1], q[2],
                     *_cache(torch, Kc, Vc, Ks, Vs, Hk, d, device), _ints(table, (B, pages), i32, device, "table"), table.stride(0), pages,
                     _ints(lens, (B,), i32, device, "lens"), 1 if causal else 0, d ** -0.5 if scale is None else scale, softcap,
                     O.data_ptr(), o[0], o[1], o[2])

@@ -117,6 +117,29 @@ def test_write_far_positions():
 
 
 @gpu
+def test_write_angles():
+    """Unit rows turned by angles of all sizes: cosine and sine are those of 64 bits, rounded to bf16 from fp32; 2^45 gives NaN."""
+    g = gen(77)
+    T, half = 4096, 32
+    pos = torch.randint(0, 2 ** 31 - 1, (T,), generator=g, device="cuda").to(torch.int32)
+    pos[:2048] = torch.arange(2048, device="cuda")
+    freq = torch.exp2(torch.rand((half,), generator=g, device="cuda") * 30 - 24)       # 2^-24 .. 2^6: angles below 2^37
+    k = torch.zeros((T, 1, 64), dtype=BF16, device="cuda")
+    k[..., :half] = 1.0
+    kc, vc, _, _ = cf.cache_pages(4, 1, 1024, 64)
+    slots = torch.arange(T, dtype=torch.int32, device="cuda")
+    cf.cache_write(k, k, slots, kc, vc, pos=pos, freq=freq)
+    angle = (pos.to(F64)[:, None] * freq.to(F64)).cpu()
+    rows = kc.view(T, 64).cpu()
+    assert torch.equal(rows[:, :half], torch.cos(angle).float().to(BF16)) and torch.equal(rows[:, half:], torch.sin(angle).float().to(BF16))
+    freq[0], freq[1] = 2.0 ** 44, float("inf")
+    pos[:] = 2
+    cf.cache_write(k, k, slots, kc, vc, pos=pos, freq=freq)
+    rows = kc.view(T, 64)
+    assert bool(rows[:, [0, 1, half, half + 1]].isnan().all()) and not bool(rows[:, 2:half].isnan().any())
+
+
+@gpu
 @pytest.mark.parametrize("code", ["int8", "e4m3"])
 @pytest.mark.parametrize("d", [64, 128])
 def test_write_special_rows(code, d):
