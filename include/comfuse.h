@@ -606,10 +606,10 @@ cf_status cf_cache_read(const cf_cache_read_args* a, void* hip_stream);
  * their own strides (multiples of 8 elements); H is a multiple of Hk, query
  * head h reads key head h / (H / Hk).  causal = 1: query i sees the keys
  * j < lens[b] - (Lq - 1 - i).  A query that sees no key gets O = 0.  Table entries behind
- * lens[b] are not read, and rows at and behind it not used, whatever they hold; an infinity or NaN
- * in a value row that causal hides from some queries of a call only may reach those of them that see
- * other keys (as 0 * NaN).  1 <= Lq <= 64 (longer parts of a prompt: cf_cache_read and
- * cf_attention_prefix).  scale finite and > 0, softcap finite and >= 0.  The softmax is exact
+ * lens[b] are not read, and rows at and behind it not used, whatever they hold; nor does a row that
+ * causal hides from a query reach it.  1 <= Lq <= 64 (longer parts of a prompt: cf_cache_read and
+ * cf_attention_prefix), batch H Lq < 2^24, pages * page <= 2^30.  scale finite and > 0,
+ * softcap finite and >= 0.  The softmax is exact
  * (running maximum and sum in fp32); its weights, times the value's scale, are
  * rounded to bf16 for the second product.
  * Workspace: cf_attention_paged_workspace() bytes (may be 0), 16-byte aligned:

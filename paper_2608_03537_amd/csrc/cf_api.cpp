@@ -1666,7 +1666,8 @@ static cf_status paged_sizes(const cf_attention_paged_args* a, PagedParams& p) {
     return fail(CF_ERR_SHAPE, "need 0 <= batch <= 65535, 0 < H <= 65535, Lq >= 0, 0 <= pages <= 2^30");
   if (a->H % a->Hk != 0) return fail(CF_ERR_SHAPE, "H = %lld is not a multiple of Hk = %lld", (long long)a->H, (long long)a->Hk);
   if (a->Lq > 64) return fail(CF_ERR_UNSUPPORTED, "Lq = %lld exceeds 64", (long long)a->Lq);
-  if (a->batch * a->H * a->Lq > (int64_t)1 << 24) return fail(CF_ERR_SHAPE, "batch * H * Lq exceeds 2^24");
+  if (a->batch * a->H * a->Lq >= (int64_t)1 << 24)   // a workgroup of 256 threads each at most, in a grid of less than 2^32
+    return fail(CF_ERR_SHAPE, "batch * H * Lq must be less than 2^24");
   if (a->d != 64 && a->d != 128) return fail(CF_ERR_UNSUPPORTED, "head dim %lld not compiled (64, 128)", (long long)a->d);
   if (a->causal != 0 && a->causal != 1) return fail(CF_ERR_UNSUPPORTED, "causal must be 0 or 1");
   if (!std::isfinite(a->scale) || !(a->scale > 0.0f)) return fail(CF_ERR_SHAPE, "scale must be finite and > 0");

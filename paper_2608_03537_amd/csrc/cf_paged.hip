@@ -80,7 +80,7 @@ __device__ __forceinline__ void paged_store(const PagedParams& p, int b, int h, 
   const float inv = 1.0f / l;
   u32x4_t w = {pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv), pack_bf16x2(o[4] * inv, o[5] * inv),
                pack_bf16x2(o[6] * inv, o[7] * inv)};
-  if (l == 0.0f) w = u32x4_t{};   // no key: o may be NaN, 0 times what a hidden value row holds
+  if (l == 0.0f) w = u32x4_t{};   // no key
   *reinterpret_cast<u32x4_t*>(p.O + b * p.o_b + h * p.o_h + i * p.o_l + d0) = w;
 }
 
@@ -95,7 +95,9 @@ struct Joined {   // running join of parts: maximum, sum, 8 d
   }
 };
 
-template <int D, int CODE, int RT, bool ONCE>
+// MIXED: rows of a block may see different keys, and a value may be infinite or NaN (a check and a second
+// way for such a step, which cost a call without them 0.5 of 9.2 us).
+template <int D, int CODE, int RT, bool ONCE, bool MIXED>
 __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, int nrb, int parts, unsigned* count) {
   using A = PagedShape<D, CODE, RT>;
   __shared__ __attribute__((aligned(16))) char smem[A::LDS];
@@ -325,8 +327,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
       pf[rt] = u32x4_t{pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7])};
     }
     // O^T += V^T P^T
-#pragma unroll
-    for (int d = 0; d < A::DT; ++d) {
+    auto values = [&](int d) {
       u32x4_t a;
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
@@ -340,8 +341,45 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
           a[x] = __builtin_amdgcn_perm(vf[2 * x + 1][d / 2], vf[2 * x][d / 2], d % 2 ? 0x07060302u : 0x05040100u);
         }
       }
+      return a;
+    };
+    bool alone = false;
+    if (MIXED && masked) {
+      // Keys that some rows see and others do not: 0 times an infinity or a NaN would reach the others.
+      constexpr uint32_t kExp = CODE == CACHE_BF16 ? 0x7f807f80u : 0x7f7f7f7fu, kOne = CODE == CACHE_BF16 ? 0x00800080u : 0x01010101u;
+      uint32_t x = 0;
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) O[rt][d] = mfma16(a, pf[rt], O[rt][d]);
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int w = 0; w < A::VW; ++w) x |= (vf[i][w] & kExp) + kOne;
+      alone = __any((x & ~kExp & (CODE == CACHE_BF16 ? 0x80008000u : 0x80808080u)) != 0);
+    }
+    if (!alone) {
+#pragma unroll
+      for (int d = 0; d < A::DT; ++d) {
+        const u32x4_t a = values(d);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) O[rt][d] = mfma16(a, pf[rt], O[rt][d]);
+      }
+    } else {   // such a value is there: key by key, kept by the rows that see it
+#pragma unroll 1
+      for (int k = 0; k < kStepKeys; ++k) {
+        u32x4_t only;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int e = (k >> 4) * 4 + (k & 3) - 2 * x;
+          only[x] = (k >> 2 & 3) != q ? 0u : e == 0 ? 0x0000ffffu : e == 1 ? 0xffff0000u : 0u;
+        }
+#pragma unroll
+        for (int d = 0; d < A::DT; ++d) {
+          const u32x4_t a = values(d) & only;
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            const f32x4_t o = mfma16(a, pf[rt] & only, O[rt][d]);
+            if (k0 + k < seen[rt]) O[rt][d] = o;
+          }
+        }
+      }
     }
     load_v(next, pages);
   }
@@ -448,10 +486,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
 // are only as many as the chip wants waves, each of 256 or 384 keys at least.  The share of the workgroups that fit the chip at
 // once, and the keys, are those with which 150 random calls (1 to 64 sequences, 64 to 16384 keys, 1 to 64 heads, measured with 1 to 48
 // parts each) are 3 % slower than with their best cut on average, 33 % at worst.  For instance (us; parts 1, 4, 8, 16, 32):
-//     1 x 32 heads of 8, 3072 keys, bf16, d 128      31   13 10.1  9.3 10.3
-//     1 x 32 heads of 8, 12288 keys, int8           131   37   22   15   15
-//     64 x 32 heads of 8, 6144 keys, int8           154  152  157
-//     16 x 16 heads of 4, 5 queries, 3072, E4M3, d 64  45 17  16   23   39
+//     1 x 4 key heads of 8 heads, 2944 keys, bf16, d 128        22   11  8.8  8.8
+//     2 x 8 of 8, 9728 keys, int8, d 128                        78   26   17   16   20
+//     40 x 8 of 4, 2176 keys, int8, d 128                       39   40   46   67
+//     33 x 4 of 4, 6 queries, 6912 keys, int8, d 64             70   30   32   45   92
 // Eight waves a workgroup in place of four were 1.4 % faster at their best over all calls, 20 % for some.
 struct PagedPlan {
   int rt, nrb, parts;
@@ -481,13 +519,19 @@ PagedPlan make_plan(const PagedParams& p) {
   return pl;
 }
 
-template <int D, int CODE, int RT, bool ONCE>
-hipError_t launch_once(PagedParams p, const PagedPlan& pl, hipStream_t st) {
+template <int D, int CODE, int RT, bool ONCE, bool MIXED>
+hipError_t launch_mixed(PagedParams p, const PagedPlan& pl, hipStream_t st) {
   unsigned* const count = reinterpret_cast<unsigned*>(p.ws);
   if (pl.parts > 1) p.ws += kCounterBytes / 4;
   const int64_t wgs = (int64_t)p.B * p.Hk * pl.nrb * pl.parts;
-  hipLaunchKernelGGL((paged_kernel<D, CODE, RT, ONCE>), dim3((unsigned)wgs), dim3(64 * kWaves), 0, st, p, pl.nrb, pl.parts, count);
+  hipLaunchKernelGGL((paged_kernel<D, CODE, RT, ONCE, MIXED>), dim3((unsigned)wgs), dim3(64 * kWaves), 0, st, p, pl.nrb, pl.parts, count);
   return hipGetLastError();
+}
+template <int D, int CODE, int RT, bool ONCE>
+hipError_t launch_once(const PagedParams& p, const PagedPlan& pl, hipStream_t st) {
+  if constexpr (CODE != CACHE_I8)   // (its codes are finite, and a scale is applied to the weights)
+    if (p.causal && p.Lq > 1) return launch_mixed<D, CODE, RT, ONCE, true>(p, pl, st);
+  return launch_mixed<D, CODE, RT, ONCE, false>(p, pl, st);
 }
 template <int D, int CODE, int RT>
 hipError_t launch_rt(const PagedParams& p, const PagedPlan& pl, hipStream_t st) {

@@ -366,7 +366,35 @@ def test_paged_hidden_rows(Lq, major, code):
 
 
 @gpu
-@pytest.mark.parametrize("code", ["bf16", "int8"])
+@pytest.mark.parametrize("code", ["bf16", "int8", "e4m3"])
+@pytest.mark.parametrize("d,H,Hk,Lq,length,spoiled", [(64, 2, 2, 5, 40, 1), (128, 4, 2, 7, 65, 3), (64, 8, 1, 64, 70, 40), (128, 1, 1, 2, 2, 1)])
+def test_paged_causal_hides_nan(d, H, Hk, Lq, length, spoiled, code):
+    """NaN in the last rows of keys and values: no query that causal hides them from sees it, all others do."""
+    g = gen(length)
+    B, page = 3, 32
+    Q, cache, table = paged_case(g, B, H, Hk, Lq, length, d, page, code)
+    lens = torch.full((B,), length, dtype=torch.int32, device="cuda")
+    for t in range(length - spoiled, length):
+        for b in range(B):
+            n = int(table[b, t // page])
+            for x in ((0, 1) if code == "bf16" else (2, 3)):
+                cache[x][n, :, t % page] = float("nan")
+            if code == "e4m3":
+                cache[0][n, :, t % page], cache[1][n, :, t % page] = 127, 127
+    O = cf.attention_paged(Q, cache[0], cache[1], table, lens, cache[2], cache[3], causal=True)
+    assert bool(O[:, :, Lq - spoiled:].isnan().all())
+    clean = slice(0, Lq - spoiled)
+    check_paged(O[:, :, clean], Q[:, :, clean], cache, code, table, lens - spoiled, page, True)
+    if code == "bf16":   # an infinity in one dimension of the last value
+        cache[0].nan_to_num_(0.0), cache[1].nan_to_num_(0.0)
+        for b in range(B):
+            cache[1][int(table[b, (length - 1) // page])][:, (length - 1) % page, 3] = -math.inf
+        P = cf.attention_paged(Q, cache[0], cache[1], table, lens, causal=True)
+        assert bool((P[:, :, -1, 3] == -math.inf).all()) and bool(P[:, :, :-1].isfinite().all()) and int((~P.isfinite()).sum()) == B * H
+
+
+@gpu
+@pytest.mark.parametrize("code", ["bf16", "int8", "e4m3"])
 def test_paged_large_scores(code):
     """Scores of hundreds: the running maximum is raised many times, and weights underflow."""
     g = gen(1)
@@ -579,6 +607,13 @@ def paged_args(**kw):
     (dict(O=D_), "CF_ERR_ALIAS"), (dict(O=G_), "CF_ERR_ALIAS")])
 def test_paged_refuses(kw, status):
     assert cf.STATUS[cf.cf_attention_paged(paged_args(**kw), None, 0, None)] == status, cf.cf_last_error()
+
+
+def test_paged_grid_limit():
+    """One (sequence, key head) a workgroup: as many as a grid has no room for."""
+    at = dict(H=1024, Hk=1024, Lq=1, q_h=64, q_l=64, q_b=65536, o_h=64, o_l=64, o_b=65536)
+    assert cf.STATUS[cf.cf_attention_paged(paged_args(batch=16384, **at), None, 0, None)] == "CF_ERR_SHAPE"
+    assert " 1 parts" in cf.cf_attention_paged_form(paged_args(batch=16383, **at))
 
 
 def test_paged_workspace():
