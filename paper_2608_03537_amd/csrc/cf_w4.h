@@ -49,7 +49,8 @@ __device__ __forceinline__ u32x4_t w4_values(uint32_t w) {
     v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2));
     v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3));
   } else {
-    const uint32_t lo = (w << 4) & 0xF0F0F0F0u, hi = w & 0xF0F0F0F0u;
+    uint32_t lo = (w << 4) & 0xF0F0F0F0u, hi = w & 0xF0F0F0F0u;
+    asm("" : "+v"(lo), "+v"(hi));   // or the conversion takes the masks apart again, byte by byte
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       v[i] = __builtin_amdgcn_perm(__float_as_uint((float)(int8_t)(hi >> (8 * i))), __float_as_uint((float)(int8_t)(lo >> (8 * i))),
@@ -167,69 +168,161 @@ __global__ __launch_bounds__(S::NT) void gemm_w4_kernel(GemmW4Params p, uint32_t
     xa[ks] = s0 + row * 128 + (((2 * ks + lg) ^ ((row >> 1) & 7)) << 4);
   }
   f32x16_t acc[S::BM][S::BN] = {}, part[S::BM][S::BN];
-  const int all = (KB + S::KW - 1) / S::KW;   // every group passes every barrier
+  if constexpr (S::KW == 1 && FOLD != 32) {
+    // Many tokens: nothing waits for the rest of its own step.  While the MFMAs of 16 k run, the next 16 k are read from
+    // LDS and their weights converted; a stage is loaded again as soon as every wave has read its last part; a group's sums
+    // are added to the tile's before the first MFMA of the next group writes them.  (Against the loop below, us: 1024 x 4096
+    // x 4096 int4 51.5 -> 42.7, 4096 x 4096 x 4096 150 -> 147, 0.94 PFLOP/s, where int4's conversion, 15 vector operations for
+    // 8 codes, and the MFMAs share the issue and the power of a CU; E2M1 124.)
+    constexpr int PER = 4 / S::BM;            // pairs of weights converted beside an MFMA
+    constexpr int RUN = PAIRS ? 2 : 1;        // steps between branches
+    u32x4_t xf[2][S::BM], v[2][S::BN];
+    float sc[S::BN] = {};
 #pragma unroll
-  for (int u = 0; u < S::AHEAD; ++u) load(u, u);
-  for (int i0 = 0; i0 < all; i0 += S::NS) {
+    for (int u = 0; u < S::NS; ++u) load(u, u);
 #pragma unroll
-    for (int u = 0; u < S::NS; ++u) {
-      const int i = i0 + u;
-      // The weights' registers are waited for, and with them the step's earlier loads into LDS.
+    for (int b = 0; b < S::BN; ++b) asm volatile("" : "+v"(wr[0][b])::"memory");
+    lds_barrier();
+    static_for<0, S::BM>([&](auto a_t) {
+      constexpr int a = decltype(a_t)::value;
+      xf[0][a] = ds_read_b128_at<a * 4096>(xa[0]);
+    });
+    auto word_of = [](uint32_t w) {
+      asm("" : "+v"(w));   // opaque: the compiler would take its bytes apart long before their use
+      return w;
+    };
 #pragma unroll
-      for (int b = 0; b < S::BN; ++b) asm volatile("" : "+v"(wr[u][b])::"memory");
-      if constexpr (S::GW > 1) lds_barrier();   // every wave's loads of step i are in, and step i - 1 has been read
-      // Fragments of k step ks of every block, in the order in which they are used; each is waited for there.
-      u32x4_t xf[4][S::BM];
-      static_for<0, 4 * S::BM>([&](auto r_t) {
-        constexpr int r = decltype(r_t)::value;
-        xf[r / S::BM][r % S::BM] = ds_read_b128_at<r % S::BM * 4096>(xa[r / S::BM] + u * S::STAGE);
-      });
-      u32x4_t w[S::BN];
-      float sc[S::BN][H];
+    for (int b = 0; b < S::BN; ++b) v[0][b] = w4_values<E2M1>(word_of(wr[0][b][0]));
+    auto fold = [&](int a, int b) {
 #pragma unroll
-      for (int b = 0; b < S::BN; ++b) {
-        w[b] = wr[u][b];
+      for (int e = 0; e < 16; ++e) acc[a][b][e] = fmaf(part[a][b][e], sc[b], acc[a][b][e]);
+    };
 #pragma unroll
-        for (int h = 0; h < H; ++h) {
-          if constexpr (sizeof(T) == 4) sc[b][h] = sr[u][b][h];
-          else sc[b][h] = bf16_to_f32(sr[u][b][h]);
-          if (!E2M1) sc[b][h] *= 0.0625f;
-        }
-      }
-      const bool half = cut && block(i) == KB - 1, in = i < steps;
-      static_for<0, 4>([&](auto ks_t) {
-        constexpr int ks = decltype(ks_t)::value, h = H == 2 ? ks / 2 : 0;
-        constexpr bool first = H == 2 ? ks % 2 == 0 : ks == 0, fold = H == 2 ? ks % 2 == 1 : ks == 3;
-        static_for<0, S::BM>([&](auto a_t) {
-          constexpr int a = decltype(a_t)::value;
-          lgkm_wait<4 * S::BM - 1 - (ks * S::BM + a)>(xf[ks][a]);
+    for (int a = 0; a < S::BM; ++a)
+#pragma unroll
+      for (int b = 0; b < S::BN; ++b) part[a][b] = f32x16_t{};
+    for (int i0 = 0; i0 < steps; i0 += S::NS) {
+      static_for<0, S::NS / RUN>([&](auto run_t) {
+        if (i0 + decltype(run_t)::value * RUN >= steps) return;
+        static_for<0, 4 * RUN>([&](auto part_t) {
+          constexpr int u = decltype(run_t)::value * RUN + decltype(part_t)::value / 4, ks = decltype(part_t)::value % 4;
+          constexpr int next = (u + 1) % S::NS, cur = ks & 1;
+          constexpr bool begins = ks == 0 && !(PAIRS && u % 2), ends = ks == 3 && !(PAIRS && u % 2 == 0);   // a group
+          if constexpr (ks < 3)
+            static_for<0, S::BM>([&](auto a_t) {
+              constexpr int a = decltype(a_t)::value;
+              xf[!cur][a] = ds_read_b128_at<a * 4096>(xa[ks + 1] + u * S::STAGE);
+            });
+          static_for<0, S::BM>([&](auto a_t) {
+            constexpr int a = decltype(a_t)::value;
+            lgkm_wait<(ks < 3 ? S::BM : 0) + S::BM - 1 - a>(xf[cur][a]);
+          });
+          uint32_t word = 0;
+          static_for<0, S::BM * S::BN>([&](auto c_t) {
+            constexpr int c = decltype(c_t)::value, b = c / S::BM, a = c % S::BM;
+            if constexpr (begins) {
+              fold(a, b);
+              part[a][b] = f32x16_t{};
+            }
+            Mma<bf16_t>::run(part[a][b], xf[cur][a], v[cur][b]);
+            if constexpr (ks == 3 && c == 0) {
+              if constexpr (ends)
+#pragma unroll
+                for (int x = 0; x < S::BN; ++x) {
+                  if constexpr (sizeof(T) == 4) sc[x] = sr[u][x][0];
+                  else sc[x] = bf16_to_f32(sr[u][x][0]);
+                  if (!E2M1) sc[x] *= 0.0625f;
+                }
+              // The next step's weights are waited for, and with them the wave's earlier loads into LDS.
+#pragma unroll
+              for (int x = 0; x < S::BN; ++x) asm volatile("" : "+v"(wr[next][x])::"memory");
+              lds_barrier();   // every wave's are in, and this step's stage has been read
+              static_for<0, S::BM>([&](auto x_t) {
+                constexpr int x = decltype(x_t)::value;
+                xf[!cur][x] = ds_read_b128_at<x * 4096>(xa[0] + next * S::STAGE);
+              });
+              __builtin_amdgcn_sched_barrier(0);
+              load(i0 + u + S::NS, u);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (a == 0) word = word_of(ks < 3 ? wr[u][b][(ks + 1) % 4] : wr[next][b][0]);
+#pragma unroll
+            for (int x = a * PER; x < a * PER + PER; ++x) v[!cur][b][x] = w4_values<E2M1>(word)[x];
+          });
         });
-        if (in && !(H == 2 && h == 1 && half)) {
+      });
+    }
+    // Reads and loads of steps that there are not: none may land after their registers and stages have a new use.
+    static_for<0, S::BM>([&](auto a_t) { lgkm_wait<0>(xf[0][decltype(a_t)::value]); });
+    wait_vmcnt<0>();
 #pragma unroll
-          for (int b = 0; b < S::BN; ++b) {
-            const u32x4_t v = w4_values<E2M1>(w[b][ks]);
+    for (int a = 0; a < S::BM; ++a)
 #pragma unroll
-            for (int a = 0; a < S::BM; ++a) {
-              if (first && !(PAIRS && u % 2)) part[a][b] = f32x16_t{};
-              Mma<bf16_t>::run(part[a][b], xf[ks][a], v);
+      for (int b = 0; b < S::BN; ++b) fold(a, b);
+  } else {
+    const int all = (KB + S::KW - 1) / S::KW;   // every group passes every barrier
+#pragma unroll
+    for (int u = 0; u < S::AHEAD; ++u) load(u, u);
+    for (int i0 = 0; i0 < all; i0 += S::NS) {
+#pragma unroll
+      for (int u = 0; u < S::NS; ++u) {
+        const int i = i0 + u;
+        // The weights' registers are waited for, and with them the step's earlier loads into LDS.
+#pragma unroll
+        for (int b = 0; b < S::BN; ++b) asm volatile("" : "+v"(wr[u][b])::"memory");
+        if constexpr (S::GW > 1) lds_barrier();   // every wave's loads of step i are in, and step i - 1 has been read
+        // Fragments of k step ks of every block, in the order in which they are used; each is waited for there.
+        u32x4_t xf[4][S::BM];
+        static_for<0, 4 * S::BM>([&](auto r_t) {
+          constexpr int r = decltype(r_t)::value;
+          xf[r / S::BM][r % S::BM] = ds_read_b128_at<r % S::BM * 4096>(xa[r / S::BM] + u * S::STAGE);
+        });
+        u32x4_t w[S::BN];
+        float sc[S::BN][H];
+#pragma unroll
+        for (int b = 0; b < S::BN; ++b) {
+          w[b] = wr[u][b];
+#pragma unroll
+          for (int h = 0; h < H; ++h) {
+            if constexpr (sizeof(T) == 4) sc[b][h] = sr[u][b][h];
+            else sc[b][h] = bf16_to_f32(sr[u][b][h]);
+            if (!E2M1) sc[b][h] *= 0.0625f;
+          }
+        }
+        const bool half = cut && block(i) == KB - 1, in = i < steps;
+        static_for<0, 4>([&](auto ks_t) {
+          constexpr int ks = decltype(ks_t)::value, h = H == 2 ? ks / 2 : 0;
+          constexpr bool first = H == 2 ? ks % 2 == 0 : ks == 0, fold = H == 2 ? ks % 2 == 1 : ks == 3;
+          static_for<0, S::BM>([&](auto a_t) {
+            constexpr int a = decltype(a_t)::value;
+            lgkm_wait<4 * S::BM - 1 - (ks * S::BM + a)>(xf[ks][a]);
+          });
+          if (in && !(H == 2 && h == 1 && half)) {
+#pragma unroll
+            for (int b = 0; b < S::BN; ++b) {
+              const u32x4_t v = w4_values<E2M1>(w[b][ks]);
+#pragma unroll
+              for (int a = 0; a < S::BM; ++a) {
+                if (first) part[a][b] = f32x16_t{};
+                Mma<bf16_t>::run(part[a][b], xf[ks][a], v);
+              }
+            }
+            if constexpr (fold) {
+#pragma unroll
+                for (int b = 0; b < S::BN; ++b)
+#pragma unroll
+                  for (int a = 0; a < S::BM; ++a)
+#pragma unroll
+                    for (int e = 0; e < RE; ++e) acc[a][b][e] = fmaf(part[a][b][e], sc[b][h], acc[a][b][e]);
             }
           }
-          if constexpr (fold) {
-            if (!PAIRS || u % 2)
-#pragma unroll
-              for (int b = 0; b < S::BN; ++b)
-#pragma unroll
-                for (int a = 0; a < S::BM; ++a)
-#pragma unroll
-                  for (int e = 0; e < RE; ++e) acc[a][b][e] = fmaf(part[a][b][e], sc[b][h], acc[a][b][e]);
+          if constexpr (ks == 0) {
+            __builtin_amdgcn_sched_barrier(0);
+            load(i + S::AHEAD, (u + S::AHEAD) % S::NS);
           }
-        }
-        if constexpr (ks == 0) {
           __builtin_amdgcn_sched_barrier(0);
-          load(i + S::AHEAD, (u + S::AHEAD) % S::NS);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      });
+        });
+      }
     }
   }
   __syncthreads();
@@ -321,7 +414,7 @@ struct W4Tiles {
 };
 using AllW4Tiles = W4Tiles<W4Tile<1, 1, 1, 1, 8, 4, 8>, W4Tile<1, 2, 1, 1, 8, 4, 16>, W4Tile<1, 1, 1, 1, 8, 4, 32>,
                            W4Tile<1, 2, 1, 1, 8, 4, 32>, W4Tile<2, 1, 1, 1, 8, 2, 64>, W4Tile<2, 2, 1, 1, 4, 4, 64>,
-                           W4Tile<2, 2, 1, 2, 4, 2, 64>, W4Tile<2, 2, 2, 2, 1, 2, 128>>;
+                           W4Tile<2, 2, 1, 2, 4, 2, 64>, W4Tile<2, 2, 2, 2, 1, 4, 128>>;
 
 }  // namespace
 

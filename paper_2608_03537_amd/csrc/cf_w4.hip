@@ -9,19 +9,19 @@ namespace cf {
 namespace {
 
 // The tiles and their estimated time (us): rounds of 256 workgroups, each `step` for every 64 k (and `busy` times the
-// share of CUs at work) and `start` besides, and `once`; int4, then E2M1.  The last tile fits a CU twice: `pair` is a
-// step of two.  Fitted to 1 to 4096 tokens, 512 to 16384 channels and 512 to 8192 k, groups of 128; for instance (us, in this
-// order; - not measured):
-//     1 x 4096 x 4096 int4       6.8  9.6  7.8   11  9.4   15   22    -
+// share of CUs at work) and `start` besides, and `once`; int4, then E2M1.  (The last tile fits a CU twice; two together
+// take as long as one after the other.)  Fitted to 1 to 4096 tokens, 512 to 16384 channels and 512 to 8192 k, groups of 128;
+// for instance (us, in this order; - not measured):
+//     1 x 4096 x 4096 int4       6.8  9.6  7.8   11  9.5   15   22    -
 //     1 x 12288 x 4096 int4      9.7 10.1   14   11   17   15   22    -
-//     16 x 12288 x 4096 E2M1    11.2  8.4 12.1  9.1   16   13   19    -
-//     32 x 4096 x 4096 E2M1      8.6  7.9  7.0  8.8  9.0   13   19   39
-//     48 x 12288 x 4096 E2M1      26   21   19   17   16 14.0   19   40
-//     128 x 4096 x 4096 int4       -    -    -    - 10.3   16   23   50
-//     512 x 4096 x 4096 int4       -    -    -    -   38   34 28.8   51
-//     1024 x 4096 x 4096 int4      -    -    -    -   71   66 51.5   54
-//     4096 x 4096 x 4096 int4      -    -    -    -  274  233  180  143
-// Over the 1011 calls that were timed the tile that the estimate takes is 0.2 % slower than the best one on average, 39 %
+//     16 x 12288 x 4096 E2M1      11  8.5   12  9.1   16   13   19    -
+//     32 x 4096 x 4096 E2M1      8.8  7.9  7.0  8.7  9.1   13   19   31
+//     48 x 12288 x 4096 E2M1      26   20   19   16   16 13.6   19   31
+//     128 x 4096 x 4096 int4       -    -    -    - 10.6   16   23   40
+//     512 x 4096 x 4096 int4       -    -    -    -   37   32 26.4   42
+//     1024 x 4096 x 4096 int4      -    -    -    -   69   65   47 42.7
+//     4096 x 4096 x 4096 int4      -    -    -    -  270  232  179  142
+// Over the 1011 calls that were timed the tile that the estimate takes is 0.2 % slower than the best one on average, 42 %
 // at worst (1024 x 512 x 8192).
 struct Cost {
   double step, start, once, busy;
@@ -29,24 +29,23 @@ struct Cost {
 struct Form {
   int tm, tn, threads;
   Cost cost[2];
-  double pair[2];   // 0: one workgroup a CU
 };
 constexpr int kCUs = 256;
 template <class S>
-constexpr Form form_of(Cost int4, Cost e2m1, double pair_int4 = 0, double pair_e2m1 = 0) {
-  return {S::TM, S::TN, S::NT, {int4, e2m1}, {pair_int4, pair_e2m1}};
+constexpr Form form_of(Cost int4, Cost e2m1) {
+  return {S::TM, S::TN, S::NT, {int4, e2m1}};
 }
 template <class... S>
 constexpr int count_of(W4Tiles<S...>) { return (int)sizeof...(S); }
 const Form kForms[] = {   // in the order of AllW4Tiles
-    form_of<W4Tile<1, 1, 1, 1, 8, 4, 8>>({0.0367, 0.90, 3.18, 0.0117}, {0.0226, 1.11, 2.83, 0.0099}),
-    form_of<W4Tile<1, 2, 1, 1, 8, 4, 16>>({0.0809, 2.53, 1.90, 0.0194}, {0.0459, 2.57, 1.80, 0.0207}),
-    form_of<W4Tile<1, 1, 1, 1, 8, 4, 32>>({0.0501, 3.10, 1.46, 0.0089}, {0.0325, 3.15, 1.47, 0.0071}),
-    form_of<W4Tile<1, 2, 1, 1, 8, 4, 32>>({0.0856, 3.84, 1.30, 0.0151}, {0.0487, 3.92, 1.24, 0.0207}),
-    form_of<W4Tile<2, 1, 1, 1, 8, 2, 64>>({0.0794, 2.86, 1.48, 0.0106}, {0.0751, 2.55, 1.44, 0.0138}),
-    form_of<W4Tile<2, 2, 1, 1, 4, 4, 64>>({0.1632, 3.73, 1.09, 0.0211}, {0.1352, 3.44, 1.00, 0.0220}),
-    form_of<W4Tile<2, 2, 1, 2, 4, 2, 64>>({0.2767, 3.62, 0.65, 0.0553}, {0.2254, 3.66, 0.53, 0.0548}),
-    form_of<W4Tile<2, 2, 2, 2, 1, 2, 128>>({0.673, 2.38, 2.21, 0.0759}, {0.542, 0.54, 3.66, 0.1118}, 1.108, 0.993),
+    form_of<W4Tile<1, 1, 1, 1, 8, 4, 8>>({0.0345, 0.90, 3.22, 0.0158}, {0.0211, 1.12, 2.84, 0.0119}),
+    form_of<W4Tile<1, 2, 1, 1, 8, 4, 16>>({0.0801, 2.51, 1.98, 0.0172}, {0.0446, 2.58, 1.81, 0.0232}),
+    form_of<W4Tile<1, 1, 1, 1, 8, 4, 32>>({0.0496, 3.03, 1.54, 0.0098}, {0.0307, 3.13, 1.52, 0.0113}),
+    form_of<W4Tile<1, 2, 1, 1, 8, 4, 32>>({0.0849, 3.75, 1.42, 0.0123}, {0.0476, 3.80, 1.40, 0.0211}),
+    form_of<W4Tile<2, 1, 1, 1, 8, 2, 64>>({0.0789, 2.83, 1.61, 0.0099}, {0.0722, 2.56, 1.50, 0.0178}),
+    form_of<W4Tile<2, 2, 1, 1, 4, 4, 64>>({0.1629, 3.71, 1.15, 0.0185}, {0.1333, 3.44, 1.05, 0.0210}),
+    form_of<W4Tile<2, 2, 1, 2, 4, 2, 64>>({0.2719, 3.62, 0.64, 0.0512}, {0.2229, 3.71, 0.53, 0.0551}),
+    form_of<W4Tile<2, 2, 2, 2, 1, 4, 128>>({0.5087, 1.40, 4.05, 0.0660}, {0.3987, 1.91, 3.28, 0.0929}),
 };
 static_assert(sizeof(kForms) / sizeof(Form) == count_of(AllW4Tiles{}), "a row for every tile");
 
@@ -59,16 +58,8 @@ int choose_form(const GemmW4Params& p) {
     const int64_t wgs = (int64_t)((p.M + f.tm - 1) / f.tm) * ((p.N + f.tn - 1) / f.tn);
     if (wgs * f.threads > UINT32_MAX) continue;   // a grid has less than 2^32 threads; 128 x 128 tiles of M N <= 2^37 fit
     const Cost& c = f.cost[p.e2m1];
-    const double pair = f.pair[p.e2m1];
-    int64_t single = (wgs + kCUs - 1) / kCUs, twos = 0, alone = wgs;   // rounds of one and of two a CU; workgroups of the former
-    if (pair > 0) {
-      alone = wgs % (2 * kCUs);
-      twos = wgs / (2 * kCUs) + (alone > kCUs);
-      if (alone > kCUs) alone = 0;
-      single = alone > 0;
-    }
-    const double t = kt * ((double)single * c.step + (double)twos * pair + std::min(1.0, (double)alone / kCUs) * c.busy) +
-                     (double)(single + twos) * c.start + c.once;
+    const double rounds = (double)((wgs + kCUs - 1) / kCUs);
+    const double t = kt * (rounds * c.step + std::min(1.0, (double)wgs / kCUs) * c.busy) + rounds * c.start + c.once;
     if (best < 0 || t < least) {
       best = i;
       least = t;

@@ -204,6 +204,37 @@ def test_w4_forms_are_all_reached():
     assert len({f.split(",")[0] for f in forms}) >= 4, forms
 
 
+TILES = ["8 x 32", "16 x 64", "32 x 32", "32 x 64", "64 x 32", "64 x 64", "64 x 128", "128 x 128"]
+TILE_K = [(64, 64), (96, 32), (128, 128), (320, 64), (480, 96), (640, 128), (960, 192), (1056, 32), (2048, 256)]   # k, group
+
+
+def tile_sizes(tile, K, group, code):
+    """Tokens and channels for which the rule takes a tile: fewest, most and between."""
+    sizes = [(M, N) for M in (1, 5, 8, 13, 16, 30, 32, 61, 64, 90, 127, 300, 700, 1100) for N in (33, 600, 2100, 4100, 8200, 16390)
+             if M * N <= 2310000 and cf.cf_gemm_w4_form(w4_args(M=M, N=N, K=K, group=group, lda=K, lds=N, w_dtype=cf._CODES4[code],
+                                                                ldc=N)).startswith(tile + " ")]
+    return sizes if len(sizes) < 4 else [sizes[0], sizes[len(sizes) // 2], sizes[-1]]
+
+
+def test_w4_every_tile_is_taken():
+    for tile in TILES:
+        for code in VALUES:
+            some = [(K, group) for K, group in TILE_K if tile_sizes(tile, K, group, code)]
+            for kind in (lambda g: g % 64, lambda g: g % 64 == 0 and g % 128, lambda g: g % 128 == 0):
+                assert any(kind(g) for _, g in some), (tile, code)
+
+
+@gpu
+@pytest.mark.parametrize("K,group", TILE_K)
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("code,sdt", [("int4", F32), ("e2m1", BF16), ("int4", BF16)])
+def test_w4_every_tile(tile, K, group, code, sdt):
+    g = gen(K)
+    for M, N in tile_sizes(tile, K, group, code):
+        A, tiles, s, bias = make(g, M, N, K, group, code, sdt, bias=True)
+        check_w4(cf.gemm_w4(A, tiles, s, code=code, bias=bias, out_dtype=F32), A, tiles, s, code, bias)
+
+
 # ---------------------------------------------------------------- refusals (no GPU)
 A_, B_, C_, D_, E_ = (0x7F0000000000 + 0x100000 * i for i in range(5))
 
