@@ -94,14 +94,16 @@ __global__ __launch_bounds__(S::NT) void gemm_w4_kernel(GemmW4Params p, uint32_t
   constexpr int H = FOLD == 32 ? 2 : 1;         // scales of a step
   constexpr bool PAIRS = FOLD == 128;           // two steps a scale
   constexpr int RE = S::AR < 32 ? S::AR / 2 : 16;   // elements of a block that are rows of their own
-  static_assert(!PAIRS || (S::KW == 1 && S::NS % 2 == 0), "steps of a pair follow each other");
+  static_assert(!PAIRS || S::NS % 2 == 0, "a pair's steps are in one turn of the ring");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lg = lane >> 5;
   const int grp = wave / S::GW, gw = wave % S::GW, wm = gw / S::WN, wn = gw % S::WN;
   int rb, c;
   big_tile_order((p.M + S::TM - 1) / S::TM, (p.N + S::TN - 1) / S::TN, rb, c);
   const int m0 = rb * S::TM, n0 = c * S::TN;
-  const int KB = (p.K + 63) / 64, steps = grp < KB ? (KB - grp - 1) / S::KW + 1 : 0;
+  // Steps of 64 k, or pairs of them, go to the groups of waves in turn.
+  constexpr int RUN = PAIRS ? 2 : 1;
+  const int KB = (p.K + 63) / 64, steps = grp < KB / RUN ? ((KB / RUN - grp - 1) / S::KW + 1) * RUN : 0;
   [[maybe_unused]] char* const ring = smem + grp * S::RING;
 
   // Load i of a wave fills rows 8 (i GW + gw) .. + 7 of a stage; rows past M are clamped.  The 16-byte chunk
@@ -127,7 +129,10 @@ __global__ __launch_bounds__(S::NT) void gemm_w4_kernel(GemmW4Params p, uint32_t
   // Tiles begin at different k: together they would read columns of rows that lie a power of two apart, which few
   // channels of the memory hold.
   const int turn = steps > 0 ? (rb * 5 + c) * 3 % steps & (PAIRS ? ~1 : ~0) : 0;
-  auto block = [&](int i) { return grp + (i + turn < steps ? i + turn : i + turn - steps) * S::KW; };
+  auto block = [&](int i) {
+    const int t = i + turn < steps ? i + turn : i + turn - steps;
+    return PAIRS ? 2 * (grp + (t >> 1) * S::KW) + (t & 1) : grp + t * S::KW;
+  };
   u32x4_t wr[S::NS][S::BN];
   T sr[S::NS][S::BN][H];
   auto load = [&](int i, int u) {   // the group's step i, stage and registers u; nothing behind the last
@@ -146,7 +151,7 @@ __global__ __launch_bounds__(S::NT) void gemm_w4_kernel(GemmW4Params p, uint32_t
 #pragma unroll
       for (int h = 0; h < H; ++h) {
         const T* row = reinterpret_cast<const T*>(p.s) + (int64_t)group_of(min(2 * kb + h, p.K / 32 - 1), mul) * p.lds;
-        sr[u][b][h] = row[col[b]];   // (kb is one that K has, for every i)
+        sr[u][b][h] = row[col[b]];
       }
     }
 #endif
@@ -168,21 +173,22 @@ __global__ __launch_bounds__(S::NT) void gemm_w4_kernel(GemmW4Params p, uint32_t
     xa[ks] = s0 + row * 128 + (((2 * ks + lg) ^ ((row >> 1) & 7)) << 4);
   }
   f32x16_t acc[S::BM][S::BN] = {}, part[S::BM][S::BN];
-  if constexpr (S::KW == 1 && FOLD != 32) {
-    // Many tokens: nothing waits for the rest of its own step.  While the MFMAs of 16 k run, the next 16 k are read from
-    // LDS and their weights converted; a stage is loaded again as soon as every wave has read its last part; a group's sums
-    // are added to the tile's before the first MFMA of the next group writes them.  (Against the loop below, us: 1024 x 4096
-    // x 4096 int4 51.5 -> 42.7, 4096 x 4096 x 4096 150 -> 147, 0.94 PFLOP/s, where int4's conversion, 15 vector operations for
-    // 8 codes, and the MFMAs share the issue and the power of a CU; E2M1 124.)
+  if constexpr (FOLD != 32 && S::BN > 1 && (S::KW == 1 || S::GW == 1)) {
+    // Blocks of two and more: nothing waits for the rest of its own step.  While the MFMAs of 16 k run, the next 16 k are
+    // read from LDS and their weights converted; a stage is loaded again as soon as its last part has been read; a
+    // group's sums are added to the tile's before the first MFMA of the next group writes them.  (Against the loop below, us:
+    // 1024 x 4096 x 4096 int4 51.5 -> 43, 4096 x 4096 x 4096 150 -> 147, 0.94 PFLOP/s, where int4's conversion, 15 vector
+    // operations for 8 codes, and the MFMAs share the issue and the power of a CU; E2M1 136 -> 124; 128 and fewer tokens by
+    // 4 to 8 %.  Tiles of single blocks are 2 to 4 % faster below, and waves that share a ring in groups of different
+    // lengths need the barriers there.)
     constexpr int PER = 4 / S::BM;            // pairs of weights converted beside an MFMA
-    constexpr int RUN = PAIRS ? 2 : 1;        // steps between branches
     u32x4_t xf[2][S::BM], v[2][S::BN];
     float sc[S::BN] = {};
 #pragma unroll
     for (int u = 0; u < S::NS; ++u) load(u, u);
 #pragma unroll
     for (int b = 0; b < S::BN; ++b) asm volatile("" : "+v"(wr[0][b])::"memory");
-    lds_barrier();
+    if constexpr (S::GW > 1) lds_barrier();
     static_for<0, S::BM>([&](auto a_t) {
       constexpr int a = decltype(a_t)::value;
       xf[0][a] = ds_read_b128_at<a * 4096>(xa[0]);
@@ -195,14 +201,14 @@ __global__ __launch_bounds__(S::NT) void gemm_w4_kernel(GemmW4Params p, uint32_t
     for (int b = 0; b < S::BN; ++b) v[0][b] = w4_values<E2M1>(word_of(wr[0][b][0]));
     auto fold = [&](int a, int b) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[a][b][e] = fmaf(part[a][b][e], sc[b], acc[a][b][e]);
+      for (int e = 0; e < RE; ++e) acc[a][b][e] = fmaf(part[a][b][e], sc[b], acc[a][b][e]);
     };
 #pragma unroll
     for (int a = 0; a < S::BM; ++a)
 #pragma unroll
       for (int b = 0; b < S::BN; ++b) part[a][b] = f32x16_t{};
     for (int i0 = 0; i0 < steps; i0 += S::NS) {
-      static_for<0, S::NS / RUN>([&](auto run_t) {
+      static_for<0, S::NS / RUN>([&](auto run_t) {   // (no branch within a pair)
         if (i0 + decltype(run_t)::value * RUN >= steps) return;
         static_for<0, 4 * RUN>([&](auto part_t) {
           constexpr int u = decltype(run_t)::value * RUN + decltype(part_t)::value / 4, ks = decltype(part_t)::value % 4;
@@ -236,7 +242,7 @@ __global__ __launch_bounds__(S::NT) void gemm_w4_kernel(GemmW4Params p, uint32_t
               // The next step's weights are waited for, and with them the wave's earlier loads into LDS.
 #pragma unroll
               for (int x = 0; x < S::BN; ++x) asm volatile("" : "+v"(wr[next][x])::"memory");
-              lds_barrier();   // every wave's are in, and this step's stage has been read
+              if constexpr (S::GW > 1) lds_barrier();   // every wave's are in, and this step's stage has been read
               static_for<0, S::BM>([&](auto x_t) {
                 constexpr int x = decltype(x_t)::value;
                 xf[!cur][x] = ds_read_b128_at<x * 4096>(xa[0] + next * S::STAGE);
@@ -260,7 +266,7 @@ __global__ __launch_bounds__(S::NT) void gemm_w4_kernel(GemmW4Params p, uint32_t
 #pragma unroll
       for (int b = 0; b < S::BN; ++b) fold(a, b);
   } else {
-    const int all = (KB + S::KW - 1) / S::KW;   // every group passes every barrier
+    const int all = (KB / RUN + S::KW - 1) / S::KW * RUN;   // every group passes every barrier
 #pragma unroll
     for (int u = 0; u < S::AHEAD; ++u) load(u, u);
     for (int i0 = 0; i0 < all; i0 += S::NS) {
@@ -303,11 +309,12 @@ __global__ __launch_bounds__(S::NT) void gemm_w4_kernel(GemmW4Params p, uint32_t
               const u32x4_t v = w4_values<E2M1>(w[b][ks]);
 #pragma unroll
               for (int a = 0; a < S::BM; ++a) {
-                if (first) part[a][b] = f32x16_t{};
+                if (first && !(PAIRS && u % 2)) part[a][b] = f32x16_t{};
                 Mma<bf16_t>::run(part[a][b], xf[ks][a], v);
               }
             }
             if constexpr (fold) {
+              if (!PAIRS || u % 2)
 #pragma unroll
                 for (int b = 0; b < S::BN; ++b)
 #pragma unroll
@@ -387,8 +394,11 @@ template <class S, bool E2M1, class T>
 hipError_t launch_code(const GemmW4Params& p, hipStream_t st) {
   const int64_t wgs = (int64_t)((p.M + S::TM - 1) / S::TM) * ((p.N + S::TN - 1) / S::TN);
   const uint32_t g32 = p.group / 32, mul = g32 == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + g32 - 1) / g32);
-  if constexpr (S::KW == 1 && S::NS % 2 == 0) {
-    if (p.group % 128 == 0) {
+  // Pairs of steps where sums are folded by more than a block (48 x 12288 x 4096 E2M1 13.6 -> 12.3 us) and every group of
+  // waves has as many pairs, or nearly.
+  if constexpr (S::BM * S::BN > 1) {
+    const int pairs = p.K / 128;
+    if (p.group % 128 == 0 && (pairs % S::KW == 0 || pairs >= 4 * S::KW)) {
       hipLaunchKernelGGL((gemm_w4_kernel<S, E2M1, 128, T>), dim3((unsigned)wgs), dim3(S::NT), 0, st, p, mul);
       return hipGetLastError();
     }

@@ -12,16 +12,16 @@ namespace {
 // share of CUs at work) and `start` besides, and `once`; int4, then E2M1.  (The last tile fits a CU twice; two together
 // take as long as one after the other.)  Fitted to 1 to 4096 tokens, 512 to 16384 channels and 512 to 8192 k, groups of 128;
 // for instance (us, in this order; - not measured):
-//     1 x 4096 x 4096 int4       6.8  9.6  7.8   11  9.5   15   22    -
-//     1 x 12288 x 4096 int4      9.7 10.1   14   11   17   15   22    -
-//     16 x 12288 x 4096 E2M1      11  8.5   12  9.1   16   13   19    -
-//     32 x 4096 x 4096 E2M1      8.8  7.9  7.0  8.7  9.1   13   19   31
-//     48 x 12288 x 4096 E2M1      26   20   19   16   16 13.6   19   31
-//     128 x 4096 x 4096 int4       -    -    -    - 10.6   16   23   40
-//     512 x 4096 x 4096 int4       -    -    -    -   37   32 26.4   42
-//     1024 x 4096 x 4096 int4      -    -    -    -   69   65   47 42.7
-//     4096 x 4096 x 4096 int4      -    -    -    -  270  232  179  142
-// Over the 1011 calls that were timed the tile that the estimate takes is 0.2 % slower than the best one on average, 42 %
+//     1 x 4096 x 4096 int4       6.8  9.3  7.9  9.9  9.0   13   20    -
+//     1 x 12288 x 4096 int4      9.7  9.9   14   10   16   13   20    -
+//     16 x 12288 x 4096 E2M1      11  8.2   12  8.9   16   11   17    -
+//     32 x 4096 x 4096 E2M1      8.5  7.3  7.0  8.2  8.8   11   17   31
+//     48 x 12288 x 4096 E2M1      26   20   19   16   16 12.2   18   31
+//     128 x 4096 x 4096 int4       -    -    -    - 10.0   14   21   40
+//     512 x 4096 x 4096 int4       -    -    -    -   37   29 25.6   45
+//     1024 x 4096 x 4096 int4      -    -    -    -   68   53 44.7 44.8
+//     4096 x 4096 x 4096 int4      -    -    -    -  259  195  164  138
+// Over the 1011 calls that were timed the tile that the estimate takes is 0.4 % slower than the best one on average, 42 %
 // at worst (1024 x 512 x 8192).
 struct Cost {
   double step, start, once, busy;
@@ -38,14 +38,14 @@ constexpr Form form_of(Cost int4, Cost e2m1) {
 template <class... S>
 constexpr int count_of(W4Tiles<S...>) { return (int)sizeof...(S); }
 const Form kForms[] = {   // in the order of AllW4Tiles
-    form_of<W4Tile<1, 1, 1, 1, 8, 4, 8>>({0.0345, 0.90, 3.22, 0.0158}, {0.0211, 1.12, 2.84, 0.0119}),
-    form_of<W4Tile<1, 2, 1, 1, 8, 4, 16>>({0.0801, 2.51, 1.98, 0.0172}, {0.0446, 2.58, 1.81, 0.0232}),
-    form_of<W4Tile<1, 1, 1, 1, 8, 4, 32>>({0.0496, 3.03, 1.54, 0.0098}, {0.0307, 3.13, 1.52, 0.0113}),
-    form_of<W4Tile<1, 2, 1, 1, 8, 4, 32>>({0.0849, 3.75, 1.42, 0.0123}, {0.0476, 3.80, 1.40, 0.0211}),
-    form_of<W4Tile<2, 1, 1, 1, 8, 2, 64>>({0.0789, 2.83, 1.61, 0.0099}, {0.0722, 2.56, 1.50, 0.0178}),
-    form_of<W4Tile<2, 2, 1, 1, 4, 4, 64>>({0.1629, 3.71, 1.15, 0.0185}, {0.1333, 3.44, 1.05, 0.0210}),
-    form_of<W4Tile<2, 2, 1, 2, 4, 2, 64>>({0.2719, 3.62, 0.64, 0.0512}, {0.2229, 3.71, 0.53, 0.0551}),
-    form_of<W4Tile<2, 2, 2, 2, 1, 4, 128>>({0.5087, 1.40, 4.05, 0.0660}, {0.3987, 1.91, 3.28, 0.0929}),
+    form_of<W4Tile<1, 1, 1, 1, 8, 4, 8>>({0.0355, 0.90, 3.20, 0.0138}, {0.0224, 1.10, 2.81, 0.0089}),
+    form_of<W4Tile<1, 2, 1, 1, 8, 4, 16>>({0.0708, 1.35, 3.02, 0.0199}, {0.0396, 2.27, 1.92, 0.0263}),
+    form_of<W4Tile<1, 1, 1, 1, 8, 4, 32>>({0.0505, 3.07, 1.48, 0.0090}, {0.0315, 3.16, 1.46, 0.0091}),
+    form_of<W4Tile<1, 2, 1, 1, 8, 4, 32>>({0.0752, 3.57, 1.41, 0.0181}, {0.0443, 3.56, 1.39, 0.0248}),
+    form_of<W4Tile<2, 1, 1, 1, 8, 2, 64>>({0.0723, 2.90, 1.38, 0.0127}, {0.0725, 2.60, 1.24, 0.0152}),
+    form_of<W4Tile<2, 2, 1, 1, 4, 4, 64>>({0.1235, 3.93, 1.19, 0.0231}, {0.0957, 3.99, 1.00, 0.0253}),
+    form_of<W4Tile<2, 2, 1, 2, 4, 2, 64>>({0.2431, 3.72, 0.58, 0.0535}, {0.1973, 3.80, 0.38, 0.0574}),
+    form_of<W4Tile<2, 2, 2, 2, 1, 4, 128>>({0.5094, 1.29, 4.14, 0.0699}, {0.3973, 1.53, 3.66, 0.0913}),
 };
 static_assert(sizeof(kForms) / sizeof(Form) == count_of(AllW4Tiles{}), "a row for every tile");
 

@@ -205,7 +205,7 @@ def test_w4_forms_are_all_reached():
 
 
 TILES = ["8 x 32", "16 x 64", "32 x 32", "32 x 64", "64 x 32", "64 x 64", "64 x 128", "128 x 128"]
-TILE_K = [(64, 64), (96, 32), (128, 128), (320, 64), (480, 96), (640, 128), (960, 192), (1056, 32), (2048, 256)]   # k, group
+TILE_K = [(64, 64), (96, 32), (128, 128), (320, 64), (480, 96), (640, 128), (960, 192), (1056, 32), (2048, 256), (2080, 32), (2112, 192)]   # k, group
 
 
 def tile_sizes(tile, K, group, code):
