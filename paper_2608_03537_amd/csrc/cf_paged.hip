@@ -141,7 +141,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
     M[rt] = kLowestF32;
     L[rt] = 0.0f;
   }
-  const float cap = p.softcap, sl = cap > 0.0f ? p.scale / cap : p.scale * 1.4426950408889634f;
+  const float cap = p.softcap, sl = (cap > 0.0f ? 2.0f * p.scale / cap : p.scale) * 1.4426950408889634f;
   const float cap2 = cap * 1.4426950408889634f;
 
   // The pages of a step's two tiles (one where pages hold 32 tokens and more).  Their entries are asked for a step
@@ -253,7 +253,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
     const bool masked = k0 + kStepKeys > first || bad0 || bad1;
     pages = resolve(next, ahead);
     ahead = look_up(next + kWaves);
-    // S^T, in log2 units; with a cap its argument first
+    // S^T, in log2 units; with a cap twice its argument first: tanh z = 1 - 2 / (1 + exp 2 z)
     float s[RT][8];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[rt][e] = cap2 * tanh_exp(s[rt][e]);
+        for (int e = 0; e < 8; ++e) s[rt][e] = fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[rt][e])), cap2);
     }
     if (masked) {
 #pragma unroll
