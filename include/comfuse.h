@@ -536,7 +536,8 @@ const char* cf_gemm_w4_form(const cf_gemm_w4_args* a);
  * text has one axis); the sections of the n_axes <= 4 axes add up to rot / 2.  pos: int32, n_axes
  * rows of T, ldpos apart; freq: fp32 [rot / 2].  The angle is a product in 64
  * bits, and so are its cosine and sine, which are then rounded to fp32; the
- * rotation is in fp32 (an angle of 2^45 and more turns its pair into NaN).  rot = 0: no rotation (pos, freq unused); rot is a multiple of 16, <= d.
+ * rotation is in fp32 (an angle of 2^45 and more turns its pair into NaN).  rot is a multiple of 16,
+ * <= d; rot = 0: no rotation (pos, freq unused).
  * Q (T x H rows of d, bf16; H = 0: none) comes back rotated in Qo, which may be Q
  * itself with the same strides.  K and V (T x Hk rows of d, bf16) go to slot
  * slots[t] (int32): a slot outside [0, n_pages * page) is padding, and not written.
