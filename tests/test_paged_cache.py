@@ -2,6 +2,7 @@
 attention over it, against the definitions in 64 bits; and a decoding step of all.
 u is fp32's half step; each bound counts roundings."""
 import math
+import threading
 
 import pytest
 import torch
@@ -455,6 +456,81 @@ def test_paged_repeatable_own_workspace_and_streams():
     got = [call(ws=ws), call(stream=s), call()]
     torch.cuda.synchronize()
     assert all(torch.equal(want, x) for x in got) and not ws[:cf.CF_PAGED_WS_HEADER_BYTES].any()
+
+
+@gpu
+@pytest.mark.parametrize("code,B,Hk,most,d", [("bf16", 12, 8, 4300, 128), ("int8", 40, 8, 2500, 128), ("e4m3", 70, 8, 2800, 64)])
+@pytest.mark.parametrize("Lq", [1, 3, 6])
+def test_paged_large_cache(code, B, Hk, most, d, Lq):
+    """More rows than the last-level cache holds are read past it."""
+    g = gen(B)
+    Q, cache, table = paged_case(g, B, 4 * Hk, Hk, Lq, most, d, 64, code)
+    lens = torch.randint(1, most + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    form = cf.cf_attention_paged_form(paged_args(batch=B, H=4 * Hk, Hk=Hk, Lq=Lq, d=d, pages=table.shape[1], page=64,
+                                                 code_dtype={"bf16": cf.CF_BF16, "int8": cf.CF_I8, "e4m3": cf.CF_FP8_E4M3}[code]))
+    assert form.endswith("read once"), form
+    O = cf.attention_paged(Q, cache[0], cache[1], table, lens, cache[2], cache[3], causal=Lq > 1)
+    check_paged(O, Q, cache, code, table, lens, 64, Lq > 1)
+
+
+@gpu
+def test_paged_two_graphs_and_threads():
+    """Two graphs replayed beside each other and beside eager calls of two threads that share a stream."""
+    cases = []
+    for seed in (1, 2):
+        Q, cache, table = paged_case(gen(seed), 2, 16, 2, 2, 6000, 128, 16, "int8")
+        lens = torch.tensor([6000, 2000 + seed], dtype=torch.int32, device="cuda")
+        cases.append((Q, cache[0], cache[1], table, lens, cache[2], cache[3]))
+    want = [cf.attention_paged(*c, causal=True) for c in cases]
+    graphs, outs, streams = [], [], [torch.cuda.Stream() for _ in cases]
+    for c in cases:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append([cf.attention_paged(*c, causal=True) for _ in range(3)])
+        graphs.append(graph)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for o in outs[0] + outs[1]:
+            o.zero_()
+        torch.cuda.synchronize()
+        got = [[], []]
+
+        def eager(i):
+            got[i] += [cf.attention_paged(*cases[i], causal=True) for _ in range(20)]
+
+        threads = [threading.Thread(target=eager, args=(i,)) for i in (0, 1)]
+        for t in threads:
+            t.start()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+                graph.replay()
+        for t in threads:
+            t.join()
+        torch.cuda.synchronize()
+        for i in (0, 1):
+            assert len(got[i]) == 20 and all(torch.equal(want[i], o) for o in got[i] + outs[i])
+
+
+@gpu
+def test_cache_operators_on_another_stream():
+    g = gen(12)
+    s = torch.cuda.Stream()
+    caches = [cf.cache_pages(20, 4, 16, 64, "e4m3") for _ in range(2)]
+    k, v, q = (torch.randn((100, h, 64), generator=g, device="cuda").to(BF16) for h in (4, 4, 8))
+    slots, pos = torch.randperm(320, generator=g, device="cuda")[:100].to(torch.int32), torch.arange(100, dtype=torch.int32, device="cuda")
+    table, lens = torch.arange(20, dtype=torch.int32, device="cuda").view(2, 10), torch.tensor([150, 77], dtype=torch.int32, device="cuda")
+    freq = torch.rand((32,), generator=g, device="cuda")
+    s.wait_stream(torch.cuda.current_stream())
+    got = []
+    for c, kw in zip(caches, ({}, {"stream": s})):
+        r = cf.cache_write(k, v, slots, *c, q=q, pos=pos, freq=freq, **kw)
+        K, V = (torch.zeros((2, 4, 160, 64), dtype=BF16, device="cuda") for _ in range(2))
+        torch.cuda.synchronize()
+        cf.cache_read(c[0], c[1], table, lens, c[2], c[3], out=(K, V), **kw)
+        got.append((r, K, V, *c))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and bool(got[0][1].any())
 
 
 # ---------------------------------------------------------------- a decoding step

@@ -73,7 +73,8 @@ def test_pack(N, K):
 @gpu
 @pytest.mark.parametrize("code,top", [("int4", 7.0), ("e2m1", 6.0)])
 @pytest.mark.parametrize("dtype,sdt", [(BF16, BF16), (BF16, F32), (F32, F32)])
-@pytest.mark.parametrize("N,K,group", [(1, 32, 32), (37, 96, 96), (64, 256, 128), (130, 1056, 32), (5, 640, 64)])
+@pytest.mark.parametrize("N,K,group", [(1, 32, 32), (37, 96, 96), (64, 256, 128), (130, 1056, 32), (5, 640, 64), (33, 1056, 1056), (40, 2048, 1024),
+                                       (7, 4128, 1376), (3, 1152, 576)])
 def test_quant(N, K, group, dtype, sdt, code, top):
     g = gen(N * K)
     W = padded(N, K, dtype, g, pad=16)
@@ -202,6 +203,52 @@ def test_w4_forms_are_all_reached():
                 a = w4_args(M=M, N=N, K=4096, group=group, ldc=N, lda=4096, lds=N)
                 forms.add(cf.cf_gemm_w4_form(a))
     assert len({f.split(",")[0] for f in forms}) >= 4, forms
+
+
+@gpu
+def test_w4_offsets_pass_32_bits():
+    """More than 2^32 bytes of output, and of weights: the last rows and channels are those of a small call."""
+    g = gen(1)
+    M, N, K = 70001, 33000, 64
+    A, tiles, s, _ = make(g, M, N, K, 32, "int4", F32)
+    C = cf.gemm_w4(A, tiles, s)
+    assert C.numel() * 2 > 2 ** 32
+    check_w4(C[-300:], A[-300:], tiles, s, "int4", None)
+    del C
+    N, K = 1 << 20, 8256
+    codes = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    tiles = cf.w4_pack(codes)
+    assert tiles.numel() > 2 ** 32
+    s = torch.rand((1, N), generator=g, device="cuda")
+    A = padded(3, K, BF16, g)
+    last = cf.w4_pack(codes[-64:].contiguous())
+    assert torch.equal(tiles[-2:], last)
+    check_w4(cf.gemm_w4(A, tiles, s)[:, -64:], A, last, s[:, -64:], "int4", None)
+
+
+@gpu
+def test_w4_repeatable_on_streams_and_captured():
+    """The same bits again, on another stream and from a graph replayed with new tokens between eager calls."""
+    g = gen(3)
+    for M in (1, 48, 1100):
+        A, tiles, s, bias = make(g, M, 2100, 512, 128, "int4", F32, bias=True)
+        B, _, _, _ = make(g, M, 2100, 512, 128, "int4", F32)
+        call = lambda **kw: cf.gemm_w4(A, tiles, s, bias=bias, act="gelu", **kw)  # noqa: E731
+        first = call()
+        other = torch.cuda.Stream()
+        other.wait_stream(torch.cuda.current_stream())
+        on = call(stream=other)
+        torch.cuda.synchronize()
+        assert torch.equal(first, on)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            C = call()
+        for x in (B, A.clone(), B):
+            A.copy_(x)
+            graph.replay()
+            want = call()
+            torch.cuda.synchronize()
+            assert torch.equal(C, want)
 
 
 TILES = ["8 x 32", "16 x 64", "32 x 32", "32 x 64", "64 x 32", "64 x 64", "64 x 128", "128 x 128"]
