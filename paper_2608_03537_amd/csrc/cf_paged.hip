@@ -101,8 +101,8 @@ struct Joined {   // running join of parts: maximum, sum, 8 d
   }
 };
 
-// MIXED: rows of a block may see different keys, and a value may be infinite or NaN (a check and a second
-// way for such a step, which cost a call without them 0.5 of 9.2 us).
+// MIXED: rows of a block may see different keys, and a value may be infinite or NaN (a check and products of their own for
+// such a step; kept out of other calls, which the longer code would cost up to 5 %).
 template <int D, int CODE, int RT, bool ONCE, bool MIXED>
 __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, int nrb, int parts, unsigned* count) {
   using A = PagedShape<D, CODE, RT>;
@@ -349,43 +349,48 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
       }
       return a;
     };
-    bool alone = false;
+    // MIXED: where rows of a step see different keys, an infinity or a NaN must not reach a row that does not see it (0 times
+    // it would be NaN).  Such values are left out of the product; rows that see them are found by a product of ones.
+    bool spoiled = false;
     if (MIXED && masked) {
-      // Keys that some rows see and others do not: 0 times an infinity or a NaN would reach the others.
-      constexpr uint32_t kExp = CODE == CACHE_BF16 ? 0x7f807f80u : 0x7f7f7f7fu, kOne = CODE == CACHE_BF16 ? 0x00800080u : 0x01010101u;
+      constexpr uint32_t kExp = CODE == CACHE_BF16 ? 0x7F807F80u : 0x7F7F7F7Fu, kOne = CODE == CACHE_BF16 ? 0x00800080u : 0x01010101u;
       uint32_t x = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int w = 0; w < A::VW; ++w) x |= (vf[i][w] & kExp) + kOne;
-      alone = __any((x & ~kExp & (CODE == CACHE_BF16 ? 0x80008000u : 0x80808080u)) != 0);
+      spoiled = __any((x & (CODE == CACHE_BF16 ? 0x80008000u : 0x80808080u)) != 0);
     }
-    if (!alone) {
 #pragma unroll
-      for (int d = 0; d < A::DT; ++d) {
-        const u32x4_t a = values(d);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) O[rt][d] = mfma16(a, pf[rt], O[rt][d]);
-      }
-    } else {   // such a value is there: key by key, kept by the rows that see it
-#pragma unroll 1
-      for (int k = 0; k < kStepKeys; ++k) {
-        u32x4_t only;
+    for (int d = 0; d < A::DT; ++d) {
+      u32x4_t a = values(d);
+      if (MIXED && spoiled) {
+        constexpr uint32_t kOnes = 0x3F803F80u;   // 1, 1
+        u32x4_t up, down;                         // ones for + infinity and NaN, and for - infinity and NaN
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const int e = (k >> 4) * 4 + (k & 3) - 2 * x;
-          only[x] = (k >> 2 & 3) != q ? 0u : e == 0 ? 0x0000ffffu : e == 1 ? 0xffff0000u : 0u;
+          const uint32_t all = ((((a[x] & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xFFFFu;   // not finite
+          const uint32_t nan = ((((a[x] & 0x007F007Fu) + 0x007F007Fu) >> 7) & 0x00010001u) * 0xFFFFu;
+          const uint32_t neg = ((a[x] >> 15) & 0x00010001u) * 0xFFFFu;
+          up[x] = all & (nan | ~neg) & kOnes;
+          down[x] = all & (nan | neg) & kOnes;
+          a[x] &= ~all;
         }
 #pragma unroll
-        for (int d = 0; d < A::DT; ++d) {
-          const u32x4_t a = values(d) & only;
+        for (int rt = 0; rt < RT; ++rt) {
+          u32x4_t sees;
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            const f32x4_t o = mfma16(a, pf[rt] & only, O[rt][d]);
-            if (k0 + k < seen[rt]) O[rt][d] = o;
+          for (int x = 0; x < 4; ++x) {
+            const int key = k0 + 16 * (x >> 1) + 4 * q + 2 * (x & 1);
+            sees[x] = (key < seen[rt] ? 0x00003F80u : 0u) | (key + 1 < seen[rt] ? 0x3F800000u : 0u);
           }
+          const f32x4_t u = mfma16(up, sees, f32x4_t{}), n = mfma16(down, sees, f32x4_t{});
+#pragma unroll
+          for (int i = 0; i < 4; ++i) O[rt][d][i] += (u[i] > 0.0f ? INFINITY : 0.0f) + (n[i] > 0.0f ? -INFINITY : 0.0f);
         }
       }
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) O[rt][d] = mfma16(a, pf[rt], O[rt][d]);
     }
     load_v(next, pages);
   }
