@@ -1672,6 +1672,9 @@ static cf_status paged_sizes(const cf_attention_paged_args* a, PagedParams& p) {
   if (a->causal != 0 && a->causal != 1) return fail(CF_ERR_UNSUPPORTED, "causal must be 0 or 1");
   if (!std::isfinite(a->scale) || !(a->scale > 0.0f)) return fail(CF_ERR_SHAPE, "scale must be finite and > 0");
   if (!std::isfinite(a->softcap) || !(a->softcap >= 0.0f)) return fail(CF_ERR_SHAPE, "softcap must be finite and >= 0");
+  // the scores' factors, in powers of two (an infinite one would make NaN of a score of 0)
+  if (!std::isfinite(a->scale * 1.5f) || (a->softcap > 0.0f && !(std::isfinite(a->scale / a->softcap * 3.0f) && std::isfinite(a->softcap * 3.0f))))
+    return fail(CF_ERR_SHAPE, "scale, scale / softcap or softcap is too large");
   const cf_status s = check_cache(a->cache, a->Hk, a->d, true, p.c);
   if (s != CF_OK) return s;
   if (a->pages > kPagedMaxKeys / a->cache.page) return fail(CF_ERR_SHAPE, "pages * page exceeds 2^30");

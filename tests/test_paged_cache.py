@@ -678,6 +678,7 @@ def paged_args(**kw):
     (dict(batch=-1), "CF_ERR_SHAPE"), (dict(batch=65535, H=512, Lq=64), "CF_ERR_SHAPE"), (dict(H=5), "CF_ERR_SHAPE"), (dict(Lq=65), "CF_ERR_UNSUPPORTED"),
     (dict(pages=-1), "CF_ERR_SHAPE"), (dict(causal=2), "CF_ERR_UNSUPPORTED"), (dict(scale=0.0), "CF_ERR_SHAPE"),
     (dict(scale=math.nan), "CF_ERR_SHAPE"), (dict(softcap=-1.0), "CF_ERR_SHAPE"), (dict(softcap=math.inf), "CF_ERR_SHAPE"),
+    (dict(scale=3e38), "CF_ERR_SHAPE"), (dict(softcap=1e-44), "CF_ERR_SHAPE"), (dict(softcap=2e38), "CF_ERR_SHAPE"),
     (dict(Q=None), "CF_ERR_NULL"), (dict(O=None), "CF_ERR_NULL"), (dict(table=None), "CF_ERR_NULL"), (dict(lens=None), "CF_ERR_NULL"),
     (dict(q_l=260), "CF_ERR_ALIGN"), (dict(o_b=0), "CF_ERR_LD"), (dict(O=E_), "CF_ERR_ALIAS"), (dict(O=A_), "CF_ERR_ALIAS"),
     (dict(O=D_), "CF_ERR_ALIAS"), (dict(O=G_), "CF_ERR_ALIAS")])
