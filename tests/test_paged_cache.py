@@ -533,6 +533,28 @@ def test_cache_operators_on_another_stream():
     assert all(torch.equal(a, b) for a, b in zip(*got)) and bool(got[0][1].any())
 
 
+@gpu
+def test_helpers_of_nothing():
+    """No tokens, no sequences, no queries, no rows, no pages, no weights' tokens."""
+    cache = cf.cache_pages(4, 2, 16, 64, "int8")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    none = torch.zeros((0, 2, 64), dtype=BF16, device="cuda")
+    freq = torch.ones((32,), device="cuda")
+    q = cf.cache_write(none, none, torch.zeros((0,), **i32), *cache, q=torch.zeros((0, 4, 64), dtype=BF16, device="cuda"),
+                       pos=torch.zeros((0,), **i32), freq=freq)
+    assert q.shape == (0, 4, 64) and not any(t.any() for t in cache)
+    for B, pages in ((0, 3), (2, 0)):
+        table, lens = torch.zeros((B, pages), **i32), torch.full((B,), 5, **i32)
+        K, V = cf.cache_read(cache[0], cache[1], table, lens, cache[2], cache[3])
+        assert K.shape == V.shape == (B, 2, pages * 16, 64)
+        for Lq in (0, 1, 2):
+            Q = torch.ones((B, 4, Lq, 64), dtype=BF16, device="cuda")
+            O = cf.attention_paged(Q, cache[0], cache[1], table, lens, cache[2], cache[3], causal=Lq > 1)
+            assert O.shape == Q.shape and not O.any()
+    tiles, s = cf.w4_quant(torch.ones((40, 64), device="cuda"), 32)
+    assert cf.gemm_w4(torch.zeros((0, 64), dtype=BF16, device="cuda"), tiles, s).shape == (0, 40)
+
+
 # ---------------------------------------------------------------- a decoding step
 class Step:
     """One layer's attention block of a decoding step: 4-bit projection, rotation and cache write, attention, 4-bit projection."""
