@@ -634,7 +634,8 @@ typedef struct {
 size_t    cf_attention_paged_workspace(const cf_attention_paged_args* a);
 cf_status cf_attention_paged(const cf_attention_paged_args* a, void* workspace, size_t ws_bytes, void* hip_stream);
 
-/* How a call of these sizes is cut, in words; as cf_gemm_i8_form. */
+/* How a call of these sizes is cut, in words; as cf_gemm_i8_form.  Parts, and whether rows are read past the caches, are
+ * those of sequences that fill their tables; each sequence takes what its own length asks for. */
 const char* cf_attention_paged_form(const cf_attention_paged_args* a);
 
 /* ------------------------------------------------------------------------

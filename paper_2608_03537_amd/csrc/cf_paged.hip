@@ -19,6 +19,7 @@
 // softmax (16 sequences of 4 key heads of 4, 5 queries, 4095 E4M3 keys of 64: 15.1 us).  One sequence: its start, the
 // parts' way through the workspace and the launch (4096 bf16 keys, 8 key heads of 4: 9.2 us).
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 
 #include "cf_attn.h"
@@ -101,21 +102,57 @@ struct Joined {   // running join of parts: maximum, sum, 8 d
   }
 };
 
+// The parts that a block of `steps` steps of 32 keys is cut into, of `most` that are launched.  They go by the length: a table,
+// above all in a captured call, may be far wider than its sequences.  One part more shortens the way over the keys and lengthens
+// the join's, so the best number goes with the root of the keys, and is less where a partial result has more rows; it is less
+// again (0.7) where the parts are more than the CUs (`few`: CUs a block); then as few parts as leave the longest wave its
+// steps.  Up to kOneSteps the way through the workspace, 1 to 3 us, costs more than it gives.  Found with 110 calls (1 to 16
+// sequences, 150 to 8000 keys) under tables of 65536 keys, in 1 to 32 parts each: 15 % faster than parts of 128 keys and more,
+// at best twice as fast; 240 random calls whose tables are at most twice as wide as needed are 5 % faster, 12 % slower at
+// worst.  For instance (us; parts 1, 2, 4, 8, 16, 32):
+//     4 x 8 key heads of 4 heads, 350 keys, bf16, d 128       7.8  8.0  7.2  8.1  8.1  8.2
+//     8 x 8 of 4, 700 keys, int8, d 64                        9.6  9.3  8.9  9.5   12   12
+//     1 x 8 of 4, 6 queries, 2500 keys, bf16, d 128            38   25   17   15   17   24
+//     1 x 8 of 4, 8000 keys, E4M3, d 64                        54   33   20   13   11   11
+template <int D>
+constexpr int kOneSteps = D == 128 ? 14 : 18;
+template <int D, int RT>
+__device__ __forceinline__ int parts_of(int steps, int most, int few) {
+  if (steps <= kOneSteps<D>) return 1;
+  auto whole = [](float x) { return __builtin_amdgcn_readfirstlane((int)x); };
+  const float root = __builtin_amdgcn_sqrtf((float)steps * (2.0f / RT));
+  int n = max(1, min(most, whole(root)));
+  if (n > few) n = max(few, min(most, whole(root * 0.7f)));
+  const int each = whole((float)(steps - 1) * __builtin_amdgcn_rcpf((float)(n * kWaves))) + 1;   // steps of the longest wave
+  return min(n, whole((float)(steps - 1) * __builtin_amdgcn_rcpf((float)(each * kWaves))) + 1);
+}
+
+// Bytes of the keys and values in use from which their lines are not kept: the last-level cache has 256 MB, and a call over
+// more finds little of it there next time (215 MB: 48.3 -> 46.3 us so; 98 MB in it: 19.8 -> 20.7).  A table may be far wider
+// than its sequences, so a workgroup decides by its own length, as if all were as long.
+constexpr int64_t kOnceBytes = 192 << 20;
+__host__ __device__ constexpr bool read_past(int64_t keys, int Hk, int d, bool bf16) {
+  return keys * Hk > kOnceBytes / (2 * (bf16 ? 2 * d : d + 4));
+}
+
 // MIXED: rows of a block may see different keys, and a value may be infinite or NaN (a check and products of their own for
 // such a step; kept out of other calls, which the longer code would cost up to 5 %).
+// ONCE: the table has room for so many keys that they may be read past the caches.
 template <int D, int CODE, int RT, bool ONCE, bool MIXED>
-__global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, int nrb, int parts, unsigned* count) {
+__global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, int nrb, int parts, int few, unsigned* count) {
   using A = PagedShape<D, CODE, RT>;
   __shared__ __attribute__((aligned(16))) char smem[A::LDS];
   __shared__ int last_one;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, q = lane >> 4;
+  // Parts go slowest through the grid: a sequence may have fewer than are launched, and those in use then lie beside each other,
+  // on all XCDs (parts beside each other: 4 sequences of 1000 int8 keys, 32 heads of 8, under a wide table 9.1 -> 10.3 us).
   int task = blockIdx.x;
   const int rb = task % nrb;
   task /= nrb;
-  const int z = task % parts;
-  task /= parts;
-  const int hk = task % p.Hk, b = task / p.Hk;
+  const int hk = task % p.Hk;
+  task /= p.Hk;
+  const int z = task / p.B, b = (task % p.B + z * (p.B / parts)) % p.B;
   const int G = p.H / p.Hk, R = G * p.Lq, m0 = rb * A::ROWS;
 
   // Q fragments (on their way while the length is looked up).  16-byte pieces of a row of codes hold two steps' d of a lane.
@@ -133,9 +170,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
   const int last = paged_seen(p, len, (min(m0 + A::ROWS, R) - 1) / G);   // keys that some row sees
   const int first = paged_seen(p, len, m0 / G);                          // ... that every row sees
   const int steps = (last + kStepKeys - 1) / kStepKeys;
-  const int np = max(1, min(parts, (steps + kWaves - 1) / kWaves));      // parts of this block in use
+  const int np = parts_of<D, RT>(steps, parts, few);                          // parts of this block in use
   if (z >= np) return;
-  const int j0 = (int)((int64_t)steps * z / np), j1 = (int)((int64_t)steps * (z + 1) / np);
+  const int j0 = (int)((uint32_t)steps * z / np), j1 = (int)((uint32_t)steps * (z + 1) / np);   // (steps <= 2^25, np <= 64)
   int seen[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) seen[rt] = paged_seen(p, len, min(m0 + 16 * rt + c, R - 1) / G);
@@ -170,8 +207,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
   };
   // A tile is read through a buffer that ends behind the last key that some row sees (of no bytes where there is no
   // page): what lies there comes back as 0, whatever it holds.  A step behind the last reads nothing, so that no branch hides
-  // how many loads are under way.  ONCE: the cache is larger than the last level's, so its lines are not kept.
-  [[maybe_unused]] constexpr int kHint = ONCE ? 2 : 0;
+  // how many loads are under way.
   u32x4_t kf[2][A::KL];
   uint32_t vf[8][A::VW];
   f32x4_t ksc[2], vsc[2];
@@ -193,7 +229,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
   const char* const ksbase = reinterpret_cast<const char*>(p.c.Ks + hk * p.c.ks_h);
   const char* const vsbase = reinterpret_cast<const char*>(p.c.Vs + hk * p.c.vs_h);
 #endif
-  auto load_k = [&](int j, Pages pg) {
+  auto load_k = [&](int j, Pages pg, auto hint_t) {
+    [[maybe_unused]] constexpr int kHint = decltype(hint_t)::value;
 #if defined(__HIP_DEVICE_COMPILE__)
     const int key = j * kStepKeys;
     uint64_t at[2];
@@ -213,7 +250,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
     }
 #endif
   };
-  auto load_v = [&](int j, Pages pg) {
+  auto load_v = [&](int j, Pages pg, auto hint_t) {
+    [[maybe_unused]] constexpr int kHint = decltype(hint_t)::value;
 #if defined(__HIP_DEVICE_COMPILE__)
     const int key = j * kStepKeys;
     uint64_t at[2];
@@ -245,155 +283,160 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
 #endif
   };
 
-  Pages pages = {}, ahead = {};   // of the step whose rows are under way, and the entries of the one after it
-  if (j0 + wave < j1) {
-    pages = resolve(j0 + wave, look_up(j0 + wave));
-    load_k(j0 + wave, pages);
-    load_v(j0 + wave, pages);
-    ahead = look_up(j0 + wave + kWaves);
-  }
-  for (int j = j0 + wave; j < j1; j += kWaves) {
-    const int next = j + kWaves;
-    const int k0 = j * kStepKeys;
-    const bool bad0 = pages.at[0] < 0, bad1 = pages.at[1] < 0;
-    const bool masked = k0 + kStepKeys > first || bad0 || bad1;
-    pages = resolve(next, ahead);
-    ahead = look_up(next + kWaves);
-    // S^T, in log2 units; with a cap twice its argument first: tanh z = 1 - 2 / (1 + exp 2 z)
-    float s[RT][8];
+  // The way over the part's keys, a loop for each hint (branches around the loads: 64 x 8192 int8 keys 1 % slower, E4M3 4 %).
+  auto walk = [&](auto hint) {
+    Pages pages = {}, ahead = {};   // of the step whose rows are under way, and the entries of the one after it
+    if (j0 + wave < j1) {
+      pages = resolve(j0 + wave, look_up(j0 + wave));
+      load_k(j0 + wave, pages, hint);
+      load_v(j0 + wave, pages, hint);
+      ahead = look_up(j0 + wave + kWaves);
+    }
+    for (int j = j0 + wave; j < j1; j += kWaves) {
+      const int next = j + kWaves;
+      const int k0 = j * kStepKeys;
+      const bool bad0 = pages.at[0] < 0, bad1 = pages.at[1] < 0;
+      const bool masked = k0 + kStepKeys > first || bad0 || bad1;
+      pages = resolve(next, ahead);
+      ahead = look_up(next + kWaves);
+      // S^T, in log2 units; with a cap twice its argument first: tanh z = 1 - 2 / (1 + exp 2 z)
+      float s[RT][8];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      u32x4_t a[A::KS];
+      for (int t = 0; t < 2; ++t) {
+        u32x4_t a[A::KS];
 #pragma unroll
-      for (int ks = 0; ks < A::KS; ++ks) {
-        if constexpr (CODE == CACHE_BF16) a[ks] = kf[t][ks];
-        else {
-          const uint32_t w0 = kf[t][ks >> 1][2 * (ks & 1)], w1 = kf[t][ks >> 1][2 * (ks & 1) + 1];
-          a[ks] = u32x4_t{codes_bf16<CODE, 0>(w0), codes_bf16<CODE, 1>(w0), codes_bf16<CODE, 0>(w1), codes_bf16<CODE, 1>(w1)};
+        for (int ks = 0; ks < A::KS; ++ks) {
+          if constexpr (CODE == CACHE_BF16) a[ks] = kf[t][ks];
+          else {
+            const uint32_t w0 = kf[t][ks >> 1][2 * (ks & 1)], w1 = kf[t][ks >> 1][2 * (ks & 1) + 1];
+            a[ks] = u32x4_t{codes_bf16<CODE, 0>(w0), codes_bf16<CODE, 1>(w0), codes_bf16<CODE, 0>(w1), codes_bf16<CODE, 1>(w1)};
+          }
         }
-      }
-      f32x4_t sc = {sl, sl, sl, sl};
-      if constexpr (CODE != CACHE_BF16)
+        f32x4_t sc = {sl, sl, sl, sl};
+        if constexpr (CODE != CACHE_BF16)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sc[i] *= ksc[t][i];
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        f32x4_t acc = {};
-#pragma unroll
-        for (int ks = 0; ks < A::KS; ++ks) acc = mfma16(a[ks], qf[rt][ks], acc);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[rt][4 * t + i] = acc[i] * sc[i];
-      }
-    }
-    load_k(next, pages);
-    if (cap > 0.0f) {
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[rt][e] = fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[rt][e])), cap2);
-    }
-    if (masked) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int key = k0 + 16 * (e >> 2) + 4 * q + (e & 3);
-        const bool bad = e < 4 ? bad0 : bad1;
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-          if (bad || key >= seen[rt]) s[rt][e] = -INFINITY;
-      }
-    }
-    u32x4_t pf[RT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      float mx = s[rt][0];
-#pragma unroll
-      for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[rt][e]);
-      // The maximum is raised, and what was summed rescaled, only where a score passes it by 2^8.
-      if (__any(mx > M[rt] + 8.0f)) {
-        const float mn = fmaxf(M[rt], quad_max(mx)), f = __builtin_amdgcn_exp2f(M[rt] - mn);
-        M[rt] = mn;
-        L[rt] *= f;
-#pragma unroll
-        for (int d = 0; d < A::DT; ++d)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) O[rt][d][i] *= f;
-      }
-      float w[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        w[e] = __builtin_amdgcn_exp2f(s[rt][e] - M[rt]);
-        L[rt] += w[e];
-        if constexpr (CODE != CACHE_BF16) {
-          w[e] *= vsc[e >> 2][e & 3];
-        }
-      }
-      if (CODE != CACHE_BF16 && masked)   // whatever the scale of a hidden row holds
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = s[rt][e] == -INFINITY ? 0.0f : w[e];
-      pf[rt] = u32x4_t{pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7])};
-    }
-    // O^T += V^T P^T
-    auto values = [&](int d) {
-      u32x4_t a;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        if constexpr (CODE == CACHE_I8) {
-          a[x] = pack_bf16x2((float)(int8_t)(vf[2 * x][d / 4] >> (8 * (d % 4))), (float)(int8_t)(vf[2 * x + 1][d / 4] >> (8 * (d % 4))));
-        } else if constexpr (CODE == CACHE_E4M3) {
-          const uint32_t e0 = d % 4 / 2 ? codes_bf16<CODE, 1>(vf[2 * x][d / 4]) : codes_bf16<CODE, 0>(vf[2 * x][d / 4]);
-          const uint32_t e1 = d % 4 / 2 ? codes_bf16<CODE, 1>(vf[2 * x + 1][d / 4]) : codes_bf16<CODE, 0>(vf[2 * x + 1][d / 4]);
-          a[x] = __builtin_amdgcn_perm(e1, e0, d % 2 ? 0x07060302u : 0x05040100u);
-        } else {
-          a[x] = __builtin_amdgcn_perm(vf[2 * x + 1][d / 2], vf[2 * x][d / 2], d % 2 ? 0x07060302u : 0x05040100u);
-        }
-      }
-      return a;
-    };
-    // MIXED: where rows of a step see different keys, an infinity or a NaN must not reach a row that does not see it (0 times
-    // it would be NaN).  Such values are left out of the product; rows that see them are found by a product of ones.
-    bool spoiled = false;
-    if (MIXED && masked) {
-      constexpr uint32_t kExp = CODE == CACHE_BF16 ? 0x7F807F80u : 0x7F7F7F7Fu, kOne = CODE == CACHE_BF16 ? 0x00800080u : 0x01010101u;
-      uint32_t x = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int w = 0; w < A::VW; ++w) x |= (vf[i][w] & kExp) + kOne;
-      spoiled = __any((x & (CODE == CACHE_BF16 ? 0x80008000u : 0x80808080u)) != 0);
-    }
-#pragma unroll
-    for (int d = 0; d < A::DT; ++d) {
-      u32x4_t a = values(d);
-      if (MIXED && spoiled) {
-        constexpr uint32_t kOnes = 0x3F803F80u;   // 1, 1
-        u32x4_t up, down;                         // ones for + infinity and NaN, and for - infinity and NaN
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const uint32_t all = ((((a[x] & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xFFFFu;   // not finite
-          const uint32_t nan = ((((a[x] & 0x007F007Fu) + 0x007F007Fu) >> 7) & 0x00010001u) * 0xFFFFu;
-          const uint32_t neg = ((a[x] >> 15) & 0x00010001u) * 0xFFFFu;
-          up[x] = all & (nan | ~neg) & kOnes;
-          down[x] = all & (nan | neg) & kOnes;
-          a[x] &= ~all;
-        }
+          for (int i = 0; i < 4; ++i) sc[i] *= ksc[t][i];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-          u32x4_t sees;
+          f32x4_t acc = {};
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int key = k0 + 16 * (x >> 1) + 4 * q + 2 * (x & 1);
-            sees[x] = (key < seen[rt] ? 0x00003F80u : 0u) | (key + 1 < seen[rt] ? 0x3F800000u : 0u);
-          }
-          const f32x4_t u = mfma16(up, sees, f32x4_t{}), n = mfma16(down, sees, f32x4_t{});
+          for (int ks = 0; ks < A::KS; ++ks) acc = mfma16(a[ks], qf[rt][ks], acc);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) O[rt][d][i] += (u[i] > 0.0f ? INFINITY : 0.0f) + (n[i] > 0.0f ? -INFINITY : 0.0f);
+          for (int i = 0; i < 4; ++i) s[rt][4 * t + i] = acc[i] * sc[i];
         }
       }
+      load_k(next, pages, hint);
+      if (cap > 0.0f) {
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) O[rt][d] = mfma16(a, pf[rt], O[rt][d]);
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s[rt][e] = fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[rt][e])), cap2);
+      }
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int key = k0 + 16 * (e >> 2) + 4 * q + (e & 3);
+          const bool bad = e < 4 ? bad0 : bad1;
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+            if (bad || key >= seen[rt]) s[rt][e] = -INFINITY;
+        }
+      }
+      u32x4_t pf[RT];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        float mx = s[rt][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[rt][e]);
+        // The maximum is raised, and what was summed rescaled, only where a score passes it by 2^8.
+        if (__any(mx > M[rt] + 8.0f)) {
+          const float mn = fmaxf(M[rt], quad_max(mx)), f = __builtin_amdgcn_exp2f(M[rt] - mn);
+          M[rt] = mn;
+          L[rt] *= f;
+#pragma unroll
+          for (int d = 0; d < A::DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) O[rt][d][i] *= f;
+        }
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          w[e] = __builtin_amdgcn_exp2f(s[rt][e] - M[rt]);
+          L[rt] += w[e];
+          if constexpr (CODE != CACHE_BF16) {
+            w[e] *= vsc[e >> 2][e & 3];
+          }
+        }
+        if (CODE != CACHE_BF16 && masked)   // whatever the scale of a hidden row holds
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[e] = s[rt][e] == -INFINITY ? 0.0f : w[e];
+        pf[rt] = u32x4_t{pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7])};
+      }
+      // O^T += V^T P^T
+      auto values = [&](int d) {
+        u32x4_t a;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          if constexpr (CODE == CACHE_I8) {
+            a[x] = pack_bf16x2((float)(int8_t)(vf[2 * x][d / 4] >> (8 * (d % 4))), (float)(int8_t)(vf[2 * x + 1][d / 4] >> (8 * (d % 4))));
+          } else if constexpr (CODE == CACHE_E4M3) {
+            const uint32_t e0 = d % 4 / 2 ? codes_bf16<CODE, 1>(vf[2 * x][d / 4]) : codes_bf16<CODE, 0>(vf[2 * x][d / 4]);
+            const uint32_t e1 = d % 4 / 2 ? codes_bf16<CODE, 1>(vf[2 * x + 1][d / 4]) : codes_bf16<CODE, 0>(vf[2 * x + 1][d / 4]);
+            a[x] = __builtin_amdgcn_perm(e1, e0, d % 2 ? 0x07060302u : 0x05040100u);
+          } else {
+            a[x] = __builtin_amdgcn_perm(vf[2 * x + 1][d / 2], vf[2 * x][d / 2], d % 2 ? 0x07060302u : 0x05040100u);
+          }
+        }
+        return a;
+      };
+      // MIXED: where rows of a step see different keys, an infinity or a NaN must not reach a row that does not see it (0 times
+      // it would be NaN).  Such values are left out of the product; rows that see them are found by a product of ones.
+      bool spoiled = false;
+      if (MIXED && masked) {
+        constexpr uint32_t kExp = CODE == CACHE_BF16 ? 0x7F807F80u : 0x7F7F7F7Fu, kOne = CODE == CACHE_BF16 ? 0x00800080u : 0x01010101u;
+        uint32_t x = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int w = 0; w < A::VW; ++w) x |= (vf[i][w] & kExp) + kOne;
+        spoiled = __any((x & (CODE == CACHE_BF16 ? 0x80008000u : 0x80808080u)) != 0);
+      }
+#pragma unroll
+      for (int d = 0; d < A::DT; ++d) {
+        u32x4_t a = values(d);
+        if (MIXED && spoiled) {
+          constexpr uint32_t kOnes = 0x3F803F80u;   // 1, 1
+          u32x4_t up, down;                         // ones for + infinity and NaN, and for - infinity and NaN
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t all = ((((a[x] & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xFFFFu;   // not finite
+            const uint32_t nan = ((((a[x] & 0x007F007Fu) + 0x007F007Fu) >> 7) & 0x00010001u) * 0xFFFFu;
+            const uint32_t neg = ((a[x] >> 15) & 0x00010001u) * 0xFFFFu;
+            up[x] = all & (nan | ~neg) & kOnes;
+            down[x] = all & (nan | neg) & kOnes;
+            a[x] &= ~all;
+          }
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            u32x4_t sees;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const int key = k0 + 16 * (x >> 1) + 4 * q + 2 * (x & 1);
+              sees[x] = (key < seen[rt] ? 0x00003F80u : 0u) | (key + 1 < seen[rt] ? 0x3F800000u : 0u);
+            }
+            const f32x4_t u = mfma16(up, sees, f32x4_t{}), n = mfma16(down, sees, f32x4_t{});
+#pragma unroll
+            for (int i = 0; i < 4; ++i) O[rt][d][i] += (u[i] > 0.0f ? INFINITY : 0.0f) + (n[i] > 0.0f ? -INFINITY : 0.0f);
+          }
+        }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) O[rt][d] = mfma16(a, pf[rt], O[rt][d]);
+      }
+      load_v(next, pages, hint);
     }
-    load_v(next, pages);
-  }
+  };
+  if (ONCE && read_past((int64_t)p.B * len, p.Hk, D, CODE == CACHE_BF16)) walk(std::integral_constant<int, 2>{});
+  else walk(std::integral_constant<int, 0>{});
 
   // The waves' results meet in LDS.  A lane holds d (4 q + i) D / 16 + t of row c: D / 4 neighbouring ones.
   float* const so = reinterpret_cast<float*>(smem);
@@ -493,25 +536,20 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
   }
 }
 
-// How a call is cut.  A part costs its start, a partial result and its place in the join, 4 to 5 us beside a call in one part, so there
-// are only as many as the chip wants waves, each of 256 or 384 keys at least.  The share of the workgroups that fit the chip at
-// once, and the keys, are those with which 150 random calls (1 to 64 sequences, 64 to 16384 keys, 1 to 64 heads, measured with 1 to 48
-// parts each) are 3 % slower than with their best cut on average, 33 % at worst.  For instance (us; parts 1, 4, 8, 16, 32):
+// How a call is cut: as many parts as the widest sequence that its table allows would take, and no more workgroups than a share
+// of those that fit the chip at once.  So one long sequence in a batch of many short ones is cut into few parts.  For instance
+// (us; parts 1, 4, 8, 16, 32):
 //     1 x 4 key heads of 8 heads, 2944 keys, bf16, d 128        22   11  8.8  8.8
 //     2 x 8 of 8, 9728 keys, int8, d 128                        78   26   17   16   20
 //     40 x 8 of 4, 2176 keys, int8, d 128                       39   40   46   67
 //     33 x 4 of 4, 6 queries, 6912 keys, int8, d 64             70   30   32   45   92
 // Eight waves a workgroup in place of four were 1.4 % faster at their best over all calls, 20 % for some.
 struct PagedPlan {
-  int rt, nrb, parts;
+  int rt, nrb, parts, few;   // few: CUs a block
   bool once;
 };
 constexpr size_t kCounterBytes = CF_PAGED_WS_HEADER_BYTES;
 constexpr int kMaxParts = 64, kCUs = 256;
-// Bytes of the cache from which its lines are not kept: the last-level cache has 256 MB, and a call over more finds little of
-// it there next time (215 MB: 48.3 -> 46.3 us so; 98 MB in it: 19.8 -> 20.7).
-constexpr int64_t kOnceBytes = 192 << 20;
-
 PagedPlan make_plan(const PagedParams& p) {
   const int64_t R = (int64_t)(p.H / p.Hk) * p.Lq;
   PagedPlan pl;
@@ -519,14 +557,16 @@ PagedPlan make_plan(const PagedParams& p) {
   pl.nrb = (int)((R + 16 * pl.rt - 1) / (16 * pl.rt));
   const int64_t blocks = (int64_t)p.B * p.Hk * pl.nrb, keys = (int64_t)p.pages << p.c.shift, rows = (int64_t)p.B * p.Hk * R;
   const bool bf16 = p.c.code == CACHE_BF16;
-  pl.once = pl.nrb == 1 && 2 * (int64_t)p.B * p.Hk * keys * (bf16 ? 2 * p.d : p.d + 4) > kOnceBytes;
+  pl.once = pl.nrb == 1 && read_past(p.B * keys, p.Hk, p.d, bf16);
   const int resident = kCUs * (p.d == 128 ? (pl.rt == 1 ? 3 : 2) : (pl.rt == 1 ? 5 : 3));   // workgroups, by registers
   const double share = bf16 && p.d == 128 && pl.rt == 1 ? 0.35 : 0.7;
-  const int64_t few_keys = pl.rt == 1 ? 256 : 384;
-  int64_t parts = std::min<int64_t>({kMaxParts, (int64_t)(resident * share) / blocks, keys / few_keys});
+  const int64_t steps = (keys + kStepKeys - 1) / kStepKeys;
+  const int64_t most = steps <= (p.d == 128 ? kOneSteps<128> : kOneSteps<64>) ? 1 : (int64_t)std::sqrt((double)steps * (2.0 / pl.rt));
+  int64_t parts = std::min<int64_t>({kMaxParts, (int64_t)(resident * share) / blocks, most});
   parts = std::min<int64_t>(parts, ((int64_t)1 << 30) / (rows * (p.d + 2) * 4));   // the partial results are addressed in 32 bits
   if (blocks > (int64_t)kCounterBytes / 4) parts = 1;
   pl.parts = (int)std::max<int64_t>(1, parts);
+  pl.few = (int)std::max<int64_t>(1, kCUs / blocks);
   return pl;
 }
 
@@ -535,7 +575,7 @@ hipError_t launch_mixed(PagedParams p, const PagedPlan& pl, hipStream_t st) {
   unsigned* const count = reinterpret_cast<unsigned*>(p.ws);
   if (pl.parts > 1) p.ws += kCounterBytes / 4;
   const int64_t wgs = (int64_t)p.B * p.Hk * pl.nrb * pl.parts;
-  hipLaunchKernelGGL((paged_kernel<D, CODE, RT, ONCE, MIXED>), dim3((unsigned)wgs), dim3(64 * kWaves), 0, st, p, pl.nrb, pl.parts, count);
+  hipLaunchKernelGGL((paged_kernel<D, CODE, RT, ONCE, MIXED>), dim3((unsigned)wgs), dim3(64 * kWaves), 0, st, p, pl.nrb, pl.parts, pl.few, count);
   return hipGetLastError();
 }
 template <int D, int CODE, int RT, bool ONCE>

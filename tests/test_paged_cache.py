@@ -443,6 +443,41 @@ def test_paged_offsets_pass_32_bits():
 
 
 @gpu
+@pytest.mark.parametrize("code,B,H,Hk,Lq,d", [("bf16", 1, 32, 8, 1, 128), ("int8", 4, 8, 8, 1, 64), ("e4m3", 2, 16, 4, 5, 64), ("bf16", 9, 8, 2, 3, 128),
+                                              ("int8", 1, 16, 2, 12, 128)])
+def test_paged_width_of_the_table_changes_nothing(code, B, H, Hk, Lq, d):
+    """A sequence is cut by its length: under a table as wide as it needs and under one of 65536 keys, the same bits."""
+    g = gen(B + H)
+    for most in (20, 300, 580, 1000, 4096, 9000):
+        Q, cache, table = paged_case(g, B, H, Hk, Lq, most, d, 16, code)
+        lens = torch.randint(1, most + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+        lens[0] = most
+        wide = torch.full((B, 4096), -1, dtype=torch.int32, device="cuda")
+        wide[:, :table.shape[1]] = table
+        O, P = (cf.attention_paged(Q, cache[0], cache[1], t, lens, cache[2], cache[3], causal=Lq > 1) for t in (table, wide))
+        assert torch.equal(O, P), most
+        check_paged(P, Q, cache, code, table, lens, 16, Lq > 1)
+
+
+@gpu
+def test_paged_short_sequences_take_no_workspace():
+    """Up to 300 keys a block is not cut, however wide its table: its partial results are not written."""
+    g = gen(15)
+    for d, Lq in ((64, 1), (64, 6), (128, 1), (128, 6)):
+        Q, cache, table = paged_case(g, 3, 8, 2, Lq, 300, d, 16, "bf16")
+        wide = torch.full((3, 4096), -1, dtype=torch.int32, device="cuda")
+        wide[:, :table.shape[1]] = table
+        lens = torch.tensor([300, 299, 130], dtype=torch.int32, device="cuda")
+        need = cf.cf_attention_paged_workspace(paged_args(code_dtype=cf.CF_BF16, batch=3, H=8, Hk=2, Lq=Lq, d=d, pages=4096))
+        assert need > cf.CF_PAGED_WS_HEADER_BYTES
+        ws = torch.full((need,), 0x5A, dtype=torch.uint8, device="cuda")
+        ws[:cf.CF_PAGED_WS_HEADER_BYTES] = 0
+        O = cf.attention_paged(Q, cache[0], cache[1], wide, lens, causal=Lq > 1, ws=ws)
+        check_paged(O, Q, cache, "bf16", table, lens, 16, Lq > 1)
+        assert not ws[:cf.CF_PAGED_WS_HEADER_BYTES].any() and bool((ws[cf.CF_PAGED_WS_HEADER_BYTES:] == 0x5A).all())
+
+
+@gpu
 def test_paged_repeatable_own_workspace_and_streams():
     """The same bits again, from a workspace of the caller's own and on another stream; counters are left zero."""
     g = gen(6)
