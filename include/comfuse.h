@@ -610,7 +610,7 @@ cf_status cf_cache_read(const cf_cache_read_args* a, void* hip_stream);
  * lens[b] are not read, and rows at and behind it not used, whatever they hold; nor does a row that
  * causal hides from a query reach it.  1 <= Lq <= 64 (longer parts of a prompt: cf_cache_read and
  * cf_attention_prefix), batch H Lq < 2^24, pages * page <= 2^30.  scale finite and > 0,
- * softcap finite and >= 0 (a capped score is off by up to 2^-21 softcap), both and scale / softcap
+ * softcap finite and >= 0 (a capped score is off by up to 2^-21 softcap, where softcap > 64 by up to 2^-19 of itself), both and scale / softcap
  * below 2^126.  The softmax is exact (running maximum and sum in fp32); its weights, times the
  * value's scale, are rounded to bf16 for the second product.
  * Workspace: cf_attention_paged_workspace() bytes (may be 0), 16-byte aligned:

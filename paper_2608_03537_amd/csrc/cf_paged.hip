@@ -138,7 +138,11 @@ __host__ __device__ constexpr bool read_past(int64_t keys, int Hk, int d, bool b
 // MIXED: rows of a block may see different keys, and a value may be infinite or NaN (a check and products of their own for
 // such a step; kept out of other calls, which the longer code would cost up to 5 %).
 // ONCE: the table has room for so many keys that they may be read past the caches.
-template <int D, int CODE, int RT, bool ONCE, bool MIXED>
+// FAR: a cap beyond kNearCap.  1 - 2 / (1 + exp 2 z) is tanh z but for an ulp or two of 1, so a capped score is off by as much of
+// the cap, which up to kNearCap is below its own error.  Beyond, where |z| is below 1 / 4 the score is z's odd series up to z^7
+// (the next term: 2^-21 of it).  In a kernel of its own: its code beside the other cost short calls 4 %.
+constexpr float kNearCap = 64.0f;
+template <int D, int CODE, int RT, bool ONCE, bool MIXED, bool FAR>
 __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, int nrb, int parts, int few, unsigned* count) {
   using A = PagedShape<D, CODE, RT>;
   __shared__ __attribute__((aligned(16))) char smem[A::LDS];
@@ -184,7 +188,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
     M[rt] = kLowestF32;
     L[rt] = 0.0f;
   }
-  const float cap = p.softcap, sl = (cap > 0.0f ? 2.0f * p.scale / cap : p.scale) * 1.4426950408889634f;
+  const float cap = p.softcap, sl = (cap > 0.0f && !FAR ? 2.0f * p.scale / cap : p.scale) * 1.4426950408889634f;
   const float cap2 = cap * 1.4426950408889634f;
 
   // The pages of a step's two tiles (one where pages hold 32 tokens and more).  Their entries are asked for a step
@@ -299,7 +303,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
       const bool masked = k0 + kStepKeys > first || bad0 || bad1;
       pages = resolve(next, ahead);
       ahead = look_up(next + kWaves);
-      // S^T, in log2 units; with a cap twice its argument first: tanh z = 1 - 2 / (1 + exp 2 z)
+      // S^T, in log2 units; with a cap its 2 z first
       float s[RT][8];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -326,7 +330,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
         }
       }
       load_k(next, pages, hint);
-      if (cap > 0.0f) {
+      if (FAR) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float z2 = s[rt][e] * (2.0f / cap), y = z2 * z2 * 0.12011325347955035f;   // 2 z in log2 units, z^2
+            const float series = s[rt][e] * fmaf(fmaf(fmaf(-17.0f / 315.0f, y, 2.0f / 15.0f), y, -1.0f / 3.0f), y, 1.0f);
+            const float full = fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z2)), cap2);
+            s[rt][e] = y < 0.0625f ? series : full;
+          }
+      } else if (cap > 0.0f) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -557,7 +571,7 @@ PagedPlan make_plan(const PagedParams& p) {
   pl.nrb = (int)((R + 16 * pl.rt - 1) / (16 * pl.rt));
   const int64_t blocks = (int64_t)p.B * p.Hk * pl.nrb, keys = (int64_t)p.pages << p.c.shift, rows = (int64_t)p.B * p.Hk * R;
   const bool bf16 = p.c.code == CACHE_BF16;
-  pl.once = pl.nrb == 1 && read_past(p.B * keys, p.Hk, p.d, bf16);
+  pl.once = pl.nrb == 1 && p.softcap <= kNearCap && read_past(p.B * keys, p.Hk, p.d, bf16);
   const int resident = kCUs * (p.d == 128 ? (pl.rt == 1 ? 3 : 2) : (pl.rt == 1 ? 5 : 3));   // workgroups, by registers
   const double share = bf16 && p.d == 128 && pl.rt == 1 ? 0.35 : 0.7;
   const int64_t steps = (keys + kStepKeys - 1) / kStepKeys;
@@ -570,23 +584,25 @@ PagedPlan make_plan(const PagedParams& p) {
   return pl;
 }
 
-template <int D, int CODE, int RT, bool ONCE, bool MIXED>
-hipError_t launch_mixed(PagedParams p, const PagedPlan& pl, hipStream_t st) {
+template <int D, int CODE, int RT, bool ONCE, bool MIXED, bool FAR>
+hipError_t launch_kernel(PagedParams p, const PagedPlan& pl, hipStream_t st) {
   unsigned* const count = reinterpret_cast<unsigned*>(p.ws);
   if (pl.parts > 1) p.ws += kCounterBytes / 4;
   const int64_t wgs = (int64_t)p.B * p.Hk * pl.nrb * pl.parts;
-  hipLaunchKernelGGL((paged_kernel<D, CODE, RT, ONCE, MIXED>), dim3((unsigned)wgs), dim3(64 * kWaves), 0, st, p, pl.nrb, pl.parts, pl.few, count);
+  hipLaunchKernelGGL((paged_kernel<D, CODE, RT, ONCE, MIXED, FAR>), dim3((unsigned)wgs), dim3(64 * kWaves), 0, st, p, pl.nrb, pl.parts, pl.few,
+                     count);
   return hipGetLastError();
 }
-template <int D, int CODE, int RT, bool ONCE>
-hipError_t launch_once(const PagedParams& p, const PagedPlan& pl, hipStream_t st) {
-  if constexpr (CODE != CACHE_I8)   // (its codes are finite, and a scale is applied to the weights)
-    if (p.causal && p.Lq > 1) return launch_mixed<D, CODE, RT, ONCE, true>(p, pl, st);
-  return launch_mixed<D, CODE, RT, ONCE, false>(p, pl, st);
+template <int D, int CODE, int RT, bool MIXED>
+hipError_t launch_mixed(const PagedParams& p, const PagedPlan& pl, hipStream_t st) {
+  if (p.softcap > kNearCap) return launch_kernel<D, CODE, RT, false, MIXED, true>(p, pl, st);
+  return pl.once ? launch_kernel<D, CODE, RT, true, MIXED, false>(p, pl, st) : launch_kernel<D, CODE, RT, false, MIXED, false>(p, pl, st);
 }
 template <int D, int CODE, int RT>
 hipError_t launch_rt(const PagedParams& p, const PagedPlan& pl, hipStream_t st) {
-  return pl.once ? launch_once<D, CODE, RT, true>(p, pl, st) : launch_once<D, CODE, RT, false>(p, pl, st);
+  if constexpr (CODE != CACHE_I8)   // (its codes are finite, and a scale is applied to the weights)
+    if (p.causal && p.Lq > 1) return launch_mixed<D, CODE, RT, true>(p, pl, st);
+  return launch_mixed<D, CODE, RT, false>(p, pl, st);
 }
 template <int D, int CODE>
 hipError_t launch_code(const PagedParams& p, const PagedPlan& pl, hipStream_t st) {

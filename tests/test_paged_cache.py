@@ -405,6 +405,26 @@ def test_paged_large_scores(code):
 
 
 @gpu
+@pytest.mark.parametrize("code", ["bf16", "int8", "e4m3"])
+@pytest.mark.parametrize("cap", [50.0, 65.0, 200.0, 1e3, 1e6, 1e30])
+def test_paged_caps(cap, code):
+    """Scores of up to hundreds under caps of all sizes: what a cap adds to their error does not grow with it."""
+    g = gen(21)
+    d, page = 128, 32
+    Q, cache, table = paged_case(g, 3, 8, 2, 2, 900, d, page, code, std=5.0)
+    lens = torch.tensor([900, 333, 40], dtype=torch.int32, device="cuda")
+    O = cf.attention_paged(Q, cache[0], cache[1], table, lens, cache[2], cache[3], causal=True, softcap=cap)
+    ref, a = paged64(Q, cache, code, table, lens, page, True, d ** -0.5, cap)
+    longest = max(float(k.norm(dim=-1).max()) for k, _, _ in sequences(cache, code, table, lens, page))
+    most = float(Q.float().norm(dim=-1).max()) * longest * d ** -0.5
+    # as check_paged, but for the cap: 2^-21 of it, and past 64 2^-19 of the score
+    e = 2 * ((d + 2) * U * most + (2.0 ** -21 * cap if cap <= 64 else 2.0 ** -19 * most)) + 2 * 2.0 ** 10 * U
+    top = max(float(v.abs().max()) for _, v, _ in sequences(cache, code, table, lens, page))
+    tol = (2.0 ** -8 * 1.01 + e) * a + e * ref.abs() + 2.0 ** -8 * 1.01 * ref.abs() + table.shape[1] * page * 2.0 ** -118 * top
+    assert bool(((O.to(F64) - ref).abs() <= tol).all())
+
+
+@gpu
 def test_paged_shares_pages():
     """Two sequences on the same pages, the same page twice in one, a shared table row (stride 0)."""
     g = gen(2)
