@@ -394,20 +394,26 @@ __global__ __launch_bounds__(S::NT) void gemm_w4_kernel(GemmW4Params p, uint32_t
   });
 }
 
+// The k that a tile's sums take a scale for: pairs of steps where more than a block is folded (48 x 12288 x 4096 E2M1
+// 13.6 -> 12.3 us) and every group of waves has as many pairs, or nearly.
+inline int w4_fold(int blocks, int KW, int K, int group) {
+  const int pairs = K / 128;
+  if (blocks > 1 && group % 128 == 0 && (pairs % KW == 0 || pairs >= 4 * KW)) return 128;
+  return group % 64 == 0 ? 64 : 32;
+}
+
 template <class S, bool E2M1, class T>
 hipError_t launch_code(const GemmW4Params& p, hipStream_t st) {
   const int64_t wgs = (int64_t)((p.M + S::TM - 1) / S::TM) * ((p.N + S::TN - 1) / S::TN);
   const uint32_t g32 = p.group / 32, mul = g32 == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + g32 - 1) / g32);
-  // Pairs of steps where sums are folded by more than a block (48 x 12288 x 4096 E2M1 13.6 -> 12.3 us) and every group of
-  // waves has as many pairs, or nearly.
+  const int fold = w4_fold(S::BM * S::BN, S::KW, p.K, p.group);
   if constexpr (S::BM * S::BN > 1) {
-    const int pairs = p.K / 128;
-    if (p.group % 128 == 0 && (pairs % S::KW == 0 || pairs >= 4 * S::KW)) {
+    if (fold == 128) {
       hipLaunchKernelGGL((gemm_w4_kernel<S, E2M1, 128, T>), dim3((unsigned)wgs), dim3(S::NT), 0, st, p, mul);
       return hipGetLastError();
     }
   }
-  if (p.group % 64 == 0) hipLaunchKernelGGL((gemm_w4_kernel<S, E2M1, 64, T>), dim3((unsigned)wgs), dim3(S::NT), 0, st, p, mul);
+  if (fold == 64) hipLaunchKernelGGL((gemm_w4_kernel<S, E2M1, 64, T>), dim3((unsigned)wgs), dim3(S::NT), 0, st, p, mul);
   else hipLaunchKernelGGL((gemm_w4_kernel<S, E2M1, 32, T>), dim3((unsigned)wgs), dim3(S::NT), 0, st, p, mul);
   return hipGetLastError();
 }

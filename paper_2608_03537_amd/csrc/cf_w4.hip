@@ -27,13 +27,13 @@ struct Cost {
   double step, start, once, busy;
 };
 struct Form {
-  int tm, tn, threads;
+  int tm, tn, threads, blocks, groups;   // blocks of a wave, groups of waves
   Cost cost[2];
 };
 constexpr int kCUs = 256;
 template <class S>
 constexpr Form form_of(Cost int4, Cost e2m1) {
-  return {S::TM, S::TN, S::NT, {int4, e2m1}};
+  return {S::TM, S::TN, S::NT, S::BM * S::BN, S::KW, {int4, e2m1}};
 }
 template <class... S>
 constexpr int count_of(W4Tiles<S...>) { return (int)sizeof...(S); }
@@ -172,7 +172,8 @@ hipError_t launch_gemm_w4(const GemmW4Params& p, hipStream_t st) {
 
 void gemm_w4_form(const GemmW4Params& p, char* text, size_t bytes) {
   const Form& f = kForms[choose_form(p)];
-  snprintf(text, bytes, "%d x %d tiles of %d threads, scales every %d", f.tm, f.tn, f.threads, p.group % 64 == 0 ? 64 : 32);
+  snprintf(text, bytes, "%d x %d tiles of %d threads, scales every %d", f.tm, f.tn, f.threads,
+           w4_fold(f.blocks, f.groups, p.K, p.group));
 }
 
 hipError_t launch_w4_pack(int N, int K, const uint8_t* codes, int64_t ldc, uint8_t* tiles, hipStream_t st) {

@@ -282,6 +282,52 @@ def test_w4_every_tile(tile, K, group, code, sdt):
         check_w4(cf.gemm_w4(A, tiles, s, code=code, bias=bias, out_dtype=F32), A, tiles, s, code, bias)
 
 
+# Groups of 128 t: pairs of steps of 64 k share a scale where a tile has more than a block and its groups of waves (8, 4 or 1)
+# have as many pairs, or four each at least; else every step has its own.
+PAIRED = {"16 x 64": 8, "32 x 64": 8, "64 x 32": 8, "64 x 64": 4, "64 x 128": 4, "128 x 128": 1}
+PAIR_K = [(640, 128), (1024, 128), (2176, 128), (2432, 128), (2560, 512), (4224, 128), (4480, 640), (4992, 128)]
+
+
+def shares(tile, K):
+    """Whether the groups of waves have equal numbers of pairs, unequal ones, or (None) steps."""
+    groups, pairs = PAIRED.get(tile, 0), K // 128
+    return None if not groups or pairs % groups and pairs < 4 * groups else "unequal" if pairs % groups else "equal"
+
+
+def pair_form(M, N, K, group, code):
+    return cf.cf_gemm_w4_form(w4_args(M=M, N=N, K=K, group=group, lda=K, lds=N, w_dtype=cf._CODES4[code], ldc=-(-N // 8) * 8))
+
+
+def test_w4_form_says_what_a_scale_is_for():
+    """The form's last word is the k of a scale: 32, 64, or 128 for pairs of steps."""
+    seen = set()
+    for K, group in TILE_K + PAIR_K:
+        for M in (1, 8, 13, 32, 48, 64, 90, 127, 300, 700, 1100):
+            for N in (33, 600, 2100, 4100, 8200, 16390):
+                for code in VALUES:
+                    tile, rest = pair_form(M, N, K, group, code).split(" tiles of ")
+                    share = shares(tile, K) if group % 128 == 0 else None
+                    every = 128 if share else 64 if group % 64 == 0 else 32
+                    assert rest.endswith(f"scales every {every}"), (tile, rest, K, group)
+                    seen.add((tile, every, share))
+    for tile in TILES:
+        assert {e for t, e, _ in seen if t == tile} == ({32, 64, 128} if PAIRED.get(tile, 0) else {32, 64}), tile
+    for tile, groups in PAIRED.items():
+        assert (tile, 128, "equal") in seen and (groups == 1 or (tile, 128, "unequal") in seen), tile
+
+
+@gpu
+@pytest.mark.parametrize("K,group", PAIR_K)
+@pytest.mark.parametrize("tile", sorted(PAIRED))
+@pytest.mark.parametrize("code,sdt", [("int4", BF16), ("e2m1", F32)])
+def test_w4_pairs(tile, K, group, code, sdt):
+    """Every tile of two blocks and more with equal and unequal shares of pairs, and with fewer than it takes pairs for."""
+    g = gen(K)
+    for M, N in tile_sizes(tile, K, group, code):
+        A, tiles, s, bias = make(g, M, N, K, group, code, sdt, bias=True)
+        check_w4(cf.gemm_w4(A, tiles, s, code=code, bias=bias, out_dtype=F32), A, tiles, s, code, bias)
+
+
 # ---------------------------------------------------------------- refusals (no GPU)
 A_, B_, C_, D_, E_ = (0x7F0000000000 + 0x100000 * i for i in range(5))
 
