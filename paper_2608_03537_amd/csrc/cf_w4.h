@@ -23,8 +23,6 @@ namespace cf {
 
 namespace {
 
-typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2_t;
-
 template <int ACT>
 __device__ __forceinline__ float act_w4(float x) {
   if constexpr (ACT == ACT_GELU) return gelu_erf(x);
@@ -262,9 +260,7 @@ __global__ __launch_bounds__(S::NT) void gemm_w4_kernel(GemmW4Params p, uint32_t
         });
       });
     }
-    // Reads and loads of steps that there are not: none may land after their registers and stages have a new use.
-    static_for<0, S::BM>([&](auto a_t) { lgkm_wait<0>(xf[0][decltype(a_t)::value]); });
-    wait_vmcnt<0>();
+    static_for<0, S::BM>([&](auto a_t) { lgkm_wait<0>(xf[0][decltype(a_t)::value]); });   // (of a step that there is not)
 #pragma unroll
     for (int a = 0; a < S::BM; ++a)
 #pragma unroll
@@ -336,6 +332,7 @@ __global__ __launch_bounds__(S::NT) void gemm_w4_kernel(GemmW4Params p, uint32_t
       }
     }
   }
+  wait_vmcnt<0>();   // loads into LDS of steps that there are not, in either loop: none may land when its stage has a new use
   __syncthreads();
   // Sums to LDS, KW planes of TM rows; then a thread adds the planes of 8 columns of a row at a time.
   float* const out = reinterpret_cast<float*>(smem + grp * S::TM * S::PITCH);
