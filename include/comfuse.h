@@ -492,7 +492,10 @@ cf_status cf_w4_pack(int64_t N, int64_t K, const void* codes, int64_t ldc, void*
  * A M x K bf16, W in tiles as above, s K / group rows of N (s_dtype F32 or
  * BF16, lds elements apart), bias fp32 [N] or NULL, C M x N in out_dtype F32
  * or BF16.  The codes enter the products as exact bf16 values, the sums of a
- * group and over the groups and the scales are fp32: no weight is rounded.
+ * group and over the groups and the scales are fp32: no weight is rounded.  I4
+ * codes enter as 16 w and their scales as s / 16, which is the same to the last bit
+ * while scales are 0 or 2^-122 and more in magnitude; a group's sum of A w whose
+ * magnitude, or that of a part of it, reaches 2^124 may come out infinite or NaN.
  * Shape rules: group % 32 == 0, K % group == 0, K <= 2^20, 1 <= N <= 2^20,
  * M * N <= 2^37; columns between N and ldc are left as they are.  act as in cf_gemm_i8.
  * ------------------------------------------------------------------------ */

@@ -181,6 +181,25 @@ def test_w4_all_codes_exact():
 
 
 @gpu
+@pytest.mark.parametrize("M", [64, 200, 1100])
+def test_w4_ends_of_the_range(M):
+    """Scales down to 2^-122 and sums of a group up to just below 2^124, exact: one product a group, powers of two."""
+    K, N = 256, 64
+    c = (torch.arange(N)[:, None] + torch.arange(K)[None]) % 16
+    tiles = cf.w4_pack((c[:, 0::2] | c[:, 1::2] << 4).to(torch.uint8).cuda())
+    A = torch.zeros((M, K), dtype=BF16, device="cuda")
+    at = torch.arange(M, device="cuda")
+    for code in VALUES:
+        w = torch.tensor(VALUES[code])[c].t().double().cuda()[at % K]
+        for a, scale in ((2.0 ** 120, 2.0 ** -122), (2.0 ** 120, 2.0 ** 4), (1.0, 2.0 ** -122), (1.0, 1.375 * 2.0 ** -122), (-(2.0 ** 100), 2.0 ** -100)):
+            A.zero_()
+            A[at, at % K] = a
+            for group in (32, 128):
+                C = cf.gemm_w4(A, tiles, torch.full((K // group, N), scale, device="cuda"), code=code, out_dtype=F32)
+                assert torch.equal(C.double(), a * w * scale), (code, a, scale, group)
+
+
+@gpu
 def test_w4_of_quantised_weights():
     """w4_quant and gemm_w4 together: near the product with the weights themselves."""
     g = gen(5)
