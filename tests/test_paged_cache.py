@@ -182,6 +182,31 @@ def test_write_more_tasks_than_a_grid():
     assert torch.equal(vc.view(-1, 64)[:T], k[:, 0]) and not kc.view(-1, 64)[T:].any()
 
 
+@gpu
+@pytest.mark.parametrize("code", ["bf16", "int8"])
+def test_write_waves_take_several_tokens(code):
+    """As many tokens as a call may have, several for every wave of a full grid: each is turned by its own angles."""
+    T = (1 << 24) - 5
+    k = torch.zeros((T, 1, 64), dtype=BF16, device="cuda")
+    k[:, 0, 0] = 1.0
+    pos = torch.arange(T, dtype=torch.int32, device="cuda") % 1009        # differ between the tokens of a wave
+    freq = torch.full((8,), 1e-3, device="cuda")
+    kc, vc, ks, vs = cf.cache_pages(-(-T // 1024), 1, 1024, 64, code)
+    cf.cache_write(k, k, torch.arange(T, dtype=torch.int32, device="cuda"), kc, vc, ks, vs, pos=pos, freq=freq)
+    angle = torch.arange(1009, device="cuda").to(F64) * freq[0].to(F64)
+    want = torch.zeros((1009, 64), device="cuda")
+    want[:, 0], want[:, 8] = torch.cos(angle).float(), torch.sin(angle).float()
+    at = pos.long()
+    if code == "bf16":
+        assert torch.equal(kc.view(-1, 64)[:T], want.to(BF16)[at]) and torch.equal(vc.view(-1, 64)[:T], k[:, 0])
+    else:
+        c, s = quantise32(want.cpu(), code)
+        assert torch.equal(kc.view(-1, 64)[:T], c.cuda()[at]) and torch.equal(ks.view(-1)[:T], s.cuda()[at])
+        assert bool((vc.view(-1, 64)[:T, 0] == 127).all()) and not vc.view(-1, 64)[:, 1:].any()
+        assert not ks.view(-1)[T:].any() and not vs.view(-1)[T:].any()
+    assert not kc.view(-1, 64)[T:].any() and not vc.view(-1, 64)[T:].any()
+
+
 # ---------------------------------------------------------------- filled caches
 def fill_pages(g, n, Hk, page, d, code, major="heads", std=1.0):
     kc, vc, ks, vs = new_cache(n, Hk, page, d, code, major)
@@ -262,6 +287,24 @@ def test_read(B, Hk, S, d, page, pages, major, code):
     assert bool((out[0]._base[..., d:] == 7).all())
     K2, _ = cf.cache_read(cache[0], cache[1], table, lens, cache[2], cache[3])
     assert K2.shape == (B, Hk, pages * page, d)
+
+
+@gpu
+@pytest.mark.parametrize("code", ["bf16", "e4m3"])
+def test_read_more_tasks_than_a_grid(code):
+    """More than twice 2^20 groups of 32 rows: workgroups take several, the last rows of the last sequence among them."""
+    g = gen(31)
+    B, S, page, n = 5, 1 << 24, 1024, 7
+    cache = fill_pages(g, n, 1, page, 64, code)
+    table = torch.randint(0, n, (B, S // page), generator=g, device="cuda", dtype=torch.int32)
+    lens = torch.tensor([S, 3, S - 40, 0, S - 1], dtype=torch.int32, device="cuda")
+    K, V = (torch.full((B, 1, S, 64), 7.0, dtype=BF16, device="cuda") for _ in range(2))
+    cf.cache_read(cache[0], cache[1], table, lens, cache[2], cache[3], out=(K, V))
+    for out, rows, scales in ((K, cache[0], cache[2]), (V, cache[1], cache[3])):
+        rows = values(rows, scales, code).float().to(BF16)[:, 0]          # [n, page, 64]
+        for b in range(B):
+            m = int(lens[b])
+            assert torch.equal(out[b, 0, :m], rows[table[b].long()].view(S, 64)[:m]) and bool((out[b, 0, m:] == 7).all())
 
 
 # ---------------------------------------------------------------- attention_paged

@@ -106,6 +106,18 @@ def test_quant(N, K, group, dtype, sdt, code, top):
         assert bool(torch.isin(got[tie & ~bad[..., None]], even).all())
 
 
+@gpu
+@pytest.mark.parametrize("K,group", [(2112, 32), (2560, 512)])
+def test_quant_more_groups_than_a_grid(K, group):
+    """Workgroups take several groups: channels of the start, the middle and the end are those of small calls."""
+    N = 1 << 20
+    W = torch.empty((N, K), dtype=BF16, device="cuda").normal_(generator=gen(K))
+    tiles, s = cf.w4_quant(W, group)
+    for at in (0, N // 2, N - 64):
+        t, u = cf.w4_quant(W[at:at + 64], group)
+        assert torch.equal(tiles[at // 32:at // 32 + 2], t) and torch.equal(s[:, at:at + 64], u)
+
+
 # ---------------------------------------------------------------- the product
 @gpu
 @pytest.mark.parametrize("M,N,K", [
