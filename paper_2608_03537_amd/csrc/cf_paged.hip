@@ -104,12 +104,12 @@ struct Joined {   // running join of parts: maximum, sum, 8 d
 
 // The parts that a block of `steps` steps of 32 keys is cut into, of `most` that are launched.  They go by the length: a table,
 // above all in a captured call, may be far wider than its sequences.  One part more shortens the way over the keys and lengthens
-// the join's, so the best number goes with the root of the keys, and is less where a partial result has more rows; it is less
-// again (0.7) where the parts are more than the CUs (`few`: CUs a block); then as few parts as leave the longest wave its
-// steps.  Up to kOneSteps the way through the workspace, 1 to 3 us, costs more than it gives.  Found with 110 calls (1 to 16
-// sequences, 150 to 8000 keys) under tables of 65536 keys, in 1 to 32 parts each: 15 % faster than parts of 128 keys and more,
-// at best twice as fast; 240 random calls whose tables are at most twice as wide as needed are 5 % faster, 12 % slower at
-// worst.  For instance (us; parts 1, 2, 4, 8, 16, 32):
+// the join's, so the best number goes with the root of the keys, and is less where a partial result has more rows.  Of these,
+// as few as leave the longest wave its steps; where there are more than give every CU a workgroup (`each_cu`), a multiple of
+// that, for 0.8 of the root.  Up to kOneSteps the way through the workspace, 1 to 3 us, costs more than it gives.  Found with
+// 110 calls (1 to 16 sequences, 150 to 8000 keys) under tables of 65536 keys, in 1 to 32 parts each: in 0.84 of the time that
+// parts of 128 keys and more take, half of it at best; 240 random calls whose tables are at most twice as wide as needed take
+// 0.94 of it, 1.11 at worst.  For instance (us; parts 1, 2, 4, 8, 16, 32):
 //     4 x 8 key heads of 4 heads, 350 keys, bf16, d 128       7.8  8.0  7.2  8.1  8.1  8.2
 //     8 x 8 of 4, 700 keys, int8, d 64                        9.6  9.3  8.9  9.5   12   12
 //     1 x 8 of 4, 6 queries, 2500 keys, bf16, d 128            38   25   17   15   17   24
@@ -117,12 +117,15 @@ struct Joined {   // running join of parts: maximum, sum, 8 d
 template <int D>
 constexpr int kOneSteps = D == 128 ? 14 : 18;
 template <int D, int RT>
-__device__ __forceinline__ int parts_of(int steps, int most, int few) {
+__device__ __forceinline__ int parts_of(int steps, int most, float each_cu) {
   if (steps <= kOneSteps<D>) return 1;
   auto whole = [](float x) { return __builtin_amdgcn_readfirstlane((int)x); };
   const float root = __builtin_amdgcn_sqrtf((float)steps * (2.0f / RT));
-  int n = max(1, min(most, whole(root)));
-  if (n > few) n = max(few, min(most, whole(root * 0.7f)));
+  const int n = max(1, min(most, whole(root)));
+  if ((float)n > each_cu) {
+    const int times = max(1, whole(root * 0.8f * __builtin_amdgcn_rcpf(each_cu)));
+    return max(1, min(most, whole((float)times * each_cu + 0.01f)));
+  }
   const int each = whole((float)(steps - 1) * __builtin_amdgcn_rcpf((float)(n * kWaves))) + 1;   // steps of the longest wave
   return min(n, whole((float)(steps - 1) * __builtin_amdgcn_rcpf((float)(each * kWaves))) + 1);
 }
@@ -143,20 +146,24 @@ __host__ __device__ constexpr bool read_past(int64_t keys, int Hk, int d, bool b
 // (the next term: 2^-21 of it).  In a kernel of its own: its code beside the other cost short calls 4 %.
 constexpr float kNearCap = 64.0f;
 template <int D, int CODE, int RT, bool ONCE, bool MIXED, bool FAR>
-__global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, int nrb, int parts, int few, unsigned* count) {
+__global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, int nrb, int parts, int turn, float each_cu, unsigned* count) {
   using A = PagedShape<D, CODE, RT>;
   __shared__ __attribute__((aligned(16))) char smem[A::LDS];
   __shared__ int last_one;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, q = lane >> 4;
   // Parts go slowest through the grid: a sequence may have fewer than are launched, and those in use then lie beside each other,
-  // on all XCDs (parts beside each other: 4 sequences of 1000 int8 keys, 32 heads of 8, under a wide table 9.1 -> 10.3 us).
+  // on all XCDs (parts beside each other: 4 sequences of 1000 int8 keys, 32 heads of 8, under a wide table 9.1 -> 10.3 us).  Each
+  // part begins with other sequences (`turn`), or a CU would have the parts of one (8 x 32 heads of 8, 7759 to 14909 int8 keys
+  // 46 -> 40 us).
   int task = blockIdx.x;
   const int rb = task % nrb;
   task /= nrb;
   const int hk = task % p.Hk;
   task /= p.Hk;
-  const int z = task / p.B, b = (task % p.B + z * (p.B / parts)) % p.B;
+  const int z = task / p.B;
+  int b = task % p.B + z * turn;
+  if (b >= p.B) b -= p.B;
   const int G = p.H / p.Hk, R = G * p.Lq, m0 = rb * A::ROWS;
 
   // Q fragments (on their way while the length is looked up).  16-byte pieces of a row of codes hold two steps' d of a lane.
@@ -174,7 +181,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
   const int last = paged_seen(p, len, (min(m0 + A::ROWS, R) - 1) / G);   // keys that some row sees
   const int first = paged_seen(p, len, m0 / G);                          // ... that every row sees
   const int steps = (last + kStepKeys - 1) / kStepKeys;
-  const int np = parts_of<D, RT>(steps, parts, few);                          // parts of this block in use
+  const int np = parts_of<D, RT>(steps, parts, each_cu);                          // parts of this block in use
   if (z >= np) return;
   const int j0 = (int)((uint32_t)steps * z / np), j1 = (int)((uint32_t)steps * (z + 1) / np);   // (steps <= 2^25, np <= 64)
   int seen[RT];
@@ -559,7 +566,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(PagedParams p, in
 //     33 x 4 of 4, 6 queries, 6912 keys, int8, d 64             70   30   32   45   92
 // Eight waves a workgroup in place of four were 1.4 % faster at their best over all calls, 20 % for some.
 struct PagedPlan {
-  int rt, nrb, parts, few;   // few: CUs a block
+  int rt, nrb, parts;
+  float each_cu;   // parts of a block with which every CU has a workgroup
   bool once;
 };
 constexpr size_t kCounterBytes = CF_PAGED_WS_HEADER_BYTES;
@@ -580,7 +588,7 @@ PagedPlan make_plan(const PagedParams& p) {
   parts = std::min<int64_t>(parts, ((int64_t)1 << 30) / (rows * (p.d + 2) * 4));   // the partial results are addressed in 32 bits
   if (blocks > (int64_t)kCounterBytes / 4) parts = 1;
   pl.parts = (int)std::max<int64_t>(1, parts);
-  pl.few = (int)std::max<int64_t>(1, kCUs / blocks);
+  pl.each_cu = (float)kCUs / (float)blocks;
   return pl;
 }
 
@@ -589,7 +597,7 @@ hipError_t launch_kernel(PagedParams p, const PagedPlan& pl, hipStream_t st) {
   unsigned* const count = reinterpret_cast<unsigned*>(p.ws);
   if (pl.parts > 1) p.ws += kCounterBytes / 4;
   const int64_t wgs = (int64_t)p.B * p.Hk * pl.nrb * pl.parts;
-  hipLaunchKernelGGL((paged_kernel<D, CODE, RT, ONCE, MIXED, FAR>), dim3((unsigned)wgs), dim3(64 * kWaves), 0, st, p, pl.nrb, pl.parts, pl.few,
+  hipLaunchKernelGGL((paged_kernel<D, CODE, RT, ONCE, MIXED, FAR>), dim3((unsigned)wgs), dim3(64 * kWaves), 0, st, p, pl.nrb, pl.parts, p.B / pl.parts, pl.each_cu,
                      count);
   return hipGetLastError();
 }
