@@ -10,7 +10,7 @@
 // the formula in fp32, bit for bit.
 //
 // Read: the rows of a sequence gathered from its pages; memory bounds it (16 sequences of 4096 to 8192 int8 rows of 8 heads,
-// d 128: 108 us, 5.4 TB/s; with a row's loads and stores one after the other 142).
+// d 128: 109 to 114 us, 5.6 to 5.4 TB/s; with a row's loads and stores one after the other 142).
 #include <algorithm>
 
 #include "cf_device.h"

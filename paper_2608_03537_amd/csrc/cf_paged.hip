@@ -13,11 +13,16 @@
 // D / 16 neighbouring ones of each (16 lanes a whole row), and picking the t-th of each, in the step that makes
 // bf16 of the codes, gives the operand for dimensions t, t + D / 16, ...: the transposition costs nothing.
 //
+// P, times the scale of the value, is rounded to bf16, the type in which the MFMA takes it beside V's exact codes: off by 2^-9 of
+// a weight, while the output is rounded to bf16 as well.  Against 64 bits the result is off by 0.0021 to 0.0024 in relative norm,
+// 0.0017 of which is the output's rounding.  The sum of the weights is taken before it, in fp32, as maxima and O are.
+//
 // Bound.  bf16: memory, 6.05 TB/s where the cache is larger than the last-level one (a streaming read with no work
 // reaches 6.9).  int8: the conversion of the codes, 3 vector operations for two, with the softmax; three waves a SIMD
-// keep 5.4 TB/s (64 sequences of up to 8192 keys, 8 key heads of 4, 832 MB: 155 us).  Several queries and capped scores: the
-// softmax (16 sequences of 4 key heads of 4, 5 queries, 4095 E4M3 keys of 64: 15.1 us).  One sequence: its start, the
-// parts' way through the workspace and the launch (4096 bf16 keys, 8 key heads of 4: 9.2 us).
+// keep 5.3 TB/s (64 sequences of up to 8192 keys, 8 key heads of 4, 832 MB: 156 us).  Several queries and capped scores: the
+// softmax (16 sequences of 4 key heads of 4, 5 queries, 4095 E4M3 keys of 64: 15.8 us).  One sequence: its start, the
+// parts' way through the workspace and the launch (4096 bf16 keys, 8 key heads of 4: 10.0 us).  More than 32 rows a key head:
+// every 32 read and convert the keys and values again.
 #include <algorithm>
 #include <cmath>
 #include <cstdio>
@@ -580,7 +585,7 @@ PagedPlan make_plan(const PagedParams& p) {
   const int64_t blocks = (int64_t)p.B * p.Hk * pl.nrb, keys = (int64_t)p.pages << p.c.shift, rows = (int64_t)p.B * p.Hk * R;
   const bool bf16 = p.c.code == CACHE_BF16;
   pl.once = pl.nrb == 1 && p.softcap <= kNearCap && read_past(p.B * keys, p.Hk, p.d, bf16);
-  const int resident = kCUs * (p.d == 128 ? (pl.rt == 1 ? 3 : 2) : (pl.rt == 1 ? 5 : 3));   // workgroups, by registers
+  const int resident = kCUs * (p.d == 128 ? (pl.rt == 1 ? 3 : 2) : (pl.rt == 1 ? 5 : 3));   // workgroups, by registers (without MIXED)
   const double share = bf16 && p.d == 128 && pl.rt == 1 ? 0.35 : 0.7;
   const int64_t steps = (keys + kStepKeys - 1) / kStepKeys;
   const int64_t most = steps <= (p.d == 128 ? kOneSteps<128> : kOneSteps<64>) ? 1 : (int64_t)std::sqrt((double)steps * (2.0 / pl.rt));

@@ -7,9 +7,10 @@
 // MFMAs from zero, then added to the tile's sums with the group's scale, one fused step in fp32: a lane holds one
 // channel of a block, so the scale is one value a lane.
 //
-// Bound.  One token: the launch (1 x 4096 x 4096 int4, 8.7 MB: 6.6 us, in a loop of calls 7.2).  Tens: the conversion and the
-// folds of the one wave that a SIMD has (48 x 12288 x 4096 E2M1, 28 MB: 12.35 us, 2.2 TB/s).  Thousands: the issue of MFMAs and
-// conversions, and power (4096 x 4096 x 4096 int4: 148 us, 0.93 PFLOP/s; the clock falls to 1.7 GHz).
+// Bound.  One token: the launch, and 128 workgroups for 256 CUs with eight steps a wave (1 x 4096 x 4096 int4, 8.7 MB: 6.7 us,
+// in a loop of calls 7.4).  Tens: the conversion and the folds of the one wave that a SIMD has (48 x 12288 x 4096 E2M1, 28 MB:
+// 12.2 us, 2.3 TB/s).  Thousands: the issue of MFMAs and conversions, and power (4096 x 4096 x 4096 int4: 142 to 147 us, 0.97 to
+// 0.93 PFLOP/s; more than eight launches in a row lower the clock to 1.7 GHz and less, and take 171 to 192 us each).
 #pragma once
 
 #include <algorithm>

@@ -11,7 +11,7 @@ namespace {
 // The tiles and their estimated time (us): rounds of 256 workgroups, each `step` for every 64 k (and `busy` times the
 // share of CUs at work) and `start` besides, and `once`; int4, then E2M1.  (The last tile fits a CU twice; two together
 // take as long as one after the other.)  Fitted to 1 to 4096 tokens, 512 to 16384 channels and 512 to 8192 k, groups of 128;
-// for instance (us, in this order; - not measured):
+// for instance (us, in this order; - not measured; single kernels with pauses, at a full clock):
 //     1 x 4096 x 4096 int4       6.8  9.3  7.9  9.9  9.0   13   20    -
 //     1 x 12288 x 4096 int4      9.7  9.9   14   10   16   13   20    -
 //     16 x 12288 x 4096 E2M1      11  8.2   12  8.9   16   11   17    -
